@@ -1,0 +1,420 @@
+"""Performance cases of the decoder layer's path from its projection to the 4-bit store and back.
+
+Four kinds of pass, each one call (or one call and its counterpart) of a layer:
+
+  rope    norms of queries and keys for each head with the position rotation, from the packed projection
+          of a chunk's or an answer's tokens; the values are copied out of the same projection
+  store   a chunk's keys and values into the 4-bit store, and the chunk read back from it
+  recall  the chunks of a segment table from the 4-bit store as bf16 (to refill a bf16 ring)
+  attend  attention of query rows over sink, segments of the 4-bit store and causal tail: a decode step, a
+          short query, a chunk over a ring window of the store
+
+`own` false computes them from elementary torch operations, true by the package's entry points.  Head
+counts, head sizes, sinks and windows are those of the repository's workloads (3B and 7B layers; small
+ones at head size 64).
+"""
+import math
+
+import torch
+
+own = False
+
+# heads (query, key/value, size)
+HEADS = {"3b": (16, 2, 128), "7b": (28, 4, 128), "small": (8, 2, 64)}
+SIGMA_QK = 2.0 ** 0.5    # logits of standard deviation 2
+DEV = "cuda"
+GROUP = 32               # elements that share a scale of the 4-bit store
+WORKSPACE = 48 << 20     # scratch that a program keeps for all its attention calls
+ADJACENT, STRIDED_AXES = 1, 2
+
+
+# ---------------------------------------------------------------- the cases
+
+def _rope(name, model, T, norm, axes, rot, adjacent=False, strided=False, f32_weights=False):
+    return {"name": name, "kind": "rope", "model": model, "T": T, "norm": norm, "axes": axes, "rot": rot,
+            "adjacent": adjacent, "strided": strided, "f32_weights": f32_weights}
+
+
+def _store(name, model, C, slots, H):
+    return {"name": name, "kind": "store", "model": model, "C": C, "slots": slots, "H": H}
+
+
+def _recall(name, model, chunks, lo, hi, top_k):
+    return {"name": name, "kind": "recall", "model": model, "chunks": chunks, "lo": lo, "hi": hi, "top_k": top_k}
+
+
+def _attend(name, model, q_len, tail, chunks, lo, hi, top_k, S=64, lse=False):
+    return {"name": name, "kind": "attend", "model": model, "q_len": q_len, "tail": tail, "chunks": chunks, "lo": lo,
+            "hi": hi, "top_k": top_k, "S": S, "lse": lse, "window": 0}
+
+
+def _window(name, model, C, W, S=64, lse=False):
+    return {"name": name, "kind": "attend", "model": model, "q_len": C, "tail": C, "chunks": 0, "lo": 0, "hi": 0,
+            "top_k": 0, "S": S, "lse": lse, "window": W}
+
+
+def listed():
+    return [
+        # an answer token of the larger model: the smallest call there is
+        _rope("rope_decode_7b", "7b", 1, True, 1, 128),
+        # a single-frame chunk, rotation by time, row and column without norms
+        _rope("rope_frame_3b", "3b", 77, False, 3, 128),
+        # an odd count on a small layer, half of each head rotated in adjacent pairs
+        _rope("rope_small_odd", "small", 333, True, 1, 32, adjacent=True, f32_weights=True),
+        # the large visual chunk, norms and the three position axes dealt out in turn
+        _rope("rope_chunk_7b", "7b", 2048, True, 3, 128, strided=True),
+        # a single-frame chunk into the store, and back
+        _store("store_frame_3b", "3b", 77, 4096, 4001),
+        # the large chunk, across the end of the store's slots
+        _store("store_chunk_7b", "7b", 2048, 18432, 5 * 18432 + 17777),
+        # a few short chunks called back
+        _recall("recall_3b_short", "3b", 64, 64, 320, 8),
+        # 32 of 256 chunks called back for the larger model's ring
+        _recall("recall_7b", "7b", 256, 256, 1024, 32),
+        # an answer token over 32 retrieved chunks
+        _attend("decode_7b", "7b", 1, 64, 256, 256, 1024, 32),
+        # an answer token over all of a long stream
+        _attend("decode_7b_long", "7b", 1, 64, 256, 1024, 1024, 256),
+        # a 32-token query over 32 retrieved chunks (time to first token)
+        _attend("query_7b", "7b", 32, 32, 256, 256, 1024, 32, lse=True),
+        # a visual chunk over a window of the store used as a ring
+        _window("chunk_7b", "7b", 1024, 8192),
+    ]
+
+
+def _log(rng, lo, hi):
+    """A whole number from lo to hi, spread evenly over the logarithm."""
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    case = _draw(rng)
+    case.pop("name")
+    return case
+
+
+def _draw(rng):
+    kind = rng.choice(["rope", "rope", "store", "recall", "decode", "decode", "query", "window"])
+    model = rng.choice(["3b", "7b", "small"])
+    D = HEADS[model][2]
+    if kind == "rope":
+        axes = rng.choice([1, 3])
+        return _rope("", model, _log(rng, 1, 2048), rng.random() < 0.6, axes, rng.choice([D, D, D // 2]),
+                     adjacent=rng.random() < 0.3, strided=axes == 3 and rng.random() < 0.4,
+                     f32_weights=rng.random() < 0.3)
+    if kind == "store":
+        C = _log(rng, 1, 2048)
+        return _store("", model, C, C + rng.randrange(16384), rng.randrange(100000))
+    if kind == "recall":
+        chunks, lo = _log(rng, 4, 256), _log(rng, 1, 512)
+        return _recall("", model, chunks, lo, lo + rng.randrange(512), _log(rng, 1, min(32, chunks)))
+    S, lse = rng.choice([0, 16, 64, 100]), rng.random() < 0.3
+    if kind == "window":
+        return _window("", model, _log(rng, 65, 1024), _log(rng, 128, 8192), S=S, lse=lse)
+    chunks, lo = _log(rng, 2, 256), _log(rng, 1, 512)
+    if kind == "decode":
+        return _attend("", model, 1, 1 + rng.randrange(300), chunks, lo, lo + rng.randrange(512),
+                       _log(rng, 1, chunks), S=S, lse=lse)
+    q_len = _log(rng, 2, 64)
+    return _attend("", model, q_len, q_len + rng.randrange(100), chunks, lo, lo + rng.randrange(512),
+                   _log(rng, 1, min(64, chunks)), S=S, lse=lse)
+
+
+# ---------------------------------------------------------------- inputs
+
+def _normal(g, sigma, *shape):
+    return (torch.randn(*shape, generator=g, device=DEV) * sigma).to(torch.bfloat16)
+
+
+def _quantise(x):
+    """bf16 [n, heads, D] -> (codes uint8 [n, heads, D/2], scales uint8 [n, heads, D/32]) of the 4-bit store."""
+    n, h, d = x.shape
+    x = x.float().reshape(n, h, d // GROUP, GROUP)
+    amax = x.abs().amax(-1)
+    _, e = torch.frexp(amax / 1.75)                        # 2^(e-1) <= amax / 1.75 < 2^e
+    e = torch.where(torch.ldexp(torch.ones_like(amax), e - 1) * 1.75 == amax, e - 1, e)
+    byte = torch.where(torch.isfinite(amax), (e - 2 + 127).clamp(4, 252), 255)
+    u = torch.where(torch.isfinite(amax)[..., None], x / torch.ldexp(torch.ones_like(amax), byte - 127)[..., None], 0)
+    a = u.abs()
+    code = ((a > 0.25).int() + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5)
+            + 8 * torch.signbit(u))
+    code = code.reshape(n, h, d // 2, 2)
+    return (code[..., 0] + 16 * code[..., 1]).to(torch.uint8), byte.to(torch.uint8)
+
+
+def _values(codes, scales):
+    """What codes and scales of the 4-bit store stand for, fp32."""
+    table = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, -0., -.5, -1, -1.5, -2, -3, -4, -6], device=codes.device)
+    n, h, half = codes.shape
+    v = table[torch.stack([codes & 15, codes >> 4], -1).int()].reshape(n, h, half * 2 // GROUP, GROUP)
+    s = torch.ldexp(torch.ones_like(scales, dtype=torch.float32), scales.int() - 127)
+    s = torch.where(scales == 255, torch.nan, s)
+    return (v * s[..., None]).reshape(n, h, half * 2)
+
+
+def _filled(g, sigma, slots, Hkv, D):
+    """A store whose slots hold normal keys or values, in pieces: a long one takes no fp32 copy of its own."""
+    codes = torch.empty(slots, Hkv, D // 2, dtype=torch.uint8, device=DEV)
+    scales = torch.empty(slots, Hkv, D // GROUP, dtype=torch.uint8, device=DEV)
+    for at in range(0, slots, 65536):
+        n = min(65536, slots - at)
+        codes[at:at + n], scales[at:at + n] = _quantise(_normal(g, sigma, n, Hkv, D))
+    return codes, scales
+
+
+def _lengths(case):
+    """Ragged chunk lengths of a store and the chunks that are taken of it: properties of the case, not of the seed."""
+    g = torch.Generator()
+    g.manual_seed(case["chunks"] * 7919 + case["lo"])
+    lens = torch.randint(case["lo"], case["hi"] + 1, (case["chunks"],), generator=g)
+    return lens, torch.randperm(case["chunks"], generator=g)[:case["top_k"]].sort().values
+
+
+def _segments(case):
+    """(store slots, segment starts, segment lengths) on the host."""
+    if W := case.get("window"):                            # a ring as long as the window, its oldest token at 3/8
+        first = 3 * W // 8
+        return W, torch.tensor([first, 0]), torch.tensor([W - first, first])
+    lens, picked = _lengths(case)
+    starts = torch.cumsum(lens, 0) - lens
+    return int(lens.sum()), starts[picked], lens[picked]
+
+
+def _sections(case):
+    half = case["rot"] // 2
+    return [half] if case["axes"] == 1 else [half // 4, half // 4 + half // 8, half - half // 2 - half // 8]
+
+
+def _axis_of_pair(case):
+    """The position axis of each rotated pair."""
+    s = _sections(case)
+    if not case["strided"]:
+        return torch.repeat_interleave(torch.arange(len(s)), torch.tensor(s))
+    i = torch.arange(case["rot"] // 2)                     # axes 1 and 2 take every third pair up to their count
+    return torch.where((i % 3 == 1) & (i < 3 * s[1]), 1, torch.where((i % 3 == 2) & (i < 3 * s[2]), 2, 0))
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    Hq, Hkv, D = HEADS[case["model"]]
+    kind = case["kind"]
+    empty = lambda *s, dtype=torch.bfloat16: torch.empty(*s, dtype=dtype, device=DEV)   # noqa: E731
+    if kind == "rope":
+        T, rot = case["T"], case["rot"]
+        wt = torch.float32 if case["f32_weights"] else torch.bfloat16
+        weights = [(1 + 0.2 * torch.randn(D, generator=g, device=DEV)).to(wt) if case["norm"] else None for _ in "qk"]
+        # a stream that has run for long: far positions in time, a grid in rows and columns
+        p0 = int(torch.randint(0, 1 << 20, (1,), generator=g, device=DEV))
+        t = torch.arange(T, device=DEV)
+        pos = t[None] if case["axes"] == 1 else torch.stack([t // 256, t % 256 // 16, t % 16])
+        return {"kind": kind, "case": case, "qkv": _normal(g, 1.5, T, (Hq + 2 * Hkv) * D), "weights": weights,
+                "positions": (p0 + pos).to(torch.int32).contiguous(),
+                "inv_freq": (1e6 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)).float().to(DEV),
+                "axis": _axis_of_pair(case).to(DEV), "sections": _sections(case) if case["axes"] > 1 else None,
+                "flags": ADJACENT * case["adjacent"] + STRIDED_AXES * case["strided"],
+                "q": empty(T, Hq, D), "k": empty(T, Hkv, D), "v": empty(T, Hkv, D)}
+    if kind == "store":
+        C = case["C"]
+        (k, ks), (v, vs) = (_filled(g, s, case["slots"], Hkv, D) for s in (SIGMA_QK, 1.0))
+        first = case["H"] % case["slots"]
+        n = min(C, case["slots"] - first)
+        return {"kind": kind, "case": case, "k": _normal(g, SIGMA_QK, C, Hkv, D), "v": _normal(g, 1.0, C, Hkv, D),
+                "store": (k, v, ks, vs), "H": case["H"],
+                "seg": (torch.tensor([first, 0], device=DEV), torch.tensor([n, C - n], dtype=torch.int32, device=DEV)),
+                "slot": (first + torch.arange(C, device=DEV)) % case["slots"],
+                "back": (empty(C, Hkv, D), empty(C, Hkv, D)), "count": empty(1, dtype=torch.int32)}
+    slots, start, length = _segments(case)
+    (k, ks), (v, vs) = (_filled(g, s, slots, Hkv, D) for s in (SIGMA_QK, 1.0))
+    n = int(length.sum())
+    st = {"kind": kind, "case": case, "store": (k, v, ks, vs), "n": n,
+          "seg": (start.to(DEV), length.to(torch.int32).to(DEV))}
+    if kind == "recall":
+        st.update(back=(empty(n, Hkv, D), empty(n, Hkv, D)), count=empty(1, dtype=torch.int32))
+        return st
+    S, q_len, tail = case["S"], case["q_len"], case["tail"]
+    st.update(q=_normal(g, SIGMA_QK, q_len, Hq, D), S=S,
+              tail=(_normal(g, SIGMA_QK, tail, Hkv, D), _normal(g, 1.0, tail, Hkv, D)),
+              sink=(_normal(g, SIGMA_QK, S, Hkv, D), _normal(g, 1.0, S, Hkv, D)) if S else (None, None),
+              out=empty(q_len, Hq, D), lse=empty(Hq, q_len, dtype=torch.float32) if case["lse"] else None,
+              workspace=empty(WORKSPACE, dtype=torch.uint8))
+    return st
+
+
+# ---------------------------------------------------------------- one pass
+
+def run(st):
+    return _run_own(st) if own else _run_plain(st)
+
+
+def _run_own(st):
+    import paper_2606_19849_amd as vico
+    kind = st["kind"]
+    if kind == "rope":
+        Hq, Hkv, D = HEADS[st["case"]["model"]]
+        q, k, v = st["qkv"].view(-1, Hq + 2 * Hkv, D).split((Hq, Hkv, Hkv), 1)
+        vico.vico_qk_norm_rope(q, k, st["positions"], st["inv_freq"], st["q"], st["k"], v=v, v_out=st["v"],
+                               q_weight=st["weights"][0], k_weight=st["weights"][1], eps=1e-6,
+                               sections=st["sections"], flags=st["flags"])
+        return {"q": st["q"], "k": st["k"], "v": st["v"]}
+    if kind == "store":
+        vico.vico_kv_append_q4(st["k"], st["v"], *st["store"], st["H"])
+    if kind in ("store", "recall"):
+        vico.vico_kv_load_q4(*st["store"], *st["seg"], *st["back"], out_count=st["count"])
+        return {"k": st["back"][0], "v": st["back"][1], "count": st["count"]}
+    vico.vico_gather_attn_q4(st["q"], *st["tail"], *st["sink"], *st["store"], *st["seg"], st["out"], lse=st["lse"],
+                             workspace=st["workspace"], keys_hint=st["n"])
+    return {"out": st["out"], "lse": st["lse"]}
+
+
+def _gathered(st):
+    """Store slots of the segment table, one after the other."""
+    start, length = st["seg"]
+    before = torch.cumsum(length, 0) - length
+    return torch.repeat_interleave(start - before, length, output_size=st["n"]) + torch.arange(st["n"], device=DEV)
+
+
+def _run_plain(st):
+    kind, case = st["kind"], st["case"]
+    Hq, Hkv, D = HEADS[case["model"]]
+    if kind == "rope":
+        rot = case["rot"]
+        angle = st["positions"].double()[st["axis"]].T * st["inv_freq"].double()       # [T, rot/2]
+        cos, sin = angle.cos().float()[:, None], angle.sin().float()[:, None]
+
+        def rotated(x, w):
+            x = x.float()
+            if w is not None:
+                x = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-6) * w.float()
+            if case["adjacent"]:
+                a, b = x[..., 0:rot:2], x[..., 1:rot:2]
+                y = torch.stack([a * cos - b * sin, b * cos + a * sin], -1).flatten(-2)
+            else:
+                a, b = x[..., :rot // 2], x[..., rot // 2:rot]
+                y = torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
+            return torch.cat([y, x[..., rot:]], -1).to(torch.bfloat16)
+
+        q, k, v = st["qkv"].view(-1, Hq + 2 * Hkv, D).split((Hq, Hkv, Hkv), 1)
+        return {"q": rotated(q, st["weights"][0]), "k": rotated(k, st["weights"][1]), "v": v.contiguous()}
+    k4, v4, ks, vs = st["store"]
+    if kind == "store":
+        slot = st["slot"]
+        (k4[slot], ks[slot]), (v4[slot], vs[slot]) = _quantise(st["k"]), _quantise(st["v"])
+        k, v, n = _values(k4[slot], ks[slot]), _values(v4[slot], vs[slot]), st["seg"][1].sum(dtype=torch.int32)
+        return {"k": k.to(torch.bfloat16), "v": v.to(torch.bfloat16), "count": n.view(1)}
+    slot = _gathered(st)
+    k, v = _values(k4[slot], ks[slot]), _values(v4[slot], vs[slot])
+    if kind == "recall":
+        return {"k": k.to(torch.bfloat16), "v": v.to(torch.bfloat16),
+                "count": st["seg"][1].sum(dtype=torch.int32).view(1)}
+    sink = [st["sink"][i].float() for i in range(2)] if st["S"] else [k[:0], v[:0]]
+    k = torch.cat([sink[0], k, st["tail"][0].float()]).transpose(0, 1)                 # [Hkv, keys, D]
+    v = torch.cat([sink[1], v, st["tail"][1].float()]).transpose(0, 1)
+    q_len, g, n = case["q_len"], Hq // Hkv, k.shape[1]
+    q = st["q"].float().view(q_len, Hkv, g, D).permute(1, 2, 0, 3).reshape(Hkv, g * q_len, D)
+    s = torch.matmul(q, k.transpose(1, 2).contiguous()).mul_(D ** -0.5).view(Hkv, g, q_len, n)
+    row, key = torch.arange(q_len, device=DEV), torch.arange(n, device=DEV)
+    s = s.masked_fill_(key > n - q_len + row[:, None], -torch.inf).view(Hkv, g * q_len, n)
+    m = s.amax(-1, keepdim=True)
+    p = s.sub_(m).exp_()
+    total = p.sum(-1, keepdim=True)
+    o = (torch.matmul(p, v.contiguous()) / total).view(Hkv, g, q_len, D).permute(2, 0, 1, 3).reshape(q_len, Hq, D)
+    return {"out": o.to(torch.bfloat16), "lse": (m + total.log()).view(Hq, q_len) if case["lse"] else None}
+
+
+# ---------------------------------------------------------------- the definition in 64 bits
+
+def _decoded(codes, scales):
+    """Values of the 4-bit store from the bits of sign, exponent and fraction, in 64 bits."""
+    n, h, half = codes.shape
+    c = torch.empty(n, h, 2 * half, dtype=torch.int64, device=codes.device)
+    c[..., 0::2], c[..., 1::2] = codes.long() & 15, codes.long() >> 4
+    expo, frac = (c >> 1) & 3, (c & 1).double()
+    mag = torch.where(expo == 0, frac * 0.5, (1 + frac * 0.5) * 2.0 ** (expo - 1).double())
+    scale = 2.0 ** (scales.double() - 127).repeat_interleave(GROUP, -1)
+    return torch.where(c >= 8, -mag, mag) * scale
+
+
+def _nearest(x):
+    """bf16 keys or values after the store: the nearest of the values at the group's scale, in 64 bits."""
+    n, h, d = x.shape
+    x = x.double().reshape(-1, GROUP)
+    need = x.abs().amax(-1) / 7
+    scale = torch.where(need > 0, 2.0 ** need.clamp(min=2.0 ** -200).log2().ceil(), 0).clamp(2.0 ** -123, 2.0 ** 125)
+    scale = torch.where(need <= scale / 2, (scale / 2).clamp(min=2.0 ** -123), scale)   # log2 may round upwards
+    points = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device=x.device)
+    a = (x.abs() / scale[:, None])
+    upper = torch.bucketize(a, points).clamp(max=7)        # points[upper-1] < a <= points[upper]
+    lower = (upper - 1).clamp(min=0)
+    up, down = points[upper] - a, a - points[lower]
+    take = torch.where((up < down) | ((up == down) & (upper % 2 == 0)), upper, lower)
+    take = torch.where(a >= 6, torch.full_like(take, 7), take)
+    return (torch.sign(x) * points[take] * scale[:, None]).reshape(n, h, d)
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    Hq, Hkv, D = HEADS[case["model"]]
+    kind = case["kind"]
+    if kind == "rope":
+        rot, T = case["rot"], case["T"]
+        x = st["qkv"].double().view(T, Hq + 2 * Hkv, D)
+        turn = torch.empty(T, rot // 2, dtype=torch.complex128, device=DEV)
+        for i, axis in enumerate(st["axis"].tolist()):
+            a = st["positions"][axis].double() * st["inv_freq"][i].double()
+            turn[:, i] = torch.complex(a.cos(), a.sin())
+        res = []
+        for y, w in ((x[:, :Hq], st["weights"][0]), (x[:, Hq:Hq + Hkv], st["weights"][1])):
+            if w is not None:
+                y = y / (y.square().sum(-1, keepdim=True) / D + 1e-6).sqrt() * w.double()
+            y = y.clone()
+            i, j = (slice(0, rot, 2), slice(1, rot, 2)) if case["adjacent"] else (slice(0, rot // 2), slice(rot // 2, rot))
+            z = torch.complex(y[..., i].contiguous(), y[..., j].contiguous()) * turn[:, None]
+            y[..., i], y[..., j] = z.real, z.imag
+            res.append(y)
+        return {"q": res[0], "k": res[1], "v": x[:, Hq + Hkv:]}
+    if kind == "store":
+        return {"k": _nearest(st["k"]), "v": _nearest(st["v"]), "count": None}
+    k4, v4, ks, vs = st["store"]
+    pieces = [slice(a, a + b) for a, b in zip(*(x.tolist() for x in st["seg"]))]
+    k = torch.cat([_decoded(k4[p], ks[p]) for p in pieces])
+    v = torch.cat([_decoded(v4[p], vs[p]) for p in pieces])
+    if kind == "recall":
+        return {"k": k, "v": v, "count": None}
+    if st["S"]:
+        k, v = torch.cat([st["sink"][0].double(), k]), torch.cat([st["sink"][1].double(), v])
+    k, v = torch.cat([k, st["tail"][0].double()]), torch.cat([v, st["tail"][1].double()])
+    q_len, n = case["q_len"], k.shape[0]
+    out = torch.empty(q_len, Hq, D, dtype=torch.float64, device=DEV)
+    lse = torch.empty(Hq, q_len, dtype=torch.float64, device=DEV)
+    hidden = torch.ones(q_len, n, dtype=torch.bool, device=DEV).triu(n - q_len + 1)
+    for h in range(Hq):
+        kh, vh = k[:, h * Hkv // Hq], v[:, h * Hkv // Hq]
+        s = (st["q"][:, h].double() @ kh.T.contiguous()) / math.sqrt(D)
+        s[hidden] = -math.inf
+        lse[h] = torch.logsumexp(s, 1)
+        out[:, h] = torch.exp(s - lse[h][:, None]) @ vh.contiguous()
+    return {"out": out, "lse": lse if case["lse"] else None}
+
+
+# ---------------------------------------------------------------- what a pass cannot do without
+
+def work(case):
+    Hq, Hkv, D = HEADS[case["model"]]
+    kind = case["kind"]
+    row = 2 * Hkv * D                                      # elements of a token's key and value
+    row4 = row // 2 + row // GROUP                         # its bytes in the store
+    if kind == "rope":
+        T = case["T"]
+        read = 2 * D * (Hq + 2 * Hkv) * T
+        more = 4 * case["axes"] * T + 2 * case["rot"] + (2 * D * (4 if case["f32_weights"] else 2) if case["norm"] else 0)
+        return {"bytes": 2 * read + more, "flops": T * (Hq + Hkv) * (3 * case["rot"] + (4 * D if case["norm"] else 0))}
+    if kind == "store":
+        return {"bytes": case["C"] * 2 * (2 * row + row4), "flops": case["C"] * 4 * row}
+    n = int(_segments(case)[2].sum())
+    if kind == "recall":
+        return {"bytes": n * (2 * row + row4), "flops": n * row}
+    S, q_len, tail = case["S"], case["q_len"], case["tail"]
+    pairs = q_len * (S + n + tail) - q_len * (q_len - 1) // 2
+    nbytes = n * row4 + (S + tail) * 2 * row + 4 * q_len * Hq * D + (4 * Hq * q_len if case["lse"] else 0)
+    return {"bytes": nbytes, "flops": 4 * Hq * D * pairs}

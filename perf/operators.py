@@ -182,6 +182,8 @@ def _segments(case):
 
 def _sections(case):
     half = case["rot"] // 2
+    if case["strided"]:
+        return [half - half // 16 * 10, half // 16 * 5, half // 16 * 5]
     return [half] if case["axes"] == 1 else [half // 4, half // 4 + half // 8, half - half // 2 - half // 8]
 
 

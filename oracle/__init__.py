@@ -21,11 +21,14 @@ Modules
                 top-k selection) and attention over the retrieved chunks
   token_drop -- chunk-level temporal token dropping (pairwise cosine over
                 frames, anchor frame) and the retained-token order
+  rope       -- norms of queries and keys for each head, position rotation
+  kv4        -- the 4-bit store of keys and values
 
 Parity status: every function here is pinned by tests in
 tests/test_oracle_pins.py, tests/test_oracle_retrieval_pins.py,
-tests/test_oracle_acn_pins.py and tests/test_oracle_drop_pins.py against library routines, closed forms,
-invariants and brute force; none is "parity unpinned".
+tests/test_oracle_acn_pins.py, tests/test_oracle_drop_pins.py and
+tests/test_cache_host.py against library routines, closed forms, invariants and
+brute force; none is "parity unpinned".
 """
 from .bf16 import bf16_bits_to_f64
 from .attention import (

@@ -7,9 +7,11 @@ to a sink prefix, the W newest cached visual tokens and themselves
 ring-buffer cache.  Query-side retrieval (token means, cosine scores, top-k
 chunks) and attention of short queries or decode steps over the retrieved
 chunks complete the query path; temporal token dropping thins each chunk's
-tokens before they reach the LLM.  All arithmetic runs in the hand-written HIP
-kernels of libvico.so (C ABI in include/vico.h); this package only marshals
-arguments.
+tokens before they reach the LLM.  Head norms with the position rotation make
+the attention's inputs from the projection, and a store of keys and values in 4
+bits serves the query path of long streams.  All arithmetic runs in the
+hand-written HIP kernels of libvico.so (C ABI in include/vico.h and
+include/vico_cache.h); this package only marshals arguments.
 """
 from ._binding import (
     VICO_DTYPE_BF16,
@@ -35,6 +37,13 @@ from ._binding import (
     vico_acn_window,
     vico_temporal_drop,
     vico_temporal_drop_workspace_bytes,
+    VICO_ROPE_ADJACENT,
+    VICO_ROPE_STRIDED_AXES,
+    vico_qk_norm_rope,
+    vico_kv_append_q4,
+    vico_kv_load_q4,
+    vico_gather_plan_q4,
+    vico_gather_attn_q4,
 )
 
 __all__ = [
@@ -61,4 +70,11 @@ __all__ = [
     "vico_acn_window",
     "vico_temporal_drop",
     "vico_temporal_drop_workspace_bytes",
+    "VICO_ROPE_ADJACENT",
+    "VICO_ROPE_STRIDED_AXES",
+    "vico_qk_norm_rope",
+    "vico_kv_append_q4",
+    "vico_kv_load_q4",
+    "vico_gather_plan_q4",
+    "vico_gather_attn_q4",
 ]

@@ -1,4 +1,4 @@
-"""Binding of libvico (include/vico.h): argument marshalling only.
+"""Binding of libvico (include/vico.h, include/vico_cache.h): argument marshalling only.
 
 Calls with plain arguments go through _vico_call (csrc/py_call.cpp), which
 checks and passes them in C++; it answers None for anything else, and the
@@ -30,6 +30,8 @@ VICO_SPLIT_BALANCED = -1
 VICO_ATTN_BIDIRECTIONAL = 1
 VICO_ATTN_APPEND = 2
 VICO_NOALLOC_SCRATCH_BYTES = 64 << 20
+VICO_ROPE_ADJACENT = 1
+VICO_ROPE_STRIDED_AXES = 2
 
 _i32, _i64, _f32, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
 
@@ -56,6 +58,14 @@ _SIGNATURES = {
                                 _i32, _i32, _i32, _f32, _vp, _i32, _vp, _i32, _vp, _i64, _vp]),
     "vico_gather_attn_noalloc": (_i32, [_vp, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _i32,
                                         _i64, _i32, _i32, _i32, _f32, _vp, _i32, _vp, _i32, _vp]),
+    "vico_qk_norm_rope": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _f32, _vp, _i32,
+                                 _vp, _i32, ctypes.POINTER(_i32), _i32, _vp, _vp, _vp, _vp]),
+    "vico_kv_append_q4": (_i32, [_vp, _vp, _i32, _vp, _vp, _vp, _vp, _i32, _i64, _i32, _i32, _vp]),
+    "vico_kv_load_q4": (_i32, [_vp, _vp, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _i32, _i32, _vp]),
+    "vico_gather_plan_q4": (_i32, [_i32, _i32, _i32, _i32, _i32, _i64, _i32, _i32, _i32, _i32,
+                                   ctypes.POINTER(_i32), ctypes.POINTER(_i64)]),
+    "vico_gather_attn_q4": (_i32, [_vp, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _i32,
+                                   _i64, _i32, _i32, _i32, _f32, _vp, _i32, _vp, _i32, _vp, _i64, _vp]),
     "vico_status_str": (ctypes.c_char_p, [_i32]),
     "vico_last_hip_error": (_i32, []),
 }
@@ -395,3 +405,193 @@ def vico_temporal_drop(frames, tau: float, keep, out_index, out_count, sim=None,
                                            _ptr(sim), _ptr(out_tokens), _ptr(out_index), _ptr(out_count),
                                            _ptr(workspace), wb, _stream(stream))
     _check(st, "vico_temporal_drop")
+
+
+# ---------------------------------------------------------------- include/vico_cache.h
+
+def _here(**tensors):
+    """The calls of vico_cache.h run on the current device: tensors of another one are refused."""
+    current = torch.cuda.current_device()
+    for n, t in tensors.items():
+        if t is not None and t.device.index != current:
+            raise ValueError(f"{n}: on {t.device}, and the current device is cuda:{current}")
+
+
+def _shape(name, t, want):
+    if t is None or tuple(t.shape) != tuple(want):
+        raise ValueError(f"{name}: shape {None if t is None else tuple(t.shape)} != {tuple(want)}")
+
+
+def _rows_of_heads(name, t):
+    """Token stride of a [tokens, heads, head_dim] bf16 tensor whose heads are dense."""
+    if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3 and t.stride(2) == 1
+            and (t.shape[1] == 1 or t.stride(1) == t.shape[2])):
+        raise ValueError(f"{name}: expected a 3-d bfloat16 CUDA tensor with dense heads, got {tuple(t.shape)} "
+                         f"{t.dtype} with strides {t.stride()} on {t.device}")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _check_store(store_k, store_v, scale_k, scale_v, heads, head_dim):
+    for n, t in (("store_k", store_k), ("store_v", store_v), ("scale_k", scale_k), ("scale_v", scale_v)):
+        _dev_tensor(n, t, torch.uint8, 3)
+    R = store_k.shape[0]
+    for n, t, width in (("store_k", store_k, head_dim // 2), ("store_v", store_v, head_dim // 2),
+                        ("scale_k", scale_k, head_dim // 32), ("scale_v", scale_v, head_dim // 32)):
+        _shape(n, t, (R, heads, width))
+    _here(store_k=store_k, store_v=store_v, scale_k=scale_k, scale_v=scale_v)
+
+
+def vico_qk_norm_rope(q, k, positions, inv_freq, q_out, k_out, v=None, v_out=None, q_weight=None, k_weight=None,
+                      eps: float = 1e-6, sections=None, flags: int = 0, stream=None) -> None:
+    """Norms of queries and keys for each head with the position rotation (vico_qk_norm_rope).
+
+    q [T, Hq, D], k and v [T, Hkv, D] bf16: dense, or slices of a packed projection; positions int32 [T] or
+    [axes, T]; inv_freq fp32 [rotary_dim / 2]; sections: pair counts of the three axes."""
+    if positions.dim() == 1:
+        positions = positions[None]
+    s = sections if sections is not None and len(sections) == 3 else (0, 0, 0)
+    if sections is None or len(sections) == positions.shape[0] == 3:
+        st = (_calls or _fast()).qk_norm_rope(q, k, positions, inv_freq, q_out, k_out, v, v_out, q_weight, k_weight, eps,
+                                              s[0], s[1], s[2], flags, _handle(stream))
+        if st is not None:
+            return _check(st, "vico_qk_norm_rope")
+    strides = [_rows_of_heads(n, t) for n, t in (("q", q), ("k", k))]
+    if (v is None) != (v_out is None):
+        raise ValueError("v and v_out: both or neither")
+    T, Hq, D = q.shape
+    Hkv = k.shape[1]
+    _dev_tensor("positions", positions, torch.int32, 2)
+    _dev_tensor("inv_freq", inv_freq, torch.float32, 1)
+    _dev_bf16("q_out", q_out)
+    _dev_bf16("k_out", k_out)
+    _shape("k", k, (T, Hkv, D))
+    _shape("q_out", q_out, q.shape)
+    _shape("k_out", k_out, k.shape)
+    _shape("positions", positions, (positions.shape[0], T))
+    if inv_freq.shape[0] > D:
+        raise ValueError("inv_freq: one frequency for each rotated pair")
+    strides.append(0)
+    if v is not None:
+        strides[2] = _rows_of_heads("v", v)
+        _dev_bf16("v_out", v_out)
+        _shape("v", v, k.shape)
+        _shape("v_out", v_out, k.shape)
+    wt = next((w.dtype for w in (q_weight, k_weight) if w is not None), torch.bfloat16)
+    if wt not in (torch.bfloat16, torch.float32):
+        raise ValueError("q_weight, k_weight: bfloat16 or float32")
+    for n, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _dev_tensor(n, w, wt, 1)
+            _shape(n, w, (D,))
+    if sections is not None and len(sections) != positions.shape[0]:
+        raise ValueError("sections: one pair count for each position axis")
+    _here(q=q, k=k, v=v, positions=positions, inv_freq=inv_freq, q_out=q_out, k_out=k_out, v_out=v_out,
+          q_weight=q_weight, k_weight=k_weight)
+    arr = None if sections is None else (_i32 * len(sections))(*[int(x) for x in sections])
+    st = load_library().vico_qk_norm_rope(
+        _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v), strides[2], T, Hq, Hkv, D, _ptr(q_weight), _ptr(k_weight),
+        VICO_DTYPE_F32 if wt == torch.float32 else VICO_DTYPE_BF16, float(eps), _ptr(positions), positions.shape[0],
+        _ptr(inv_freq), 2 * inv_freq.shape[0], arr, int(flags), _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(stream))
+    _check(st, "vico_qk_norm_rope")
+
+
+def vico_kv_append_q4(k_chunk, v_chunk, store_k, store_v, scale_k, scale_v, hist_len: int, stream=None) -> None:
+    """store[(hist_len + j) % R] <- chunk[j] for K and V, in 4 bits (vico_kv_append_q4).
+
+    store_k, store_v uint8 [R, Hkv, D / 2]; scale_k, scale_v uint8 [R, Hkv, D / 32]."""
+    st = (_calls or _fast()).append_q4(k_chunk, v_chunk, store_k, store_v, scale_k, scale_v, hist_len, _handle(stream))
+    if st is not None:
+        return _check(st, "vico_kv_append_q4")
+    _dev_bf16("k_chunk", k_chunk)
+    _dev_bf16("v_chunk", v_chunk)
+    C, Hkv, D = k_chunk.shape
+    _shape("v_chunk", v_chunk, k_chunk.shape)
+    _check_store(store_k, store_v, scale_k, scale_v, Hkv, D)
+    _here(k_chunk=k_chunk, v_chunk=v_chunk)
+    st = load_library().vico_kv_append_q4(_ptr(k_chunk), _ptr(v_chunk), C, _ptr(store_k), _ptr(store_v), _ptr(scale_k),
+                                          _ptr(scale_v), store_k.shape[0], int(hist_len), Hkv, D, _stream(stream))
+    _check(st, "vico_kv_append_q4")
+
+
+def vico_kv_load_q4(store_k, store_v, scale_k, scale_v, seg_start, seg_len, out_k, out_v, out_count=None,
+                    stream=None) -> None:
+    """Segments of the 4-bit store as bf16 rows, in table order (vico_kv_load_q4)."""
+    st = (_calls or _fast()).load_q4(store_k, store_v, scale_k, scale_v, seg_start, seg_len, out_k, out_v, out_count,
+                                     _handle(stream))
+    if st is not None:
+        return _check(st, "vico_kv_load_q4")
+    _dev_bf16("out_k", out_k)
+    _dev_bf16("out_v", out_v)
+    rows, Hkv, D = out_k.shape
+    _shape("out_v", out_v, out_k.shape)
+    _check_store(store_k, store_v, scale_k, scale_v, Hkv, D)
+    _dev_tensor("seg_start", seg_start, torch.int64, 1)
+    _dev_tensor("seg_len", seg_len, torch.int32, 1)
+    _shape("seg_len", seg_len, seg_start.shape)
+    if out_count is not None:
+        _dev_tensor("out_count", out_count, torch.int32, 1)
+        if out_count.shape[0] < 1:
+            raise ValueError("out_count: needs 1 entry")
+    _here(seg_start=seg_start, seg_len=seg_len, out_k=out_k, out_v=out_v, out_count=out_count)
+    st = load_library().vico_kv_load_q4(_ptr(store_k), _ptr(store_v), _ptr(scale_k), _ptr(scale_v), store_k.shape[0],
+                                        _ptr(seg_start), _ptr(seg_len), seg_start.shape[0], _ptr(out_k), _ptr(out_v), rows,
+                                        _ptr(out_count), Hkv, D, _stream(stream))
+    _check(st, "vico_kv_load_q4")
+
+
+def vico_gather_plan_q4(q_len, tail_len, sink_len, store_slots, num_segments, keys_hint, num_q_heads, num_kv_heads,
+                        head_dim, num_splits=0):
+    """(most parts, workspace_bytes) of vico_gather_attn_q4 for these arguments."""
+    ns, wb = _i32(0), _i64(0)
+    st = load_library().vico_gather_plan_q4(q_len, tail_len, sink_len, store_slots, num_segments, int(keys_hint),
+                                            num_q_heads, num_kv_heads, head_dim, num_splits,
+                                            ctypes.byref(ns), ctypes.byref(wb))
+    _check(st, "vico_gather_plan_q4")
+    return ns.value, wb.value
+
+
+def vico_gather_attn_q4(q, tail_k, tail_v, sink_k, sink_v, store_k, store_v, scale_k, scale_v, seg_start, seg_len, out,
+                        lse=None, workspace=None, keys_hint: int = 0, num_splits: int = 0, softmax_scale: float = 0.0,
+                        stream=None) -> None:
+    """vico_gather_attn over a store in 4 bits (vico_gather_attn_q4)."""
+    st = (_calls or _fast()).gather_q4(q, tail_k, tail_v, sink_k, sink_v, store_k, store_v, scale_k, scale_v, seg_start,
+                                       seg_len, out, lse, keys_hint, num_splits, softmax_scale, _handle(stream), workspace)
+    if st is not None:
+        return _check(st, "vico_gather_attn_q4")
+    for n, t in (("q", q), ("tail_k", tail_k), ("tail_v", tail_v), ("sink_k", sink_k), ("sink_v", sink_v)):
+        _dev_bf16(n, t)
+    Lq, Hq, D = q.shape
+    T, Hkv = tail_k.shape[0], tail_k.shape[1]
+    _shape("tail_k", tail_k, (T, Hkv, D))
+    _shape("tail_v", tail_v, tail_k.shape)
+    if (sink_k is None) != (sink_v is None) or (seg_start is None) != (seg_len is None):
+        raise ValueError("sink_k and sink_v, seg_start and seg_len: both or neither")
+    S = 0
+    if sink_k is not None:
+        S = sink_k.shape[0]
+        _shape("sink_k", sink_k, (S, Hkv, D))
+        _shape("sink_v", sink_v, sink_k.shape)
+    n_segs = 0
+    if seg_start is not None:
+        n_segs = seg_start.shape[0]
+        _dev_tensor("seg_start", seg_start, torch.int64, 1)
+        _dev_tensor("seg_len", seg_len, torch.int32, 1)
+        _shape("seg_len", seg_len, seg_start.shape)
+    _check_store(store_k, store_v, scale_k, scale_v, Hkv, D)
+    if not (out.is_cuda and out.is_contiguous() and out.dtype in (torch.bfloat16, torch.float32)):
+        raise ValueError("out: expected a contiguous bfloat16 or float32 CUDA tensor")
+    _shape("out", out, q.shape)
+    if lse is not None:
+        _dev_tensor("lse", lse, torch.float32, 2)
+        _shape("lse", lse, (Hq, Lq))
+    if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor")
+    _here(q=q, tail_k=tail_k, tail_v=tail_v, sink_k=sink_k, sink_v=sink_v, seg_start=seg_start, seg_len=seg_len, out=out,
+          lse=lse, workspace=workspace)
+    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    odt = VICO_DTYPE_F32 if out.dtype == torch.float32 else VICO_DTYPE_BF16
+    st = load_library().vico_gather_attn_q4(
+        _ptr(q), Lq, _ptr(tail_k), _ptr(tail_v), T, _ptr(sink_k), _ptr(sink_v), S, _ptr(store_k), _ptr(store_v),
+        _ptr(scale_k), _ptr(scale_v), store_k.shape[0], _ptr(seg_start), _ptr(seg_len), n_segs, int(keys_hint), Hq, Hkv, D,
+        float(softmax_scale), _ptr(out), odt, _ptr(lse), int(num_splits), _ptr(workspace), wb, _stream(stream))
+    _check(st, "vico_gather_attn_q4")

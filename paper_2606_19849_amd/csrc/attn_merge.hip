@@ -36,6 +36,11 @@ __device__ __forceinline__ bool append_block(const AttnArgs& a, int merge_blocks
   return true;
 }
 
+// The log-sum-exp of a row whose weights are NaN: NaN where the caller asks for it.
+__device__ __forceinline__ float lse_or_nan(float lse, float sum, const AttnArgs& a) {
+  return a.nan_lse && sum != sum ? sum : lse;
+}
+
 // Few parts, many rows (chunk prefill splits): one thread per (head, row,
 // 4-column group) reads every part's value at once; neighbouring threads
 // read neighbouring columns, so every load is a full coalesced row.
@@ -83,7 +88,7 @@ __global__ __launch_bounds__(kMergeThreads) void attn_merge_rows_kernel(AttnArgs
   } else {
     *(bf16x4*)((__bf16*)a.out + oo) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
   }
-  if (dq == 0 && a.lse) a.lse[(int64_t)h * a.C + row] = wsum > 0.f ? (m_use + __log2f(wsum)) * kLn2 : -INFINITY;
+  if (dq == 0 && a.lse) a.lse[(int64_t)h * a.C + row] = lse_or_nan(wsum > 0.f ? (m_use + __log2f(wsum)) * kLn2 : -INFINITY, wsum, a);
 }
 
 // Many parts (short queries): see the file comment.
@@ -117,7 +122,7 @@ __global__ __launch_bounds__(kMergeThreads) void attn_merge_kernel(AttnArgs a, i
     w_s[r][lane] = w;
     if (lane == 0) {
       inv_s[r] = sum > 0.f ? 1.f / sum : 0.f;
-      lse_s[r] = sum > 0.f ? (m_use + __log2f(sum)) * kLn2 : -INFINITY;
+      lse_s[r] = lse_or_nan(sum > 0.f ? (m_use + __log2f(sum)) * kLn2 : -INFINITY, sum, a);
     }
   }
   __syncthreads();

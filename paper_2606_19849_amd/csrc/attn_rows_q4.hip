@@ -1,0 +1,497 @@
+// Attention over a 4-bit store: query rows against [sink | store segments |
+// tail, causal], the store's keys and values in 4 bits (q4_common.h), sink and
+// tail in bf16 (ViCoStream Sec. 3, query-time decoding; query rows of Eq. (4)).
+//
+//   O = softmax(scale Q K^T) V,  K, V of a store row = code * 2^(scale byte - 127)
+//
+// Every wave takes 32-key blocks of its work-group's key range in turn, loads
+// them into registers, turns the codes into bf16 there (exactly) and keeps a
+// running softmax of its own; the waves' states are merged through LDS at the
+// end.  A block lies in one region, so the three regions' last blocks may be
+// part-filled.
+//   * S^T = K Q^T with v_mfma_f32_16x16x32_bf16.  Lane (n, j), n = lane % 16,
+//     j = lane / 16, holds D/4 consecutive dims of one key: one load of its
+//     codes, and one scale for all of them.  The order of the dims inside the
+//     k-steps differs from memory's for that; Q is loaded in the same order.
+//     Key rows are ordered so that lane group j ends with the logits of keys
+//     8j .. 8j+7, and P^T is the second product's B operand as it stands.
+//   * O^T = V^T P^T: the lane holds D/16 dims of its 8 keys, converted two dims
+//     at a time and transposed with one v_perm_b32 per two values.  The scale
+//     bytes of a quad's 4 lanes cover the quad's 8 keys; a DPP step broadcasts
+//     each.
+// Probabilities are rounded to bf16 for the second product, as in the bf16
+// kernels; logits, softmax state and sums are fp32.
+//
+// A masked key's probability is 0, but 0 times a NaN or an infinity is not: in
+// a block that the causal mask cuts, such values are taken out of V and added
+// for the rows that see them alone.
+
+#include "q4_common.h"
+
+namespace vico {
+namespace {
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
+}
+
+// A row tile's state and block bodies; D dims a head, NRB blocks of 16 rows.
+template <int D, int NRB, int NW>
+__global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) {
+  constexpr int NKS = D / 32;              // k-steps of Q K^T
+  constexpr int DPL = D / 4;               // dims of a key per lane
+  constexpr int VE = D / 16;               // dims per lane of a V row
+  constexpr int RT = 16 * NRB;             // rows of the work-group
+  constexpr int BK = kRowsBlock;           // keys per block
+  constexpr int OS = D + 8;                // row stride of the merge buffer (floats)
+  constexpr int PER = kMaxSegments / (NW * 64);
+  static_assert(BK == 32, "two 16-key products per block");
+  typedef uint32_t krow_t __attribute__((ext_vector_type(DPL / 8)));
+  typedef uint32_t vrow_t __attribute__((ext_vector_type(VE / 2)));
+  typedef const __attribute__((address_space(1))) char* gptr;
+
+  __shared__ __attribute__((aligned(16))) float o_s[NW][RT][OS];
+  __shared__ float m_s[NW][RT], l_s[NW][RT];
+  // segment table of a call with more segments than lanes; the merge buffer is not in use yet, but blocks are
+  // looked up while other waves merge
+  __shared__ int incl_s[kMaxSegments], shift_s[kMaxSegments];
+  __shared__ int wave_s[NW];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, j = lane >> 4;
+  const int g = a.Hq / a.Hkv;
+  const int NR = g * a.Lq;
+
+  // ---- work item: row tiles of one key range side by side (they share its K/V in an XCD's L2)
+  const int L = xcd_remap(blockIdx.x, gridDim.x);
+  const int rt = L % a.n_rt;
+  const int part = (L / a.n_rt) % a.parts;
+  const int kv = L / (a.n_rt * a.parts);
+
+  // ---- segment table: the lanes hold a window of 64 segments, `incl` keys up to a segment's end, `shift` from
+  // gathered key to slot.  Up to 64 segments that is all; more are scanned by the work-group into LDS.
+  auto clipped = [&](int s, int& slot) __attribute__((always_inline)) {
+    const int64_t st = a.seg_start[s], en = st + (int64_t)a.seg_len[s];
+    const int64_t lo = st > 0 ? st : 0, hi = en < (int64_t)a.cap ? en : (int64_t)a.cap;
+    slot = hi > lo ? (int)lo : 0;
+    return hi > lo ? (int)(hi - lo) : 0;
+  };
+  auto scan = [&](int x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(x, o, 64);
+      x += lane >= o ? y : 0;
+    }
+    return x;
+  };
+  int incl = 0, shift = 0, G = 0, win = 0;
+  if (a.n_segs > 64) {
+    int len[PER], run = 0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int s = tid * PER + e;
+      int slot = 0;
+      len[e] = s < a.n_segs ? clipped(s, slot) : 0;
+      shift_s[s] = slot;
+      run += len[e];
+    }
+    const int upto = scan(run);
+    if (lane == 63) wave_s[wave] = upto;
+    __syncthreads();
+    int base = upto - run;
+    for (int w = 0; w < wave; ++w) base += wave_s[w];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int s = tid * PER + e;
+      shift_s[s] -= base;
+      base += len[e];
+      incl_s[s] = base;
+    }
+    __syncthreads();
+    G = __builtin_amdgcn_readfirstlane(incl_s[kMaxSegments - 1]);
+    incl = incl_s[lane];
+    shift = shift_s[lane];
+  } else {
+    int slot = 0;
+    const int len = lane < a.n_segs ? clipped(lane, slot) : 0;
+    incl = scan(len);
+    shift = slot - (incl - len);
+    G = __builtin_amdgcn_readlane(incl, 63);
+  }
+  // the window that holds gathered key i (0 <= i < G); keys are asked for in rising order
+  auto window_of = [&](int i) __attribute__((always_inline)) {
+    while (__builtin_amdgcn_readlane(incl, 63) <= i) {      // there are further segments: incl of the last one is G
+      win += 64;
+      incl = incl_s[win + lane];
+      shift = shift_s[win + lane];
+    }
+  };
+
+  // ---- Q rows as B fragments; rows past the end repeat the last one and are never stored
+  bf16x8 qf[NRB][NKS];
+  int tok[NRB];
+#pragma unroll
+  for (int rb = 0; rb < NRB; ++rb) {
+    const int r = min(rt * RT + rb * 16 + n, NR - 1);
+    tok[rb] = r / g;
+    const uint16_t* qp = a.q + ((int64_t)tok[rb] * a.Hq + kv * g + r % g) * D + j * DPL;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) qf[rb][ks] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + ks * 8));
+  }
+
+  // ---- blocks: sink, store, tail
+  const int tail0 = a.T - a.Lq;                                // tail key `tail0 + t` is row t's last
+  const int tail_first = tail0 + min(rt * RT, NR - 1) / g, tail_last = tail0 + (min((rt + 1) * RT, NR) - 1) / g;
+  const int nb_s = (a.S + BK - 1) / BK, nb_g = (G + BK - 1) / BK, nb_t = tail_last / BK + 1;
+  const int n_blocks = nb_s + nb_g + nb_t;
+  const int b_lo = (int)((int64_t)n_blocks * part / a.parts);
+  const int b_hi = (int)((int64_t)n_blocks * (part + 1) / a.parts);
+
+  const int rbytes = a.Hkv * D * 2, cbytes = a.Hkv * (D / 2), sbytes = a.Hkv * (D / kQ4Group);
+  const int ka = 8 * (n >> 2) + (n & 3);                       // this lane's key of the first product; second: + 4
+  const int kg = j * DPL / kQ4Group, vg = n * VE / kQ4Group;   // scale groups of this lane's dims
+
+  // ---- running state: row n of each 16-row block, shared by the lanes n, n+16, n+32, n+48
+  f32x4 o[NRB][VE];
+  float m_run[NRB], l_run[NRB], neg_m[NRB];        // neg_m: -m_run, +inf while there is no max
+#pragma unroll
+  for (int rb = 0; rb < NRB; ++rb) {
+#pragma unroll
+    for (int e = 0; e < VE; ++e) o[rb][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run[rb] = -INFINITY;
+    neg_m[rb] = INFINITY;
+    l_run[rb] = 0.f;
+  }
+  const float c = a.scale_log2;
+
+  // Softmax of the block's logits (key 8j + v in s[v / 4][v % 4]); key index past lim[rb] is masked.
+  auto softmax = [&](f32x4 (&s)[2], int rb, int lim, bool masked) __attribute__((always_inline)) {
+    if (masked) {
+#pragma unroll
+      for (int v = 0; v < 8; ++v) s[v / 4][v % 4] = 8 * j + v > lim ? -INFINITY : s[v / 4][v % 4];
+    }
+    float e[8], sum;
+    auto expo = [&](float nm) __attribute__((always_inline)) {
+#pragma unroll
+      for (int v = 0; v < 8; ++v) e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v / 4][v % 4], c, nm));
+      sum = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+    };
+    expo(neg_m[rb]);
+    // the max is raised when a lane's sum of 8 (which bounds each) passes kLaneSumLimit, or there is none yet
+    if (__builtin_amdgcn_ballot_w64(!(sum <= kLaneSumLimit))) {
+      float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                       fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float m_new = fmaxf(m_run[rb], mx * c);
+      const float alpha = (m_new == m_run[rb]) ? 1.f : __builtin_amdgcn_exp2f(m_run[rb] - m_new);
+      l_run[rb] *= alpha;
+#pragma unroll
+      for (int d = 0; d < VE; ++d) o[rb][d] *= alpha;
+      m_run[rb] = m_new;
+      neg_m[rb] = -m_new;
+      expo(m_new == -INFINITY ? 0.f : -m_new);
+    }
+    l_run[rb] += sum;
+    bf16x8 p;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) p[v] = (__bf16)e[v];
+    return p;
+  };
+
+  // ---- a block of bf16 keys, rows row0 .. row0 + 31 of a tensor with `rows` (rows past it read as zero); the key
+  // index that lim[] masks by counts from row0
+  auto bf16_block = [&](const uint16_t* bk, const uint16_t* bv, int rows, int row0, const int (&lim)[NRB],
+                        bool masked) __attribute__((always_inline)) {
+    const int left = min(rows - row0, BK) * rbytes;
+    const rsrc_t rk = make_rsrc((const char*)bk + (int64_t)row0 * rbytes, left);
+    const rsrc_t rv = make_rsrc((const char*)bv + (int64_t)row0 * rbytes, left);
+    u32x4 kr[2][NKS];
+    vrow_t vr[8];
+    const uint32_t k_off = (uint32_t)(ka * rbytes + kv * D * 2 + j * DPL * 2);
+    const uint32_t v_off = (uint32_t)(8 * j * rbytes + kv * D * 2 + n * VE * 2);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks)
+        kr[h][ks] = __builtin_amdgcn_raw_buffer_load_b128(rk, k_off + h * 4 * rbytes + ks * 16, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (VE == 8) vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, v_off + i * rbytes, 0, 0);
+      else vr[i] = __builtin_amdgcn_raw_buffer_load_b64(rv, v_off + i * rbytes, 0, 0);
+    }
+    bf16x8 pf[NRB];
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+      f32x4 s[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks)
+          s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][ks]), qf[rb][ks], s[h], 0, 0, 0);
+      }
+      pf[rb] = softmax(s, rb, lim[rb], masked);
+    }
+    if (masked) {
+      // values that are not finite: out of V, and added for the rows that see them
+      uint32_t odd = 0;                            // bit i: this lane's key 8j + i
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int d = 0; d < VE / 2; ++d) {
+          const uint32_t x = vr[i][d];
+          const bool lo = (x & 0x7F80u) == 0x7F80u, hi = (x & 0x7F800000u) == 0x7F800000u;
+          odd |= (lo || hi) ? 1u << i : 0u;
+        }
+      if (__builtin_amdgcn_ballot_w64(odd != 0)) {
+        uint32_t keys = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint64_t who = __builtin_amdgcn_ballot_w64((odd >> i) & 1);
+#pragma unroll
+          for (int jj = 0; jj < 4; ++jj) keys |= (who >> (16 * jj) & 0xFFFF) ? 1u << (8 * jj + i) : 0u;
+#pragma unroll
+          for (int d = 0; d < VE / 2; ++d) {
+            uint32_t x = vr[i][d];
+            if ((x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
+            if ((x & 0x7F800000u) == 0x7F800000u) x &= 0xFFFFu;
+            vr[i][d] = x;
+          }
+        }
+        for (; keys; keys &= keys - 1) {           // wave-uniform
+          const int key = __builtin_ctz(keys);
+          u32x4 x[VE / 2];                         // this lane's dims of O^T, VE * 4j .. + 4 * VE - 1, of the key
+#pragma unroll
+          for (int q = 0; q < VE / 2; ++q)
+            x[q] = __builtin_amdgcn_raw_buffer_load_b128(rv, (uint32_t)(key * rbytes + kv * D * 2 + VE * 8 * j + 16 * q), 0, 0);
+#pragma unroll
+          for (int rb = 0; rb < NRB; ++rb) {
+            float p = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p = (key & 7) == i ? (float)pf[rb][i] : p;
+            p = __shfl(p, 16 * (key >> 3) + n, 64);
+#pragma unroll
+            for (int d = 0; d < 4 * VE; ++d) {
+              const uint32_t w = x[d / 8][d % 8 / 2], bits = (d & 1) ? w & 0xFFFF0000u : w << 16;
+              const bool add = key <= lim[rb] && (bits & 0x7F800000u) == 0x7F800000u;
+              o[rb][d % VE][d / VE] += add ? p * __uint_as_float(bits) : 0.f;
+            }
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      u32x4 w;           // value e of this lane's 8 keys
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        w[p] = __builtin_amdgcn_perm(vr[2 * p + 1][e / 2], vr[2 * p][e / 2], (e & 1) ? 0x07060302u : 0x05040100u);
+      const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) o[rb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb], o[rb][e], 0, 0, 0);
+    }
+  };
+
+  // ---- a block of the store
+  struct Q4Block {
+    krow_t k[2];                  // this lane's dims of keys ka, ka + 4
+    uint32_t v[8];                // its dims of keys 8j .. 8j + 7
+    uint32_t ks[2], vs[2];        // scale bytes: K of the two keys; V of keys 8j + n%4, 8j + 4 + n%4
+  };
+  auto load_q4 = [&](int i0, Q4Block& x) __attribute__((always_inline)) {      // gathered keys i0 .. i0 + 31, i0 < G
+    window_of(i0);
+    int s = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= i0));      // segment of key i0, in the window
+    const uint32_t kc = (uint32_t)(kv * (D / 2) + j * (DPL / 2)), vc = (uint32_t)(kv * (D / 2) + n * (VE / 2));
+    const uint32_t ksc = (uint32_t)(kv * (D / kQ4Group) + kg), vsc = (uint32_t)(kv * (D / kQ4Group) + vg);
+    if (i0 + BK <= __builtin_amdgcn_readlane(incl, s)) {
+      // consecutive slots: base + fixed per-lane offsets
+      const int64_t slot = i0 + __builtin_amdgcn_readlane(shift, s);
+      const rsrc_t rk = make_rsrc(a.k4 + slot * cbytes, BK * cbytes), rv = make_rsrc(a.v4 + slot * cbytes, BK * cbytes);
+      const rsrc_t rks = make_rsrc(a.ks + slot * sbytes, BK * sbytes), rvs = make_rsrc(a.vs + slot * sbytes, BK * sbytes);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t off = (uint32_t)((ka + 4 * h) * cbytes) + kc;
+        if constexpr (D == 128) x.k[h] = __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, 0);
+        else x.k[h] = __builtin_amdgcn_raw_buffer_load_b64(rk, off, 0, 0);
+        x.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(rks, (uint32_t)((ka + 4 * h) * sbytes) + ksc, 0, 0);
+        x.vs[h] = __builtin_amdgcn_raw_buffer_load_b8(rvs, (uint32_t)((8 * j + 4 * h + (n & 3)) * sbytes) + vsc, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t off = (uint32_t)((8 * j + i) * cbytes) + vc;
+        if constexpr (D == 128) x.v[i] = __builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0);
+        else x.v[i] = __builtin_amdgcn_raw_buffer_load_b16(rv, off, 0, 0);
+      }
+      return;
+    }
+    // several segments: lane i resolves key i0 + i % 32; keys past the last read its slot and count as zero
+    const int i = i0 + (lane & 31), end = min(i0 + BK, G);
+    int where = -1, last = 0, begin = i0;
+    while (begin < end) {
+      const int e = __builtin_amdgcn_readlane(incl, s), d = __builtin_amdgcn_readlane(shift, s);
+      where = i >= begin && i < min(e, end) ? i + d : where;
+      last = e > begin ? min(e, end) - 1 + d : last;
+      begin = max(begin, e);
+      if (++s == 64 && begin < end) {
+        window_of(begin);
+        s = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= begin));
+      }
+    }
+    const int slot = where < 0 ? last : where;
+    const bool real = where >= 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t r = __shfl(slot, ka + 4 * h, 64);
+      x.k[h] = *(const __attribute__((address_space(1))) krow_t*)((gptr)a.k4 + r * cbytes + kc);
+      x.ks[h] = *(const __attribute__((address_space(1))) uint8_t*)((gptr)a.ks + r * sbytes + ksc);
+      const int64_t rv = __shfl(slot, 8 * j + 4 * h + (n & 3), 64);
+      const bool ok = __shfl((int)real, 8 * j + 4 * h + (n & 3), 64);
+      const uint32_t b = *(const __attribute__((address_space(1))) uint8_t*)((gptr)a.vs + rv * sbytes + vsc);
+      x.vs[h] = ok ? b : 127;
+    }
+#pragma unroll
+    for (int i8 = 0; i8 < 8; ++i8) {
+      const int64_t r = __shfl(slot, 8 * j + i8, 64);
+      const bool ok = __shfl((int)real, 8 * j + i8, 64);
+      uint32_t w;
+      if constexpr (D == 128) w = *(const __attribute__((address_space(1))) uint32_t*)((gptr)a.v4 + r * cbytes + vc);
+      else w = *(const __attribute__((address_space(1))) uint16_t*)((gptr)a.v4 + r * cbytes + vc);
+      x.v[i8] = ok ? w : 0;
+    }
+  };
+  auto q4_block = [&](int i0, const Q4Block& x) __attribute__((always_inline)) {
+    bf16x8 kf[2][NKS];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) kf[h][ks] = __builtin_bit_cast(bf16x8, q4_eight(x.k[h][ks], q4_scale(x.ks[h])));
+    bf16x8 pf[NRB];
+    const int lim = G - 1 - i0;
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+      f32x4 s[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][ks], qf[rb][ks], s[h], 0, 0, 0);
+      }
+      pf[rb] = softmax(s, rb, lim, lim < BK - 1);
+    }
+    float vs[8];
+    const uint32_t b0 = x.vs[0] << 23, b1 = x.vs[1] << 23;
+    vs[0] = __uint_as_float(dpp<0x00>(b0)); vs[1] = __uint_as_float(dpp<0x55>(b0));
+    vs[2] = __uint_as_float(dpp<0xAA>(b0)); vs[3] = __uint_as_float(dpp<0xFF>(b0));
+    vs[4] = __uint_as_float(dpp<0x00>(b1)); vs[5] = __uint_as_float(dpp<0x55>(b1));
+    vs[6] = __uint_as_float(dpp<0xAA>(b1)); vs[7] = __uint_as_float(dpp<0xFF>(b1));
+    auto two_dims = [&](auto sel) __attribute__((always_inline)) {
+      constexpr int E = 2 * decltype(sel)::value;
+      uint32_t p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = q4_pair<E / 2>(x.v[i], vs[i]);
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd) {
+        u32x4 w;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = __builtin_amdgcn_perm(p[2 * q + 1], p[2 * q], odd ? 0x07060302u : 0x05040100u);
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb)
+          o[rb][E + odd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb], o[rb][E + odd], 0, 0, 0);
+      }
+    };
+    two_dims(std::integral_constant<int, 0>{});
+    two_dims(std::integral_constant<int, 1>{});
+    if constexpr (VE == 8) {
+      two_dims(std::integral_constant<int, 2>{});
+      two_dims(std::integral_constant<int, 3>{});
+    }
+  };
+
+  // ---- the wave's blocks
+  for (int b = b_lo + wave; b < b_hi; b += NW) {
+    int lim[NRB];
+    if (b >= nb_s && b < nb_s + nb_g) {
+      Q4Block x;
+      load_q4((b - nb_s) * BK, x);
+      q4_block((b - nb_s) * BK, x);
+    } else {
+      const bool sink = b < nb_s;
+      const int row0 = (sink ? b : b - nb_s - nb_g) * BK;
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) lim[rb] = (sink ? a.S - 1 : tail0 + tok[rb]) - row0;
+      bf16_block(sink ? a.sink_k : a.tail_k, sink ? a.sink_v : a.tail_v, sink ? a.S : a.T, row0, lim,
+                 row0 + BK - 1 > (sink ? a.S - 1 : tail_first));
+    }
+  }
+
+  // ---- merge of the waves: O^T lane (n, j) holds row n, dims VE*(4j+i) + e
+#pragma unroll
+  for (int rb = 0; rb < NRB; ++rb) {
+    float l = l_run[rb];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (j == 0) {
+      m_s[wave][rb * 16 + n] = m_run[rb];
+      l_s[wave][rb * 16 + n] = l;
+    }
+    float* op = &o_s[wave][rb * 16 + n][VE * 4 * j];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < VE; e += 4)
+        *(f32x4*)(op + i * VE + e) = f32x4{o[rb][e][i], o[rb][e + 1][i], o[rb][e + 2][i], o[rb][e + 3][i]};
+  }
+  __syncthreads();
+  constexpr int NQ = D / 4;
+  const int rows = min(RT, NR - rt * RT);
+  for (int it = tid; it < rows * NQ; it += NW * 64) {
+    const int r = it / NQ, dq = it % NQ;
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, m_s[w][r]);
+    const float m_use = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = __builtin_amdgcn_exp2f(m_s[w][r] - m_use);      // 0 for a wave that saw no key of the row
+      l += f * l_s[w][r];
+      acc += f * *(const f32x4*)&o_s[w][r][dq * 4];
+    }
+    acc *= l > 0.f ? 1.f / l : l == l ? 0.f : l;                       // an empty row is 0, a NaN stays one
+    const float lse2 = l > 0.f ? m_use + __log2f(l) : l == l ? -INFINITY : l;
+    const int pr = rt * RT + r, t = pr / g, h = kv * g + pr % g;
+    if (a.parts > 1) {
+      const int64_t prow = ((int64_t)part * a.Hq + h) * a.Lq + t;      // the merge kernel's layout
+      *(f32x4*)(a.ws_o + prow * D + dq * 4) = acc;
+      if (dq == 0) a.ws_lse[prow] = lse2;
+      continue;
+    }
+    const int64_t oo = ((int64_t)t * a.Hq + h) * D + dq * 4;
+    if (a.out_f32) *(f32x4*)((float*)a.out + oo) = acc;
+    else *(bf16x4*)((__bf16*)a.out + oo) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
+    if (dq == 0 && a.lse) a.lse[(int64_t)h * a.Lq + t] = lse2 * kLn2;
+  }
+}
+
+template <int D>
+hipError_t launch(const RowsQ4Args& a, hipStream_t stream) {
+  const dim3 grid(a.n_rt * a.parts * a.Hkv);
+  if (a.row_blocks == 1) hipLaunchKernelGGL((attn_rows_q4_kernel<D, 1, 8>), grid, dim3(512), 0, stream, a);
+  else if (a.row_blocks == 2) hipLaunchKernelGGL((attn_rows_q4_kernel<D, 2, 8>), grid, dim3(512), 0, stream, a);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rows_q4(const RowsQ4Args& a, hipStream_t stream) {
+  if (a.n_segs > kMaxSegments || a.n_rt < 1 || a.parts < 1) return hipErrorInvalidValue;
+  return a.D == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
+}
+
+}  // namespace vico

@@ -17,7 +17,7 @@
 #include <ATen/core/Tensor.h>
 #include <c10/hip/HIPStream.h>
 
-#include "vico.h"
+#include "vico_cache.h"
 
 namespace {
 
@@ -285,9 +285,136 @@ PyObject* temporal_drop(PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// The calls of vico_cache.h take tensors of the current device only.
+template <class... T>
+bool here(const T*... t) {
+  const int dev = c10::hip::current_device();
+  return ((!t || t->device().index() == dev) && ...);
+}
+bool same_shape(const at::Tensor* a, const at::Tensor* b) { return a->sizes() == b->sizes(); }
+
+// the store's arrays: codes of [slots][heads][dim / 2], scales of [slots][heads][dim / 32]
+struct Store {
+  const at::Tensor *k, *v, *ks, *vs;
+  explicit Store(Args& in)
+      : k(in.tensor(at::kByte, 3)), v(in.tensor(at::kByte, 3)), ks(in.tensor(at::kByte, 3)), vs(in.tensor(at::kByte, 3)) {}
+  bool fits(int64_t heads, int64_t dim) const {
+    return shape3(k, k->size(0), heads, dim / 2) && same_shape(k, v) && shape3(ks, k->size(0), heads, dim / 32) &&
+           same_shape(ks, vs) && here(k, v, ks, vs);
+  }
+};
+
+// a [tokens][heads][dim] bf16 tensor whose heads are dense: a slice of a packed projection
+const at::Tensor* head_rows(Args& in, bool optional) {
+  PyObject* o = in.next();
+  if (o == Py_None) return optional ? nullptr : in.no();
+  if (!THPVariable_CheckExact(o)) return in.no();
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || t.scalar_type() != at::kBFloat16 || t.dim() != 3 || t.stride(2) != 1 ||
+      (t.size(1) != 1 && t.stride(1) != t.size(2)))
+    return in.no();
+  return &t;
+}
+int64_t row_stride(const at::Tensor* t) { return t->size(0) > 1 ? t->stride(0) : t->size(1) * t->size(2); }
+
+// q, k, positions, inv_freq, q_out, k_out, v, v_out, q_weight, k_weight, eps, s0, s1, s2, flags, stream
+PyObject* qk_norm_rope(PyObject* const* args, Py_ssize_t n) {
+  Args in{args, n};
+  const at::Tensor *q = head_rows(in, false), *k = head_rows(in, false), *pos = in.tensor(at::kInt, 2);
+  const at::Tensor *freq = in.tensor(at::kFloat, 1), *qo = in.tensor(at::kBFloat16, 3), *ko = in.tensor(at::kBFloat16, 3);
+  const at::Tensor *v = head_rows(in, true), *vo = in.tensor(at::kBFloat16, 3, true);
+  const at::ScalarType wt = in.i < n && THPVariable_CheckExact(args[in.i]) ? THPVariable_Unpack(args[in.i]).scalar_type()
+                            : in.i + 1 < n && THPVariable_CheckExact(args[in.i + 1])
+                                ? THPVariable_Unpack(args[in.i + 1]).scalar_type() : at::kBFloat16;
+  if (wt != at::kBFloat16 && wt != at::kFloat) Py_RETURN_NONE;
+  const at::Tensor *qw = in.tensor(wt, 1, true), *kw = in.tensor(wt, 1, true);
+  const float eps = in.real();
+  const int32_t sections[3] = {in.int32(), in.int32(), in.int32()};
+  const int32_t flags = in.int32();
+  void* stream = in.stream();
+  if (!in.ok || !v != !vo || !here(q, k, pos, freq, qo, ko, v, vo, qw, kw)) Py_RETURN_NONE;
+  const int64_t T = q->size(0), D = q->size(2), axes = pos->size(0);
+  if (!same_shape(q, qo) || !same_shape(k, ko) || k->size(0) != T || k->size(2) != D || pos->size(1) != T) Py_RETURN_NONE;
+  if (v && (!same_shape(v, k) || !same_shape(vo, k))) Py_RETURN_NONE;
+  if ((qw && qw->size(0) != D) || (kw && kw->size(0) != D) || !fits(q) || !fits(k) || freq->size(0) > D) Py_RETURN_NONE;
+  void *const a = wptr(qo), *const b = wptr(ko), *const c = wptr(vo);
+  return called(in, [&] {
+    return vico_qk_norm_rope(ptr(q), row_stride(q), ptr(k), row_stride(k), ptr(v), v ? row_stride(v) : 0, (int32_t)T,
+                             size(q, 1), size(k, 1), (int32_t)D, ptr(qw), ptr(kw),
+                             wt == at::kFloat ? VICO_DTYPE_F32 : VICO_DTYPE_BF16, eps, (const int32_t*)ptr(pos),
+                             (int32_t)axes, (const float*)ptr(freq), 2 * size(freq, 0), axes == 3 ? sections : nullptr,
+                             flags, a, b, c, stream);
+  });
+}
+
+// k_chunk, v_chunk, the store, hist_len, stream
+PyObject* append_q4(PyObject* const* args, Py_ssize_t n) {
+  Args in{args, n};
+  const at::Tensor *kc = in.tensor(at::kBFloat16, 3), *vc = in.tensor(at::kBFloat16, 3);
+  const Store s(in);
+  const int64_t hist = in.integer();
+  void* stream = in.stream();
+  if (!in.ok || !same_shape(kc, vc) || !s.fits(kc->size(1), kc->size(2)) || !here(kc, vc)) Py_RETURN_NONE;
+  if (!fits(kc) || !fits(s.k)) Py_RETURN_NONE;
+  void *const a = wptr(s.k), *const b = wptr(s.v), *const c = wptr(s.ks), *const d = wptr(s.vs);
+  return called(in, [&] {
+    return vico_kv_append_q4(ptr(kc), ptr(vc), size(kc, 0), a, b, c, d, size(s.k, 0), hist, size(kc, 1), size(kc, 2), stream);
+  });
+}
+
+// the store, seg_start, seg_len, out_k, out_v, out_count, stream
+PyObject* load_q4(PyObject* const* args, Py_ssize_t n) {
+  Args in{args, n};
+  const Store s(in);
+  const at::Tensor *ss = in.tensor(at::kLong, 1), *sl = in.tensor(at::kInt, 1);
+  const at::Tensor *ok = in.tensor(at::kBFloat16, 3), *ov = in.tensor(at::kBFloat16, 3), *cnt = in.tensor(at::kInt, 1, true);
+  void* stream = in.stream();
+  if (!in.ok || !same_shape(ok, ov) || !same_shape(ss, sl) || !s.fits(ok->size(1), ok->size(2))) Py_RETURN_NONE;
+  if (!here(ss, sl, ok, ov, cnt) || !fits(ok) || !fits(s.k) || (cnt && cnt->size(0) < 1)) Py_RETURN_NONE;
+  void *const a = wptr(ok), *const b = wptr(ov), *const c = wptr(cnt);
+  return called(in, [&] {
+    return vico_kv_load_q4(ptr(s.k), ptr(s.v), ptr(s.ks), ptr(s.vs), size(s.k, 0), (const int64_t*)ptr(ss),
+                           (const int32_t*)ptr(sl), size(ss, 0), a, b, size(ok, 0), (int32_t*)c, size(ok, 1), size(ok, 2),
+                           stream);
+  });
+}
+
+// q, tail_k, tail_v, sink_k, sink_v, the store, seg_start, seg_len, out, lse, keys_hint, num_splits, softmax_scale,
+// stream, workspace
+PyObject* gather_q4(PyObject* const* args, Py_ssize_t n) {
+  Args in{args, n};
+  const at::Tensor *q = in.tensor(at::kBFloat16, 3), *tk = in.tensor(at::kBFloat16, 3), *tv = in.tensor(at::kBFloat16, 3);
+  const at::Tensor *sk = in.tensor(at::kBFloat16, 3, true), *sv = in.tensor(at::kBFloat16, 3, true);
+  const Store s(in);
+  const at::Tensor *ss = in.tensor(at::kLong, 1, true), *sl = in.tensor(at::kInt, 1, true);
+  const at::Tensor* out = in.output();
+  const at::Tensor* lse = in.tensor(at::kFloat, 2, true);
+  const int64_t hint = in.integer();
+  const int32_t splits = in.int32();
+  const float scale = in.real();
+  void* stream = in.stream();
+  const at::Tensor* ws = in.memory(true);
+  if (!in.ok || !same_shape(out, q) || !same_shape(tk, tv) || tk->size(2) != q->size(2) || !ss != !sl || !sk != !sv)
+    Py_RETURN_NONE;
+  if ((ss && !same_shape(ss, sl)) || (sk && (!same_shape(sk, sv) || sk->size(1) != tk->size(1) || sk->size(2) != tk->size(2))))
+    Py_RETURN_NONE;
+  if (lse && (lse->size(0) != q->size(1) || lse->size(1) != q->size(0))) Py_RETURN_NONE;
+  if (!s.fits(tk->size(1), q->size(2)) || !here(q, tk, tv, sk, sv, ss, sl, out, lse, ws)) Py_RETURN_NONE;
+  if (!fits(q) || !fits(tk) || !fits(sk) || !fits(s.k) || !fits(ss)) Py_RETURN_NONE;
+  void *const o = wptr(out), *const l = wptr(lse), *const w = wptr(ws);
+  return called(in, [&] {
+    return vico_gather_attn_q4(ptr(q), size(q, 0), ptr(tk), ptr(tv), size(tk, 0), ptr(sk), ptr(sv), size(sk, 0), ptr(s.k),
+                               ptr(s.v), ptr(s.ks), ptr(s.vs), size(s.k, 0), (const int64_t*)ptr(ss),
+                               (const int32_t*)ptr(sl), size(ss, 0), hint, size(q, 1), size(tk, 1), size(q, 2), scale, o,
+                               out->scalar_type() == at::kFloat ? VICO_DTYPE_F32 : VICO_DTYPE_BF16, (float*)l, splits, w,
+                               bytes(ws), stream);
+  });
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(prefill),      FAST(gather),      FAST(gather_noalloc), FAST(kv_append), FAST(token_mean),
-                         FAST(chunk_scores), FAST(topk_chunks), FAST(temporal_drop),  {nullptr, nullptr, 0, nullptr}};
+                         FAST(chunk_scores), FAST(topk_chunks), FAST(temporal_drop),
+                         FAST(qk_norm_rope), FAST(append_q4),   FAST(load_q4),        FAST(gather_q4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_vico_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

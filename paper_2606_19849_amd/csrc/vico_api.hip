@@ -9,31 +9,27 @@
 
 #include "vico.h"
 #include "vico_internal.h"
+#include "host_util.h"
 #include "token_drop.h"
 
 namespace {
 
 thread_local int g_last_hip_error = 0;
 
-constexpr int64_t kMaxChunk = int64_t(1) << 20;
-constexpr int64_t kMaxKeys = int64_t(1) << 30;
-constexpr int kMaxHeads = 1024;
-constexpr int64_t kMaxTensorBytes = int64_t(1) << 31;
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-bool overlaps(const void* a, int64_t na, const void* b, int64_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
-}
+using vico::aligned16;
+using vico::aligned_to;
+using vico::align256;
+using vico::kMaxChunk;
+using vico::kMaxHeads;
+using vico::kMaxKeys;
+using vico::kMaxTensorBytes;
+using vico::overlaps;
 
 struct Shape {
   int C, S, R, Wv, ws, Hq, Hkv, D, splits, balanced, grid, bidir, pack;
   int64_t total_tiles;
   int64_t ws_bytes;
 };
-
-int64_t align256(int64_t x) { return (x + 255) & ~int64_t(255); }
 
 // Row tiles of one head group: its C * pack packed rows ((token, query head)
 // pairs, token-major) in blocks of kBlockM.
@@ -314,8 +310,6 @@ int append_groups(const Shape& sh, int64_t work) {
   const int64_t idle = (vico::kNumCUs - work % vico::kNumCUs) % vico::kNumCUs, beside = std::min<int64_t>(most, kBeside);
   return (int)(beside <= idle ? beside : std::min<int64_t>(most, vico::kNumCUs));
 }
-
-bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 int hip_fail(hipError_t e) {
   g_last_hip_error = (int)e;

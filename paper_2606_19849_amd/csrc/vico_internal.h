@@ -54,6 +54,7 @@ struct AttnArgs {
   int app_p0;          // first ring slot written = hist_len mod R
   int app_blocks;      // > 0: extra work-groups of the attention launch that append (no split; the
                        // written slots are outside the window)
+  int nan_lse;              // merge: the log-sum-exp of a row with NaN logits is NaN (0: -inf)
 };
 
 // Short-query attention over gathered key segments: query rows are the last
@@ -122,6 +123,73 @@ struct RowsArgs {
   AppendArgs app;
 };
 
+// ---- the 4-bit store (q4_common.h)
+struct AppendQ4Args {
+  const uint16_t* kc;      // [C][row_elems]
+  const uint16_t* vc;
+  uint8_t* k4;             // codes, [R][row_elems / 2]
+  uint8_t* v4;
+  uint8_t* ks;             // scales, [R][row_elems / 32]
+  uint8_t* vs;
+  int C, R, p0;            // p0 = hist_len mod R
+  int row_elems;           // Hkv * D
+};
+
+struct LoadQ4Args {
+  const uint8_t* k4;
+  const uint8_t* v4;
+  const uint8_t* ks;
+  const uint8_t* vs;
+  const int64_t* seg_start;
+  const int32_t* seg_len;
+  uint16_t* k;             // [out_rows][row_elems]
+  uint16_t* v;
+  int32_t* out_count;      // may be null
+  int cap, n_segs, out_rows, row_elems;
+};
+
+// Keys as in GatherArgs, the store in 4 bits; row tiles and parts as in RowsArgs.
+struct RowsQ4Args {
+  const uint16_t* q;
+  const uint16_t* tail_k;
+  const uint16_t* tail_v;
+  const uint16_t* sink_k;
+  const uint16_t* sink_v;
+  const uint8_t* k4;
+  const uint8_t* v4;
+  const uint8_t* ks;
+  const uint8_t* vs;
+  const int64_t* seg_start;
+  const int32_t* seg_len;
+  void* out;
+  float* lse;               // may be null
+  float* ws_o;              // [parts][Hq][Lq][D] fp32 when parts > 1
+  float* ws_lse;            // [parts][Hq][Lq] (log2 units)
+  int Lq, T, S, cap, n_segs;
+  int Hq, Hkv, D;
+  int parts, n_rt, row_blocks;
+  int out_f32;
+  float scale_log2;
+};
+
+struct RopeArgs {
+  const uint16_t* q;        // token t at q + t * q_stride (elements), its heads dense
+  const uint16_t* k;
+  const uint16_t* v;        // null: no values to copy
+  uint16_t* q_out;          // dense
+  uint16_t* k_out;
+  uint16_t* v_out;
+  const void* q_weight;     // null: no norm
+  const void* k_weight;
+  const int32_t* positions; // [axes][T]
+  const float* inv_freq;    // [rot / 2]
+  int64_t q_stride, k_stride, v_stride;
+  int T, Hq, Hkv, D;
+  int axes, rot, s0, s1, s2;
+  int adjacent, strided, weight_f32;
+  float eps;
+};
+
 // The append of a chunk, ring[(p0 + j) mod R] <- chunk[j] for K and V, as
 // 16-byte units: unit u in [0, 2*C*row_elems/8) (K units first, then V);
 // threads take units first, first + stride, ...  Consecutive threads move
@@ -150,6 +218,11 @@ hipError_t launch_append(const AppendArgs& a, hipStream_t stream);
 hipError_t launch_gather(const GatherArgs& a, hipStream_t stream);
 // The rows kernel alone; the caller merges when parts > 1.
 hipError_t launch_rows(const RowsArgs& a, hipStream_t stream);
+hipError_t launch_append_q4(const AppendQ4Args& a, hipStream_t stream);
+hipError_t launch_load_q4(const LoadQ4Args& a, hipStream_t stream);
+// As launch_rows: the caller merges when parts > 1.
+hipError_t launch_rows_q4(const RowsQ4Args& a, hipStream_t stream);
+hipError_t launch_qk_norm_rope(const RopeArgs& a, hipStream_t stream);
 // Records e as the calling thread's last HIP error; returns VICO_ERR_HIP.
 int record_hip_failure(hipError_t e);
 

@@ -45,7 +45,6 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
   constexpr int RT = 16 * NRB;             // rows of the work-group
   constexpr int BK = kRowsBlock;           // keys per block
   constexpr int OS = D + 8;                // row stride of the merge buffer (floats)
-  constexpr int PER = kMaxSegments / (NW * 64);
   static_assert(BK == 32, "two 16-key products per block");
   typedef uint32_t krow_t __attribute__((ext_vector_type(DPL / 8)));
   typedef uint32_t vrow_t __attribute__((ext_vector_type(VE / 2)));
@@ -53,10 +52,7 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
 
   __shared__ __attribute__((aligned(16))) float o_s[NW][RT][OS];
   __shared__ float m_s[NW][RT], l_s[NW][RT];
-  // segment table of a call with more segments than lanes; the merge buffer is not in use yet, but blocks are
-  // looked up while other waves merge
-  __shared__ int incl_s[kMaxSegments], shift_s[kMaxSegments];
-  __shared__ int wave_s[NW];
+  __shared__ typename Segments<NW * 64>::Lds seg_s;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -70,64 +66,9 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
   const int part = (L / a.n_rt) % a.parts;
   const int kv = L / (a.n_rt * a.parts);
 
-  // ---- segment table: the lanes hold a window of 64 segments, `incl` keys up to a segment's end, `shift` from
-  // gathered key to slot.  Up to 64 segments that is all; more are scanned by the work-group into LDS.
-  auto clipped = [&](int s, int& slot) __attribute__((always_inline)) {
-    const int64_t st = a.seg_start[s], en = st + (int64_t)a.seg_len[s];
-    const int64_t lo = st > 0 ? st : 0, hi = en < (int64_t)a.cap ? en : (int64_t)a.cap;
-    slot = hi > lo ? (int)lo : 0;
-    return hi > lo ? (int)(hi - lo) : 0;
-  };
-  auto scan = [&](int x) __attribute__((always_inline)) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(x, o, 64);
-      x += lane >= o ? y : 0;
-    }
-    return x;
-  };
-  int incl = 0, shift = 0, G = 0, win = 0;
-  if (a.n_segs > 64) {
-    int len[PER], run = 0;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const int s = tid * PER + e;
-      int slot = 0;
-      len[e] = s < a.n_segs ? clipped(s, slot) : 0;
-      shift_s[s] = slot;
-      run += len[e];
-    }
-    const int upto = scan(run);
-    if (lane == 63) wave_s[wave] = upto;
-    __syncthreads();
-    int base = upto - run;
-    for (int w = 0; w < wave; ++w) base += wave_s[w];
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const int s = tid * PER + e;
-      shift_s[s] -= base;
-      base += len[e];
-      incl_s[s] = base;
-    }
-    __syncthreads();
-    G = __builtin_amdgcn_readfirstlane(incl_s[kMaxSegments - 1]);
-    incl = incl_s[lane];
-    shift = shift_s[lane];
-  } else {
-    int slot = 0;
-    const int len = lane < a.n_segs ? clipped(lane, slot) : 0;
-    incl = scan(len);
-    shift = slot - (incl - len);
-    G = __builtin_amdgcn_readlane(incl, 63);
-  }
-  // the window that holds gathered key i (0 <= i < G); keys are asked for in rising order
-  auto window_of = [&](int i) __attribute__((always_inline)) {
-    while (__builtin_amdgcn_readlane(incl, 63) <= i) {      // there are further segments: incl of the last one is G
-      win += 64;
-      incl = incl_s[win + lane];
-      shift = shift_s[win + lane];
-    }
-  };
+  int incl, shift, win;
+  const Segments<NW * 64> seg{seg_s, incl, shift, win};
+  const int G = seg.build(a.seg_start, a.seg_len, a.n_segs, a.cap);
 
   // ---- Q rows as B fragments; rows past the end repeat the last one and are never stored
   bf16x8 qf[NRB][NKS];
@@ -302,13 +243,12 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
     uint32_t ks[2], vs[2];        // scale bytes: K of the two keys; V of keys 8j + n%4, 8j + 4 + n%4
   };
   auto load_q4 = [&](int i0, Q4Block& x) __attribute__((always_inline)) {      // gathered keys i0 .. i0 + 31, i0 < G
-    window_of(i0);
-    int s = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= i0));      // segment of key i0, in the window
+    int slot0;
     const uint32_t kc = (uint32_t)(kv * (D / 2) + j * (DPL / 2)), vc = (uint32_t)(kv * (D / 2) + n * (VE / 2));
     const uint32_t ksc = (uint32_t)(kv * (D / kQ4Group) + kg), vsc = (uint32_t)(kv * (D / kQ4Group) + vg);
-    if (i0 + BK <= __builtin_amdgcn_readlane(incl, s)) {
+    if (seg.straight(i0, BK, slot0)) {
       // consecutive slots: base + fixed per-lane offsets
-      const int64_t slot = i0 + __builtin_amdgcn_readlane(shift, s);
+      const int64_t slot = slot0;
       const rsrc_t rk = make_rsrc(a.k4 + slot * cbytes, BK * cbytes), rv = make_rsrc(a.v4 + slot * cbytes, BK * cbytes);
       const rsrc_t rks = make_rsrc(a.ks + slot * sbytes, BK * sbytes), rvs = make_rsrc(a.vs + slot * sbytes, BK * sbytes);
 #pragma unroll
@@ -327,21 +267,9 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
       }
       return;
     }
-    // several segments: lane i resolves key i0 + i % 32; keys past the last read its slot and count as zero
-    const int i = i0 + (lane & 31), end = min(i0 + BK, G);
-    int where = -1, last = 0, begin = i0;
-    while (begin < end) {
-      const int e = __builtin_amdgcn_readlane(incl, s), d = __builtin_amdgcn_readlane(shift, s);
-      where = i >= begin && i < min(e, end) ? i + d : where;
-      last = e > begin ? min(e, end) - 1 + d : last;
-      begin = max(begin, e);
-      if (++s == 64 && begin < end) {
-        window_of(begin);
-        s = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= begin));
-      }
-    }
-    const int slot = where < 0 ? last : where;
-    const bool real = where >= 0;
+    // several segments, or the last ones: keys past the last read its slot and count as zero
+    bool real;
+    const int slot = seg.slot_of_lane(i0, BK, G, real);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int64_t r = __shfl(slot, ka + 4 * h, 64);

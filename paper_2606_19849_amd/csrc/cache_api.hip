@@ -40,9 +40,25 @@ bool collide(const Region (&w)[NW], const Region (&r)[NR]) {
 
 struct GatherQ4Shape {
   int Lq, T, S, cap, n_segs, Hq, Hkv, D;
-  int row_blocks, n_rt, parts;
+  int tile, row_blocks, n_rt, parts;     // tile: 256-row tiles; else 16 * row_blocks rows
   int64_t ws_bytes;
 };
+
+// Parts of the 256-row kernel: the count with the least time, in units of 0.1 us.  A round of work-groups takes
+// 5 us to start and end and 1.5 us a 64-key tile; a merge 4 us and the partials' way to memory and back.
+int tile_parts(int64_t groups, int64_t tiles, int64_t row_bytes, int64_t* cost) {
+  int best = 1;
+  *cost = INT64_MAX;
+  for (int p = 1; p <= kMaxGatherParts && p <= tiles; ++p) {
+    const int64_t rounds = (groups * p + kNumCUs - 1) / kNumCUs;
+    const int64_t c = rounds * (50 + 15 * ((tiles + p - 1) / p)) + (p > 1 ? 40 + p * row_bytes / 200000 : 0);
+    if (c < *cost) {
+      *cost = c;
+      best = p;
+    }
+  }
+  return best;
+}
 
 // Validates the shape arguments and plans: row tiles of 16 or 32 packed rows, and as many key-range parts as keep
 // the grid within one round of the CUs and leave each of a work-group's eight waves a block.
@@ -58,15 +74,24 @@ int check_gather_q4_shape(int32_t Lq, int32_t T, int32_t S, int32_t cap, int32_t
   if (row_bytes * T >= kMaxTensorBytes || row_bytes * S >= kMaxTensorBytes ||
       int64_t(Lq) * Hq * D * 4 >= kMaxTensorBytes)
     return VICO_ERR_INVALID_ARG;
-  *sh = GatherQ4Shape{Lq, T, S, cap, n_segs, Hq, Hkv, D, 1, 0, 1, 0};
+  *sh = GatherQ4Shape{Lq, T, S, cap, n_segs, Hq, Hkv, D, 0, 1, 0, 1, 0};
   if (Lq == 0) return VICO_OK;
   const int64_t rows = int64_t(Hq / Hkv) * Lq;
   const int64_t gathered = n_segs == 0 ? 0 : std::min<int64_t>(hint > 0 ? hint : cap, int64_t(n_segs) * cap);
-  const int64_t blocks = (S + gathered + T + kRowsBlock - 1) / kRowsBlock;
-  sh->row_blocks = rows > 16 ? 2 : 1;
-  sh->n_rt = (int)((rows + 16 * sh->row_blocks - 1) / (16 * sh->row_blocks));
-  const int64_t most = std::min<int64_t>(kNumCUs / (int64_t(Hkv) * sh->n_rt), (blocks + 7) / 8);
-  sh->parts = (int)std::min<int64_t>(splits > 0 ? splits : std::max<int64_t>(most, 1), kMaxGatherParts);
+  const int64_t keys = S + gathered + T;
+  int64_t most;
+  if (rows >= 128) {
+    sh->tile = 1;
+    sh->n_rt = (int)((rows + kBlockM - 1) / kBlockM);
+    int64_t cost;
+    most = tile_parts(int64_t(Hkv) * sh->n_rt, (keys + kKeyTile - 1) / kKeyTile, int64_t(4) * Hq * Lq * D, &cost);
+  } else {
+    sh->row_blocks = rows > 16 ? 2 : 1;
+    sh->n_rt = (int)((rows + 16 * sh->row_blocks - 1) / (16 * sh->row_blocks));
+    const int64_t blocks = (keys + kRowsBlock - 1) / kRowsBlock;
+    most = std::max<int64_t>(std::min<int64_t>(kNumCUs / (int64_t(Hkv) * sh->n_rt), (blocks + 7) / 8), 1);
+  }
+  sh->parts = (int)std::min<int64_t>(splits > 0 ? splits : most, kMaxGatherParts);
   if (sh->parts > 1) sh->ws_bytes = align256(int64_t(4) * sh->parts * Hq * Lq * D) + int64_t(4) * sh->parts * Hq * Lq;
   return VICO_OK;
 }
@@ -270,7 +295,7 @@ int vico_gather_attn_q4(const void* q, int32_t q_len, const void* tail_k, const 
   a.out_f32 = out_dtype == VICO_DTYPE_F32;
   const double scale = softmax_scale > 0.f ? double(softmax_scale) : 1.0 / sqrt(double(head_dim));
   a.scale_log2 = (float)(scale * 1.4426950408889634);
-  hipError_t e = launch_rows_q4(a, (hipStream_t)stream);
+  hipError_t e = sh.tile ? launch_tile_q4(a, (hipStream_t)stream) : launch_rows_q4(a, (hipStream_t)stream);
   if (e == hipSuccess && a.parts > 1) {
     AttnArgs m{};
     m.out = a.out; m.lse = a.lse; m.ws_o = a.ws_o; m.ws_lse = a.ws_lse;

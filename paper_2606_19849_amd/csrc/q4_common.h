@@ -34,4 +34,102 @@ __device__ __forceinline__ u32x4 q4_eight(uint32_t w, float scale) {
 
 __device__ __forceinline__ float q4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// The segment table of a work-group of NT threads.  The lanes of every wave
+// hold a window of 64 segments: `incl`, keys up to a segment's end, and
+// `shift`, from gathered key to slot.  Up to 64 segments that is all, and no
+// LDS or barrier stands between the table and the first key load; more are
+// scanned by the work-group into LDS, and a wave moves its window as it goes:
+// keys are asked for in rising order.  Segments are clipped to the store.
+template <int NT>
+struct Segments {
+  static constexpr int PER = kMaxSegments / NT;
+  static_assert(PER * NT == kMaxSegments, "segments of a thread");
+  struct Lds {
+    int incl[kMaxSegments], shift[kMaxSegments], wave[NT / 64];
+  };
+  static __device__ __forceinline__ int clipped(const int64_t* start, const int32_t* length, int s, int cap, int& slot) {
+    const int64_t st = start[s], en = st + (int64_t)length[s];
+    const int64_t lo = st > 0 ? st : 0, hi = en < (int64_t)cap ? en : (int64_t)cap;
+    slot = hi > lo ? (int)lo : 0;
+    return hi > lo ? (int)(hi - lo) : 0;
+  }
+  static __device__ __forceinline__ int scan(int x) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(x, o, 64);
+      x += (int)(threadIdx.x & 63) >= o ? y : 0;
+    }
+    return x;
+  }
+  // The state is the kernel's locals, the table in LDS, the lanes' window of it and the window's first segment:
+  Lds& l;
+  int &incl, &shift, &win;
+
+  // every thread of the work-group calls this; returns the keys of all segments
+  __device__ __forceinline__ int build(const int64_t* start, const int32_t* length, int n, int cap) const {
+    const int tid = threadIdx.x, lane = tid & 63;
+    win = 0;
+    int slot = 0;
+    if (n <= 64) {
+      const int len = lane < n ? clipped(start, length, lane, cap, slot) : 0;
+      incl = scan(len);
+      shift = slot - (incl - len);
+      return __builtin_amdgcn_readlane(incl, 63);
+    }
+    int len[PER], run = 0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int s = tid * PER + e;
+      len[e] = s < n ? clipped(start, length, s, cap, slot) : 0;
+      l.shift[s] = slot;
+      run += len[e];
+    }
+    const int upto = scan(run);
+    if (lane == 63) l.wave[tid >> 6] = upto;
+    __syncthreads();
+    int base = upto - run;
+    for (int w = 0; w < (tid >> 6); ++w) base += l.wave[w];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int s = tid * PER + e;
+      l.shift[s] -= base;
+      base += len[e];
+      l.incl[s] = base;
+    }
+    __syncthreads();
+    incl = l.incl[lane];
+    shift = l.shift[lane];
+    return __builtin_amdgcn_readfirstlane(l.incl[kMaxSegments - 1]);
+  }
+  // segment of gathered key i (0 <= i < the total) inside the window, which moves there
+  __device__ __forceinline__ int find(int i) const {
+    while (__builtin_amdgcn_readlane(incl, 63) <= i) {      // entries past the last segment hold the total
+      win += 64;
+      incl = l.incl[win + (threadIdx.x & 63)];
+      shift = l.shift[win + (threadIdx.x & 63)];
+    }
+    return __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= i));
+  }
+  // whether keys i .. i + n - 1 lie in consecutive slots, from slot0
+  __device__ __forceinline__ bool straight(int i, int n, int& slot0) const {
+    const int s = find(i);
+    slot0 = i + __builtin_amdgcn_readlane(shift, s);
+    return i + n <= __builtin_amdgcn_readlane(incl, s);
+  }
+  // slot of key i0 + lane % n (n: 32 or 64); a key past the last, `total` - 1, has its slot and real = false
+  __device__ __forceinline__ int slot_of_lane(int i0, int n, int total, bool& real) const {
+    const int i = i0 + (int)(threadIdx.x & (n - 1)), end = min(i0 + n, total);
+    int s = find(i0), slot = 0, last = 0, begin = i0;
+    while (begin < end) {
+      const int e = __builtin_amdgcn_readlane(incl, s), d = __builtin_amdgcn_readlane(shift, s);
+      slot = (i >= begin) & (i < e) ? i + d : slot;
+      last = e > begin ? min(e, end) - 1 + d : last;
+      begin = max(begin, e);
+      if (++s == 64 && begin < end) s = find(begin);
+    }
+    real = i < end;
+    return real ? slot : last;
+  }
+};
+
 }  // namespace vico

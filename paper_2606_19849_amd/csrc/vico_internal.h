@@ -220,8 +220,10 @@ hipError_t launch_gather(const GatherArgs& a, hipStream_t stream);
 hipError_t launch_rows(const RowsArgs& a, hipStream_t stream);
 hipError_t launch_append_q4(const AppendQ4Args& a, hipStream_t stream);
 hipError_t launch_load_q4(const LoadQ4Args& a, hipStream_t stream);
-// As launch_rows: the caller merges when parts > 1.
+// As launch_rows: the caller merges when parts > 1.  Row tiles of 16 * row_blocks
+// packed rows, and of 256.
 hipError_t launch_rows_q4(const RowsQ4Args& a, hipStream_t stream);
+hipError_t launch_tile_q4(const RowsQ4Args& a, hipStream_t stream);
 hipError_t launch_qk_norm_rope(const RopeArgs& a, hipStream_t stream);
 // Records e as the calling thread's last HIP error; returns VICO_ERR_HIP.
 int record_hip_failure(hipError_t e);

@@ -246,7 +246,7 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
     int slot0;
     const uint32_t kc = (uint32_t)(kv * (D / 2) + j * (DPL / 2)), vc = (uint32_t)(kv * (D / 2) + n * (VE / 2));
     const uint32_t ksc = (uint32_t)(kv * (D / kQ4Group) + kg), vsc = (uint32_t)(kv * (D / kQ4Group) + vg);
-    if (seg.straight(i0, BK, slot0)) {
+    if (seg.straight(i0, slot0) >= BK) {
       // consecutive slots: base + fixed per-lane offsets
       const int64_t slot = slot0;
       const rsrc_t rk = make_rsrc(a.k4 + slot * cbytes, BK * cbytes), rv = make_rsrc(a.v4 + slot * cbytes, BK * cbytes);

@@ -13,7 +13,9 @@
 //   * One barrier a tile.  After the barrier in the middle of step t the thread
 //     converts tile t + 2, whose codes it has in registers, writes it to LDS and
 //     sends the loads of tile t + 3, which have a whole step to arrive.  Sink and
-//     tail tiles are bf16: their loads go straight to LDS.
+//     tail tiles are bf16: their loads go straight to LDS.  Inside a run of tiles
+//     in one segment the conversion and the loads are dealt out over the slots of
+//     the tile body's second half, in the shadow of its MFMAs.
 //   * A tile lies in one region (sink, store, tail); the regions' last tiles may
 //     be part-filled, with zeros that the mask hides.
 //   * Values of tail tokens that are not finite are zeros in LDS (0 times such a
@@ -40,6 +42,7 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   constexpr int NDB = Tile::NDB, NKS = Tile::NKS;
   constexpr int NB = 4;                      // tile t in buffer t mod NB; steps t - 1 .. t + 2 are in use
   constexpr uint32_t kKBase = NB * TBY, kWrap = NB * TBY - 1;
+  static_assert(6 * NLD <= Tile::NSLOT, "a tile's conversion and loads fit a body's slots");
   static_assert(NLD * NW * 1024 == TBY && BN == 64 && (NB & (NB - 1)) == 0, "tile geometry");
   typedef __attribute__((address_space(3))) u32x4* lds_u4;
   typedef const __attribute__((address_space(1))) char* gptr;
@@ -116,26 +119,63 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
         : "v"(off), "s"(r), "s"(to)
         : "memory");
   };
-  // sends the loads of tile t: codes and scale bytes to registers, bf16 rows to their buffers at `boff`
+  // Codes.  Consecutive tiles in one segment are a run: their loads share the per-lane offsets, and the bases move
+  // on.  A wave's chunks differ by RPL rows, and K's units by an exclusive or of the lowest bit.
   uint32_t kc[NLD], vc[NLD], ks[NLD], vs[NLD];
+  uint32_t k_off[NLD], v_off, ks_off, vs_off;
+  {
+    int rk, uk, rv, uv;
+    place(0, rk, uk, rv, uv);
+    v_off = (uint32_t)(rv * cbytes + kv * (D / 2) + uv * 4);
+    ks_off = (uint32_t)(rk * sbytes + kv * (D / kQ4Group) + uk / 4);
+    vs_off = (uint32_t)(rv * sbytes + kv * (D / kQ4Group) + uv / 4);
+#pragma unroll
+    for (int n = 0; n < NLD; ++n) k_off[n] = (uint32_t)((rk + n * RPL) * cbytes + kv * (D / 2) + (uk ^ n) * 4);
+  }
+  static_assert(NLD == 1 || Tile::CPB == 4, "K units of a wave's two chunks");
+  const uint8_t *run_k = nullptr, *run_v = nullptr, *run_ks = nullptr, *run_vs = nullptr;
+  int run_left = 0;                          // tiles left in the run, all below t_hi
+  constexpr int NLOAD = 4 * NLD;
+  auto load_run = [&](auto job) __attribute__((always_inline)) {
+    constexpr int n = decltype(job)::value / 4, what = decltype(job)::value % 4;
+    if constexpr (what == 0) kc[n] = __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(run_k, BN * cbytes), k_off[n], 0, 0);
+    if constexpr (what == 1) vc[n] = __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(run_v, BN * cbytes), v_off + n * RPL * cbytes, 0, 0);
+    if constexpr (what == 2) ks[n] = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(run_ks, BN * sbytes), ks_off + n * RPL * sbytes, 0, 0);
+    if constexpr (what == 3) vs[n] = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(run_vs, BN * sbytes), vs_off + n * RPL * sbytes, 0, 0);
+  };
+  auto advance_run = [&]() __attribute__((always_inline)) {
+    run_k += BN * cbytes;
+    run_v += BN * cbytes;
+    run_ks += BN * sbytes;
+    run_vs += BN * sbytes;
+    --run_left;
+  };
+  // codes in the registers to the buffers at `boff`: job 2n: K, 2n + 1: V
+  constexpr int NCVT = 2 * NLD;
+  auto convert = [&](auto job, uint32_t boff) __attribute__((always_inline)) {
+    constexpr int n = decltype(job)::value / 2;
+    const uint32_t at = lds0 + boff + my_part + (uint32_t)(lane * 16 + n * 1024);
+    if constexpr (decltype(job)::value % 2 == 0) *(lds_u4)(uintptr_t)(at + kKBase) = q4_eight(kc[n], q4_scale(ks[n]));
+    else *(lds_u4)(uintptr_t)at = q4_eight(vc[n], q4_scale(vs[n]));
+  };
+
+  // sends the loads of tile t: codes and scale bytes to registers, bf16 rows to their buffers at `boff`
   auto send = [&](int t, uint32_t boff) __attribute__((always_inline)) {
     if (t >= t_hi) return;
     if (t >= nb_s && t < nb_sg) {
       const int i0 = (t - nb_s) * BN;
-      int slot0;
-      if (seg.straight(i0, BN, slot0)) {
-        const int64_t s = slot0;
-        const rsrc_t rk = make_rsrc(a.k4 + s * cbytes, BN * cbytes), rv = make_rsrc(a.v4 + s * cbytes, BN * cbytes);
-        const rsrc_t rks = make_rsrc(a.ks + s * sbytes, BN * sbytes), rvs = make_rsrc(a.vs + s * sbytes, BN * sbytes);
-#pragma unroll
-        for (int n = 0; n < NLD; ++n) {
-          int k_row, k_unit, v_row, v_unit;
-          place(n, k_row, k_unit, v_row, v_unit);
-          kc[n] = __builtin_amdgcn_raw_buffer_load_b32(rk, (uint32_t)(k_row * cbytes + kv * (D / 2) + k_unit * 4), 0, 0);
-          vc[n] = __builtin_amdgcn_raw_buffer_load_b32(rv, (uint32_t)(v_row * cbytes + kv * (D / 2) + v_unit * 4), 0, 0);
-          ks[n] = __builtin_amdgcn_raw_buffer_load_b8(rks, (uint32_t)(k_row * sbytes + kv * (D / kQ4Group) + k_unit / 4), 0, 0);
-          vs[n] = __builtin_amdgcn_raw_buffer_load_b8(rvs, (uint32_t)(v_row * sbytes + kv * (D / kQ4Group) + v_unit / 4), 0, 0);
-        }
+      if (run_left == 0) {
+        int slot0;
+        const int n = seg.straight(i0, slot0);
+        run_left = min(n / BN, t_hi - t);
+        run_k = a.k4 + (int64_t)slot0 * cbytes;
+        run_v = a.v4 + (int64_t)slot0 * cbytes;
+        run_ks = a.ks + (int64_t)slot0 * sbytes;
+        run_vs = a.vs + (int64_t)slot0 * sbytes;
+      }
+      if (run_left > 0) {
+        unrolled<NLOAD>(load_run);
+        advance_run();
       } else {
         bool real;
         const int slot = seg.slot_of_lane(i0, BN, G, real);
@@ -172,17 +212,13 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   bool odd = false;                          // a value of the tail that is not finite
   auto finish = [&](int t, uint32_t boff) __attribute__((always_inline)) {
     if (t >= t_hi) return;
-    const uint32_t at = lds0 + boff + my_part + (uint32_t)(lane * 16);
     if (t >= nb_s && t < nb_sg) {
-#pragma unroll
-      for (int n = 0; n < NLD; ++n) {
-        *(lds_u4)(uintptr_t)(at + kKBase + n * 1024) = q4_eight(kc[n], q4_scale(ks[n]));
-        *(lds_u4)(uintptr_t)(at + n * 1024) = q4_eight(vc[n], q4_scale(vs[n]));
-      }
+      unrolled<NCVT>([&](auto job) __attribute__((always_inline)) { convert(job, boff); });
       return;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (t < nb_s) return;
+    const uint32_t at = lds0 + boff + my_part + (uint32_t)(lane * 16);
 #pragma unroll
     for (int n = 0; n < NLD; ++n) {
       u32x4 x = *(lds_u4)(uintptr_t)(at + n * 1024);
@@ -246,10 +282,24 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
           }
         });
         meet();
-        finish(t + 2, (boff + 2 * TBY) & kWrap);
-        send(t + 3, (boff + 3 * TBY) & kWrap);
         if (__builtin_expect(masked, 0)) Tile::mask(32, lim, hh, s1);
-        wt.template half<0, 16, 32>(s1, s0, p0, p1, [](auto) __attribute__((always_inline)) {});
+        const uint32_t fill = (boff + 2 * TBY) & kWrap;
+        // tile t + 2 is codes in the registers and t + 3 the run's next: one piece of that work a slot
+        const bool in_run = run_left > 0 && t + 2 >= nb_s;
+        if (!in_run) {
+          finish(t + 2, fill);
+          send(t + 3, (fill + TBY) & kWrap);
+        }
+        wt.template half<0, 16, 32>(s1, s0, p0, p1, [&](auto slot) __attribute__((always_inline)) {
+          constexpr int s = decltype(slot)::value;
+          if constexpr (s < NCVT + NLOAD) {
+            if (in_run) {
+              if constexpr (s < NCVT) convert(slot, fill);
+              else load_run(std::integral_constant<int, s - NCVT>{});
+            }
+          }
+        });
+        if (in_run) advance_run();
         v_nx += next - boff;                 // V of tile t + 1
         boff = next;
       }

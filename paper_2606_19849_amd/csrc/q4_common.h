@@ -110,11 +110,11 @@ struct Segments {
     }
     return __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= i));
   }
-  // whether keys i .. i + n - 1 lie in consecutive slots, from slot0
-  __device__ __forceinline__ bool straight(int i, int n, int& slot0) const {
+  // how many keys from i on lie in consecutive slots, from slot0
+  __device__ __forceinline__ int straight(int i, int& slot0) const {
     const int s = find(i);
     slot0 = i + __builtin_amdgcn_readlane(shift, s);
-    return i + n <= __builtin_amdgcn_readlane(incl, s);
+    return __builtin_amdgcn_readlane(incl, s) - i;
   }
   // slot of key i0 + lane % n (n: 32 or 64); a key past the last, `total` - 1, has its slot and real = false
   __device__ __forceinline__ int slot_of_lane(int i0, int n, int total, bool& real) const {
@@ -122,7 +122,7 @@ struct Segments {
     int s = find(i0), slot = 0, last = 0, begin = i0;
     while (begin < end) {
       const int e = __builtin_amdgcn_readlane(incl, s), d = __builtin_amdgcn_readlane(shift, s);
-      slot = (i >= begin) & (i < e) ? i + d : slot;
+      slot = ((i >= begin) & (i < e)) ? i + d : slot;
       last = e > begin ? min(e, end) - 1 + d : last;
       begin = max(begin, e);
       if (++s == 64 && begin < end) s = find(begin);

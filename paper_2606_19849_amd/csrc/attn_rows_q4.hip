@@ -5,7 +5,7 @@
 //   O = softmax(scale Q K^T) V,  K, V of a store row = code * 2^(scale byte - 127)
 //
 // Every wave takes 32-key blocks of its work-group's key range in turn, loads
-// them into registers, turns the codes into bf16 there (exactly) and keeps a
+// them into registers (the next block's codes while it computes one), turns the codes into bf16 there (exactly) and keeps a
 // running softmax of its own; the waves' states are merged through LDS at the
 // end.  A block lies in one region, so the three regions' last blocks may be
 // part-filled.
@@ -23,8 +23,9 @@
 // kernels; logits, softmax state and sums are fp32.
 //
 // A masked key's probability is 0, but 0 times a NaN or an infinity is not: in
-// a block that the causal mask cuts, such values are taken out of V and added
-// for the rows that see them alone.
+// a block that the causal mask cuts, such values of V are zeros and are added at
+// the end for the rows that see them (whatever its weight, such a value is the
+// row's result).
 
 #include "q4_common.h"
 
@@ -53,6 +54,7 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
   __shared__ __attribute__((aligned(16))) float o_s[NW][RT][OS];
   __shared__ float m_s[NW][RT], l_s[NW][RT];
   __shared__ typename Segments<NW * 64>::Lds seg_s;
+  __shared__ int odd_s;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -60,12 +62,14 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
   const int g = a.Hq / a.Hkv;
   const int NR = g * a.Lq;
 
-  // ---- work item: row tiles of one key range side by side (they share its K/V in an XCD's L2)
+  // ---- work item: the row tiles of one key range side by side, then its KV heads: they share its codes, and the
+  // heads the cache lines (a head's codes of a token are 64 or 32 bytes), in an XCD's L2
   const int L = xcd_remap(blockIdx.x, gridDim.x);
   const int rt = L % a.n_rt;
-  const int part = (L / a.n_rt) % a.parts;
-  const int kv = L / (a.n_rt * a.parts);
+  const int kv = (L / a.n_rt) % a.Hkv;
+  const int part = L / (a.n_rt * a.Hkv);
 
+  if (tid == 0) odd_s = 0;
   int incl, shift, win;
   const Segments<NW * 64> seg{seg_s, incl, shift, win};
   const int G = seg.build(a.seg_start, a.seg_len, a.n_segs, a.cap);
@@ -142,10 +146,38 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
     return p;
   };
 
-  // ---- a block of bf16 keys, rows row0 .. row0 + 31 of a tensor with `rows` (rows past it read as zero); the key
-  // index that lim[] masks by counts from row0
+  // ---- a block of keys as bf16: K fragments of keys ka, ka + 4, V rows of keys 8j .. 8j + 7
+  auto compute = [&](const u32x4 (&kr)[2][NKS], const vrow_t (&vr)[8], const int (&lim)[NRB], bool masked)
+      __attribute__((always_inline)) {
+    bf16x8 pf[NRB];
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+      f32x4 s[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks)
+          s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][ks]), qf[rb][ks], s[h], 0, 0, 0);
+      }
+      pf[rb] = softmax(s, rb, lim[rb], masked);
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      u32x4 w;           // value e of this lane's 8 keys
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        w[p] = __builtin_amdgcn_perm(vr[2 * p + 1][e / 2], vr[2 * p][e / 2], (e & 1) ? 0x07060302u : 0x05040100u);
+      const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) o[rb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb], o[rb][e], 0, 0, 0);
+    }
+  };
+
+  // ---- rows row0 .. row0 + 31 of a bf16 tensor with `rows` (rows past it read as zero); lim counts from row0
+  bool odd = false;                                // a value of the tail that is not finite
   auto bf16_block = [&](const uint16_t* bk, const uint16_t* bv, int rows, int row0, const int (&lim)[NRB],
-                        bool masked) __attribute__((always_inline)) {
+                        bool masked, bool tail) __attribute__((always_inline)) {
     const int left = min(rows - row0, BK) * rbytes;
     const rsrc_t rk = make_rsrc((const char*)bk + (int64_t)row0 * rbytes, left);
     const rsrc_t rv = make_rsrc((const char*)bv + (int64_t)row0 * rbytes, left);
@@ -163,89 +195,32 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
       if constexpr (VE == 8) vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, v_off + i * rbytes, 0, 0);
       else vr[i] = __builtin_amdgcn_raw_buffer_load_b64(rv, v_off + i * rbytes, 0, 0);
     }
-    bf16x8 pf[NRB];
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-      f32x4 s[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < NKS; ++ks)
-          s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][ks]), qf[rb][ks], s[h], 0, 0, 0);
-      }
-      pf[rb] = softmax(s, rb, lim[rb], masked);
-    }
-    if (masked) {
-      // values that are not finite: out of V, and added for the rows that see them
-      uint32_t odd = 0;                            // bit i: this lane's key 8j + i
+    if (masked && tail) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int d = 0; d < VE / 2; ++d) {
-          const uint32_t x = vr[i][d];
+          uint32_t x = vr[i][d];
           const bool lo = (x & 0x7F80u) == 0x7F80u, hi = (x & 0x7F800000u) == 0x7F800000u;
-          odd |= (lo || hi) ? 1u << i : 0u;
+          odd |= lo | hi;
+          vr[i][d] = x & (lo ? 0xFFFF0000u : ~0u) & (hi ? 0xFFFFu : ~0u);
         }
-      if (__builtin_amdgcn_ballot_w64(odd != 0)) {
-        uint32_t keys = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint64_t who = __builtin_amdgcn_ballot_w64((odd >> i) & 1);
-#pragma unroll
-          for (int jj = 0; jj < 4; ++jj) keys |= (who >> (16 * jj) & 0xFFFF) ? 1u << (8 * jj + i) : 0u;
-#pragma unroll
-          for (int d = 0; d < VE / 2; ++d) {
-            uint32_t x = vr[i][d];
-            if ((x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
-            if ((x & 0x7F800000u) == 0x7F800000u) x &= 0xFFFFu;
-            vr[i][d] = x;
-          }
-        }
-        for (; keys; keys &= keys - 1) {           // wave-uniform
-          const int key = __builtin_ctz(keys);
-          u32x4 x[VE / 2];                         // this lane's dims of O^T, VE * 4j .. + 4 * VE - 1, of the key
-#pragma unroll
-          for (int q = 0; q < VE / 2; ++q)
-            x[q] = __builtin_amdgcn_raw_buffer_load_b128(rv, (uint32_t)(key * rbytes + kv * D * 2 + VE * 8 * j + 16 * q), 0, 0);
-#pragma unroll
-          for (int rb = 0; rb < NRB; ++rb) {
-            float p = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p = (key & 7) == i ? (float)pf[rb][i] : p;
-            p = __shfl(p, 16 * (key >> 3) + n, 64);
-#pragma unroll
-            for (int d = 0; d < 4 * VE; ++d) {
-              const uint32_t w = x[d / 8][d % 8 / 2], bits = (d & 1) ? w & 0xFFFF0000u : w << 16;
-              const bool add = key <= lim[rb] && (bits & 0x7F800000u) == 0x7F800000u;
-              o[rb][d % VE][d / VE] += add ? p * __uint_as_float(bits) : 0.f;
-            }
-          }
-        }
-      }
     }
-#pragma unroll
-    for (int e = 0; e < VE; ++e) {
-      u32x4 w;           // value e of this lane's 8 keys
-#pragma unroll
-      for (int p = 0; p < 4; ++p)
-        w[p] = __builtin_amdgcn_perm(vr[2 * p + 1][e / 2], vr[2 * p][e / 2], (e & 1) ? 0x07060302u : 0x05040100u);
-      const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
-#pragma unroll
-      for (int rb = 0; rb < NRB; ++rb) o[rb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb], o[rb][e], 0, 0, 0);
-    }
+    compute(kr, vr, lim, masked);
   };
 
-  // ---- a block of the store
-  struct Q4Block {
+  // ---- a block of the store: what its loads bring
+  struct Codes {
     krow_t k[2];                  // this lane's dims of keys ka, ka + 4
     uint32_t v[8];                // its dims of keys 8j .. 8j + 7
     uint32_t ks[2], vs[2];        // scale bytes: K of the two keys; V of keys 8j + n%4, 8j + 4 + n%4
   };
-  auto load_q4 = [&](int i0, Q4Block& x) __attribute__((always_inline)) {      // gathered keys i0 .. i0 + 31, i0 < G
+  const uint32_t kc = (uint32_t)(kv * (D / 2) + j * (DPL / 2)), vc = (uint32_t)(kv * (D / 2) + n * (VE / 2));
+  const uint32_t ksc = (uint32_t)(kv * (D / kQ4Group) + kg), vsc = (uint32_t)(kv * (D / kQ4Group) + vg);
+  const uint32_t k_at = (uint32_t)(ka * cbytes) + kc, v_at = (uint32_t)(8 * j * cbytes) + vc;
+  const uint32_t ks_at = (uint32_t)(ka * sbytes) + ksc, vs_at = (uint32_t)((8 * j + (n & 3)) * sbytes) + vsc;
+  auto load_codes = [&](int i0, Codes& x) __attribute__((always_inline)) {      // gathered keys i0 .. i0 + 31, i0 < G
     int slot0;
-    const uint32_t kc = (uint32_t)(kv * (D / 2) + j * (DPL / 2)), vc = (uint32_t)(kv * (D / 2) + n * (VE / 2));
-    const uint32_t ksc = (uint32_t)(kv * (D / kQ4Group) + kg), vsc = (uint32_t)(kv * (D / kQ4Group) + vg);
     if (seg.straight(i0, slot0) >= BK) {
       // consecutive slots: base + fixed per-lane offsets
       const int64_t slot = slot0;
@@ -253,17 +228,15 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
       const rsrc_t rks = make_rsrc(a.ks + slot * sbytes, BK * sbytes), rvs = make_rsrc(a.vs + slot * sbytes, BK * sbytes);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t off = (uint32_t)((ka + 4 * h) * cbytes) + kc;
-        if constexpr (D == 128) x.k[h] = __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, 0);
-        else x.k[h] = __builtin_amdgcn_raw_buffer_load_b64(rk, off, 0, 0);
-        x.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(rks, (uint32_t)((ka + 4 * h) * sbytes) + ksc, 0, 0);
-        x.vs[h] = __builtin_amdgcn_raw_buffer_load_b8(rvs, (uint32_t)((8 * j + 4 * h + (n & 3)) * sbytes) + vsc, 0, 0);
+        if constexpr (D == 128) x.k[h] = __builtin_amdgcn_raw_buffer_load_b128(rk, k_at, h * 4 * cbytes, 0);
+        else x.k[h] = __builtin_amdgcn_raw_buffer_load_b64(rk, k_at, h * 4 * cbytes, 0);
+        x.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(rks, ks_at, h * 4 * sbytes, 0);
+        x.vs[h] = __builtin_amdgcn_raw_buffer_load_b8(rvs, vs_at, h * 4 * sbytes, 0);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t off = (uint32_t)((8 * j + i) * cbytes) + vc;
-        if constexpr (D == 128) x.v[i] = __builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0);
-        else x.v[i] = __builtin_amdgcn_raw_buffer_load_b16(rv, off, 0, 0);
+        if constexpr (D == 128) x.v[i] = __builtin_amdgcn_raw_buffer_load_b32(rv, v_at, i * cbytes, 0);
+        else x.v[i] = __builtin_amdgcn_raw_buffer_load_b16(rv, v_at, i * cbytes, 0);
       }
       return;
     }
@@ -290,69 +263,55 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
       x.v[i8] = ok ? w : 0;
     }
   };
-  auto q4_block = [&](int i0, const Q4Block& x) __attribute__((always_inline)) {
-    bf16x8 kf[2][NKS];
+  auto q4_block = [&](int i0, const Codes& x) __attribute__((always_inline)) {
+    u32x4 kr[2][NKS];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int ks = 0; ks < NKS; ++ks) kf[h][ks] = __builtin_bit_cast(bf16x8, q4_eight(x.k[h][ks], q4_scale(x.ks[h])));
-    bf16x8 pf[NRB];
-    const int lim = G - 1 - i0;
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-      f32x4 s[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][ks], qf[rb][ks], s[h], 0, 0, 0);
-      }
-      pf[rb] = softmax(s, rb, lim, lim < BK - 1);
-    }
-    float vs[8];
+      for (int ks = 0; ks < NKS; ++ks) kr[h][ks] = q4_eight(x.k[h][ks], q4_scale(x.ks[h]));
+    // each scale byte of the quad's 8 keys to its four lanes
     const uint32_t b0 = x.vs[0] << 23, b1 = x.vs[1] << 23;
-    vs[0] = __uint_as_float(dpp<0x00>(b0)); vs[1] = __uint_as_float(dpp<0x55>(b0));
-    vs[2] = __uint_as_float(dpp<0xAA>(b0)); vs[3] = __uint_as_float(dpp<0xFF>(b0));
-    vs[4] = __uint_as_float(dpp<0x00>(b1)); vs[5] = __uint_as_float(dpp<0x55>(b1));
-    vs[6] = __uint_as_float(dpp<0xAA>(b1)); vs[7] = __uint_as_float(dpp<0xFF>(b1));
-    auto two_dims = [&](auto sel) __attribute__((always_inline)) {
-      constexpr int E = 2 * decltype(sel)::value;
-      uint32_t p[8];
+    const uint32_t vs[8] = {dpp<0x00>(b0), dpp<0x55>(b0), dpp<0xAA>(b0), dpp<0xFF>(b0),
+                            dpp<0x00>(b1), dpp<0x55>(b1), dpp<0xAA>(b1), dpp<0xFF>(b1)};
+    vrow_t vr[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = q4_pair<E / 2>(x.v[i], vs[i]);
-#pragma unroll
-      for (int odd = 0; odd < 2; ++odd) {
-        u32x4 w;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) w[q] = __builtin_amdgcn_perm(p[2 * q + 1], p[2 * q], odd ? 0x07060302u : 0x05040100u);
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-          o[rb][E + odd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb], o[rb][E + odd], 0, 0, 0);
-      }
-    };
-    two_dims(std::integral_constant<int, 0>{});
-    two_dims(std::integral_constant<int, 1>{});
-    if constexpr (VE == 8) {
-      two_dims(std::integral_constant<int, 2>{});
-      two_dims(std::integral_constant<int, 3>{});
+    for (int i = 0; i < 8; ++i) {
+      const float f = __uint_as_float(vs[i]);
+      if constexpr (VE == 8) vr[i] = q4_eight(x.v[i], f);
+      else vr[i] = vrow_t{q4_pair<0>(x.v[i], f), q4_pair<1>(x.v[i], f)};
     }
+    const int last = G - 1 - i0;
+    int lim[NRB];
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) lim[rb] = last;
+    compute(kr, vr, lim, last < BK - 1);
   };
 
-  // ---- the wave's blocks
-  for (int b = b_lo + wave; b < b_hi; b += NW) {
-    int lim[NRB];
-    if (b >= nb_s && b < nb_s + nb_g) {
-      Q4Block x;
-      load_q4((b - nb_s) * BK, x);
-      q4_block((b - nb_s) * BK, x);
-    } else {
-      const bool sink = b < nb_s;
-      const int row0 = (sink ? b : b - nb_s - nb_g) * BK;
+  // ---- the wave's blocks: every NW-th of the part's.  The codes of its first store block are on their way while the
+  // sink's and the tail's blocks are computed, those of the next while one is.
+  const int end_g = nb_s + nb_g;
+  auto step_to = [&](int b, int to) __attribute__((always_inline)) { return b + (max(to - b, 0) + NW - 1) / NW * NW; };
+  const int first_g = step_to(b_lo + wave, nb_s), last_g = min(b_hi, end_g);
+  Codes next;
+  for (int b = first_g - NW; b < max(last_g, first_g); b += NW) {      // (one place for the loads: the code is fetched anew by each launch)
+    const Codes now = next;
+    if (b + NW < last_g) load_codes((b + NW - nb_s) * BK, next);
+    if (b >= first_g) {
+      q4_block((b - nb_s) * BK, now);
+      continue;
+    }
+    for (int i = b_lo + wave; i < b_hi; i += NW) {
+      if (i >= nb_s && i < end_g) {
+        i = step_to(i, end_g);
+        if (i >= b_hi) break;
+      }
+      const bool sink = i < nb_s;
+      const int row0 = (sink ? i : i - end_g) * BK;
+      int lim[NRB];
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb) lim[rb] = (sink ? a.S - 1 : tail0 + tok[rb]) - row0;
       bf16_block(sink ? a.sink_k : a.tail_k, sink ? a.sink_v : a.tail_v, sink ? a.S : a.T, row0, lim,
-                 row0 + BK - 1 > (sink ? a.S - 1 : tail_first));
+                 row0 + BK - 1 > (sink ? a.S - 1 : tail_first), !sink);
     }
   }
 
@@ -374,6 +333,8 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
         *(f32x4*)(op + i * VE + e) = f32x4{o[rb][e][i], o[rb][e + 1][i], o[rb][e + 2][i], o[rb][e + 3][i]};
   }
   __syncthreads();
+  if (odd) odd_s = 1;
+  __syncthreads();
   constexpr int NQ = D / 4;
   const int rows = min(RT, NR - rt * RT);
   for (int it = tid; it < rows * NQ; it += NW * 64) {
@@ -393,6 +354,17 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
     acc *= l > 0.f ? 1.f / l : l == l ? 0.f : l;                       // an empty row is 0, a NaN stays one
     const float lse2 = l > 0.f ? m_use + __log2f(l) : l == l ? -INFINITY : l;
     const int pr = rt * RT + r, t = pr / g, h = kv * g + pr % g;
+    if (__builtin_expect(odd_s != 0, 0)) {       // values of the part's tail keys that are not finite, for the rows that see them
+      const int k1 = min(max(b_hi - end_g, 0) * BK - 1, tail0 + t);
+      for (int k = max(b_lo - end_g, 0) * BK; k <= k1; ++k) {
+        const u32x2 w = *(const u32x2*)(a.tail_v + ((int64_t)k * a.Hkv + kv) * D + dq * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t bits = (i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16;
+          acc[i] += (bits & 0x7F800000u) == 0x7F800000u ? __uint_as_float(bits) : 0.f;
+        }
+      }
+    }
     if (a.parts > 1) {
       const int64_t prow = ((int64_t)part * a.Hq + h) * a.Lq + t;      // the merge kernel's layout
       *(f32x4*)(a.ws_o + prow * D + dq * 4) = acc;

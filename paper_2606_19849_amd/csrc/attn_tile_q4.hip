@@ -58,11 +58,12 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   const int g = a.Hq / a.Hkv;
   const int NR = g * a.Lq;
 
-  // ---- work item: the row tiles of one key range of a KV head side by side (they share its codes in an XCD's L2)
+  // ---- work item: the row tiles of one key range side by side, then its KV heads: they share its codes, and the
+  // heads the cache lines (a head's codes of a token are 64 or 32 bytes), in an XCD's L2
   const int L = xcd_remap(blockIdx.x, gridDim.x);
   const int rt = a.n_rt - 1 - L % a.n_rt;    // longest first
-  const int part = (L / a.n_rt) % a.parts;
-  const int kv = L / (a.n_rt * a.parts);
+  const int kv = (L / a.n_rt) % a.Hkv;
+  const int part = L / (a.n_rt * a.Hkv);
 
   if (tid == 0) odd_s = 0;
   int incl, shift, win;

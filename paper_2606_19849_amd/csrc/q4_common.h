@@ -53,12 +53,14 @@ struct Segments {
     slot = hi > lo ? (int)lo : 0;
     return hi > lo ? (int)(hi - lo) : 0;
   }
+  // inclusive sum over the lanes up to this one: inside the rows of 16, then across them
   static __device__ __forceinline__ int scan(int x) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(x, o, 64);
-      x += (int)(threadIdx.x & 63) >= o ? y : 0;
-    }
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);       // row_shr 1, 2, 4, 8: 0 from outside of the row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);      // lane 15 of a row to the next one: rows 1, 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);      // lane 31 to rows 2, 3
     return x;
   }
   // The state is the kernel's locals, the table in LDS, the lanes' window of it and the window's first segment:

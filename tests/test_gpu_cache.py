@@ -376,6 +376,21 @@ def test_nan_of_the_store_reaches_every_row():
         assert np.isnan(o[:, 4:]).all() and np.isnan(l[4:]).all()
 
 
+@pytest.mark.parametrize("q_len,tail", [(2, 4), (60, 61)])
+@pytest.mark.parametrize("S", [5, 64])
+def test_nan_of_the_sink_or_the_old_tail_reaches_every_row(q_len, tail, S):
+    def tweak(c):
+        c.sink[1][3, 0, 7] = float("nan")                  # KV head 0
+        c.tail[1][0, 1, 9] = float("inf")                  # KV head 1: a token before every row
+    c = Case(19, 8, 2, 64, q_len, tail, S, 100, [0], [77], tweak=tweak)
+    clean = Case(19, 8, 2, 64, q_len, tail, S, 100, [0], [77])
+    for splits in (1, 3):
+        (o, l), (a, la) = c.run(splits), clean.run(splits)
+        assert np.isnan(o[:, :4, 7]).all() and np.all(o[:, 4:, 9] == np.inf) and np.array_equal(l, la)
+        o[:, :4, 7], o[:, 4:, 9], a[:, :4, 7], a[:, 4:, 9] = 0, 0, 0, 0
+        assert np.array_equal(o, a)
+
+
 def test_store_beyond_32_bit_offsets():
     """Slots past 4 GiB of codes: append, load and attention there, against the same tokens at the front."""
     Hkv, D, R, C = 64, 128, (1 << 32) // (64 * 64) + 500, 90

@@ -37,6 +37,15 @@ __device__ __forceinline__ uint32_t dpp(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
 }
 
+// The kernel's arguments, read again from memory where they are used: what only the start, the end or the bf16
+// blocks need takes no scalar registers (and, spilled, no vector ones) in the store's loop.
+typedef const __attribute__((address_space(4))) RowsQ4Args* late_args;
+__device__ __forceinline__ late_args late() {
+  late_args p = (late_args)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
 // A row tile's state and block bodies; D dims a head, NRB blocks of 16 rows.
 template <int D, int NRB, int NW>
 __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) {
@@ -65,9 +74,8 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
   // ---- work item: the row tiles of one key range side by side, then its KV heads: they share its codes, and the
   // heads the cache lines (a head's codes of a token are 64 or 32 bytes), in an XCD's L2
   const int L = xcd_remap(blockIdx.x, gridDim.x);
-  const int rt = L % a.n_rt;
-  const int kv = (L / a.n_rt) % a.Hkv;
-  const int part = L / (a.n_rt * a.Hkv);
+  const int group = a.by_rt(L), rt = L - group * a.n_rt, part = a.by_kv(group);
+  const int kv = group - part * a.Hkv;
 
   if (tid == 0) odd_s = 0;
   int incl, shift, win;
@@ -80,19 +88,19 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb) {
     const int r = min(rt * RT + rb * 16 + n, NR - 1);
-    tok[rb] = r / g;
-    const uint16_t* qp = a.q + ((int64_t)tok[rb] * a.Hq + kv * g + r % g) * D + j * DPL;
+    tok[rb] = a.by_g(r);
+    const uint16_t* qp = a.q + ((int64_t)tok[rb] * a.Hq + kv * g + r - tok[rb] * g) * D + j * DPL;
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) qf[rb][ks] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + ks * 8));
   }
 
   // ---- blocks: sink, store, tail
   const int tail0 = a.T - a.Lq;                                // tail key `tail0 + t` is row t's last
-  const int tail_first = tail0 + min(rt * RT, NR - 1) / g, tail_last = tail0 + (min((rt + 1) * RT, NR) - 1) / g;
+  const int tail_first = tail0 + a.by_g(min(rt * RT, NR - 1)), tail_last = tail0 + a.by_g(min((rt + 1) * RT, NR) - 1);
   const int nb_s = (a.S + BK - 1) / BK, nb_g = (G + BK - 1) / BK, nb_t = tail_last / BK + 1;
   const int n_blocks = nb_s + nb_g + nb_t;
-  const int b_lo = (int)((int64_t)n_blocks * part / a.parts);
-  const int b_hi = (int)((int64_t)n_blocks * (part + 1) / a.parts);
+  const int per_part = a.by_parts(n_blocks + a.parts - 1);
+  const int b_lo = min(per_part * part, n_blocks), b_hi = min(b_lo + per_part, n_blocks);
 
   const int rbytes = a.Hkv * D * 2, cbytes = a.Hkv * (D / 2), sbytes = a.Hkv * (D / kQ4Group);
   const int ka = 8 * (n >> 2) + (n & 3);                       // this lane's key of the first product; second: + 4
@@ -113,7 +121,7 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
 
   // Softmax of the block's logits (key 8j + v in s[v / 4][v % 4]); key index past lim[rb] is masked.
   auto softmax = [&](f32x4 (&s)[2], int rb, int lim, bool masked) __attribute__((always_inline)) {
-    if (masked) {
+    if (__builtin_expect(masked, 0)) {
 #pragma unroll
       for (int v = 0; v < 8; ++v) s[v / 4][v % 4] = 8 * j + v > lim ? -INFINITY : s[v / 4][v % 4];
     }
@@ -147,21 +155,22 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
   };
 
   // ---- a block of keys as bf16: K fragments of keys ka, ka + 4, V rows of keys 8j .. 8j + 7
-  auto compute = [&](const u32x4 (&kr)[2][NKS], const vrow_t (&vr)[8], const int (&lim)[NRB], bool masked)
+  auto probabilities = [&](const u32x4 (&kr)[2][NKS], bf16x8 (&pf)[NRB], const int (&lim)[NRB], bool masked)
       __attribute__((always_inline)) {
-    bf16x8 pf[NRB];
+    f32x4 s[NRB][2];
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-      f32x4 s[2];
+    for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+        s[rb][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks)
-          s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][ks]), qf[rb][ks], s[h], 0, 0, 0);
+          s[rb][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][ks]), qf[rb][ks], s[rb][h], 0, 0, 0);
       }
-      pf[rb] = softmax(s, rb, lim[rb], masked);
-    }
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) pf[rb] = softmax(s[rb], rb, lim[rb], masked);
+  };
+  auto values = [&](const vrow_t (&vr)[8], const bf16x8 (&pf)[NRB]) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
       u32x4 w;           // value e of this lane's 8 keys
@@ -181,32 +190,39 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
     const int left = min(rows - row0, BK) * rbytes;
     const rsrc_t rk = make_rsrc((const char*)bk + (int64_t)row0 * rbytes, left);
     const rsrc_t rv = make_rsrc((const char*)bv + (int64_t)row0 * rbytes, left);
-    u32x4 kr[2][NKS];
-    vrow_t vr[8];
     const uint32_t k_off = (uint32_t)(ka * rbytes + kv * D * 2 + j * DPL * 2);
     const uint32_t v_off = (uint32_t)(8 * j * rbytes + kv * D * 2 + n * VE * 2);
+    bf16x8 pf[NRB];
+    {
+      u32x4 kr[2][NKS];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int ks = 0; ks < NKS; ++ks)
-        kr[h][ks] = __builtin_amdgcn_raw_buffer_load_b128(rk, k_off + h * 4 * rbytes + ks * 16, 0, 0);
+        for (int ks = 0; ks < NKS; ++ks)
+          kr[h][ks] = __builtin_amdgcn_raw_buffer_load_b128(rk, k_off + h * 4 * rbytes + ks * 16, 0, 0);
+      probabilities(kr, pf, lim, masked);
+    }
+    vrow_t vr[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if constexpr (VE == 8) vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, v_off + i * rbytes, 0, 0);
       else vr[i] = __builtin_amdgcn_raw_buffer_load_b64(rv, v_off + i * rbytes, 0, 0);
     }
     if (masked && tail) {
+      u16x2 most{0, 0};
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int d = 0; d < VE / 2; ++d) {
-          uint32_t x = vr[i][d];
-          const bool lo = (x & 0x7F80u) == 0x7F80u, hi = (x & 0x7F800000u) == 0x7F800000u;
-          odd |= lo | hi;
-          vr[i][d] = x & (lo ? 0xFFFF0000u : ~0u) & (hi ? 0xFFFFu : ~0u);
-        }
+        for (int d = 0; d < VE / 2; ++d) largest_exponents(most, vr[i][d]);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(not_finite(most)) != 0, 0)) {
+        odd = true;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int d = 0; d < VE / 2; ++d) vr[i][d] = finite_or_zero(vr[i][d]);
+      }
     }
-    compute(kr, vr, lim, masked);
+    values(vr, pf);
   };
 
   // ---- a block of the store: what its loads bring
@@ -264,11 +280,19 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
     }
   };
   auto q4_block = [&](int i0, const Codes& x) __attribute__((always_inline)) {
-    u32x4 kr[2][NKS];
+    const int last = G - 1 - i0;
+    int lim[NRB];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int rb = 0; rb < NRB; ++rb) lim[rb] = last;
+    bf16x8 pf[NRB];
+    {
+      u32x4 kr[2][NKS];
 #pragma unroll
-      for (int ks = 0; ks < NKS; ++ks) kr[h][ks] = q4_eight(x.k[h][ks], q4_scale(x.ks[h]));
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) kr[h][ks] = q4_eight(x.k[h][ks], q4_scale(x.ks[h]));
+      probabilities(kr, pf, lim, last < BK - 1);
+    }
     // each scale byte of the quad's 8 keys to its four lanes
     const uint32_t b0 = x.vs[0] << 23, b1 = x.vs[1] << 23;
     const uint32_t vs[8] = {dpp<0x00>(b0), dpp<0x55>(b0), dpp<0xAA>(b0), dpp<0xFF>(b0),
@@ -280,11 +304,7 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
       if constexpr (VE == 8) vr[i] = q4_eight(x.v[i], f);
       else vr[i] = vrow_t{q4_pair<0>(x.v[i], f), q4_pair<1>(x.v[i], f)};
     }
-    const int last = G - 1 - i0;
-    int lim[NRB];
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) lim[rb] = last;
-    compute(kr, vr, lim, last < BK - 1);
+    values(vr, pf);
   };
 
   // ---- the wave's blocks: every NW-th of the part's.  The codes of its first store block are on their way while the
@@ -292,27 +312,24 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
   const int end_g = nb_s + nb_g;
   auto step_to = [&](int b, int to) __attribute__((always_inline)) { return b + (max(to - b, 0) + NW - 1) / NW * NW; };
   const int first_g = step_to(b_lo + wave, nb_s), last_g = min(b_hi, end_g);
-  Codes next;
-  for (int b = first_g - NW; b < max(last_g, first_g); b += NW) {      // (one place for the loads: the code is fetched anew by each launch)
-    const Codes now = next;
-    if (b + NW < last_g) load_codes((b + NW - nb_s) * BK, next);
-    if (b >= first_g) {
-      q4_block((b - nb_s) * BK, now);
-      continue;
+  for (int b = b_lo + wave; b < b_hi; b += NW) {
+    if (b >= nb_s && b < end_g) {
+      b = step_to(b, end_g);
+      if (b >= b_hi) break;
     }
-    for (int i = b_lo + wave; i < b_hi; i += NW) {
-      if (i >= nb_s && i < end_g) {
-        i = step_to(i, end_g);
-        if (i >= b_hi) break;
-      }
-      const bool sink = i < nb_s;
-      const int row0 = (sink ? i : i - end_g) * BK;
-      int lim[NRB];
+    const late_args l = late();
+    const bool sink = b < nb_s;
+    const int rows = sink ? l->S : l->T, row0 = (sink ? b : b - end_g) * BK;
+    int lim[NRB];
 #pragma unroll
-      for (int rb = 0; rb < NRB; ++rb) lim[rb] = (sink ? a.S - 1 : tail0 + tok[rb]) - row0;
-      bf16_block(sink ? a.sink_k : a.tail_k, sink ? a.sink_v : a.tail_v, sink ? a.S : a.T, row0, lim,
-                 row0 + BK - 1 > (sink ? a.S - 1 : tail_first), !sink);
-    }
+    for (int rb = 0; rb < NRB; ++rb) lim[rb] = (sink ? rows - 1 : tail0 + tok[rb]) - row0;
+    bf16_block(sink ? l->sink_k : l->tail_k, sink ? l->sink_v : l->tail_v, rows, row0, lim,
+               row0 + BK - 1 > (sink ? rows - 1 : tail_first), !sink);
+  }
+  for (int b = first_g; b < last_g; b += NW) {
+    Codes x;
+    load_codes((b - nb_s) * BK, x);
+    q4_block((b - nb_s) * BK, x);
   }
 
   // ---- merge of the waves: O^T lane (n, j) holds row n, dims VE*(4j+i) + e
@@ -337,27 +354,28 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
   __syncthreads();
   constexpr int NQ = D / 4;
   const int rows = min(RT, NR - rt * RT);
+  const late_args l = late();
   for (int it = tid; it < rows * NQ; it += NW * 64) {
     const int r = it / NQ, dq = it % NQ;
     float m = -INFINITY;
 #pragma unroll
     for (int w = 0; w < NW; ++w) m = fmaxf(m, m_s[w][r]);
     const float m_use = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
+    float sum = 0.f;
     f32x4 acc{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       const float f = __builtin_amdgcn_exp2f(m_s[w][r] - m_use);      // 0 for a wave that saw no key of the row
-      l += f * l_s[w][r];
+      sum += f * l_s[w][r];
       acc += f * *(const f32x4*)&o_s[w][r][dq * 4];
     }
-    acc *= l > 0.f ? 1.f / l : l == l ? 0.f : l;                       // an empty row is 0, a NaN stays one
-    const float lse2 = l > 0.f ? m_use + __log2f(l) : l == l ? -INFINITY : l;
-    const int pr = rt * RT + r, t = pr / g, h = kv * g + pr % g;
+    acc *= sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;                       // an empty row is 0, a NaN stays one
+    const float lse2 = sum > 0.f ? m_use + __log2f(sum) : sum == sum ? -INFINITY : sum;
+    const int pr = rt * RT + r, t = a.by_g(pr), h = kv * g + pr - t * g;
     if (__builtin_expect(odd_s != 0, 0)) {       // values of the part's tail keys that are not finite, for the rows that see them
       const int k1 = min(max(b_hi - end_g, 0) * BK - 1, tail0 + t);
       for (int k = max(b_lo - end_g, 0) * BK; k <= k1; ++k) {
-        const u32x2 w = *(const u32x2*)(a.tail_v + ((int64_t)k * a.Hkv + kv) * D + dq * 4);
+        const u32x2 w = *(const u32x2*)(l->tail_v + ((int64_t)k * l->Hkv + kv) * D + dq * 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t bits = (i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16;
@@ -365,23 +383,23 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
         }
       }
     }
-    if (a.parts > 1) {
-      const int64_t prow = ((int64_t)part * a.Hq + h) * a.Lq + t;      // the merge kernel's layout
-      *(f32x4*)(a.ws_o + prow * D + dq * 4) = acc;
-      if (dq == 0) a.ws_lse[prow] = lse2;
+    if (l->parts > 1) {
+      const int64_t prow = ((int64_t)part * l->Hq + h) * l->Lq + t;      // the merge kernel's layout
+      *(f32x4*)(l->ws_o + prow * D + dq * 4) = acc;
+      if (dq == 0) l->ws_lse[prow] = lse2;
       continue;
     }
-    const int64_t oo = ((int64_t)t * a.Hq + h) * D + dq * 4;
-    if (a.out_f32) *(f32x4*)((float*)a.out + oo) = acc;
-    else *(bf16x4*)((__bf16*)a.out + oo) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
-    if (dq == 0 && a.lse) a.lse[(int64_t)h * a.Lq + t] = lse2 * kLn2;
+    const int64_t oo = ((int64_t)t * l->Hq + h) * D + dq * 4;
+    if (l->out_f32) *(f32x4*)((float*)l->out + oo) = acc;
+    else *(bf16x4*)((__bf16*)l->out + oo) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
+    if (dq == 0 && l->lse) l->lse[(int64_t)h * l->Lq + t] = lse2 * kLn2;
   }
 }
 
 template <int D>
 hipError_t launch(const RowsQ4Args& a, hipStream_t stream) {
   const dim3 grid(a.n_rt * a.parts * a.Hkv);
-  if (a.row_blocks == 1) hipLaunchKernelGGL((attn_rows_q4_kernel<D, 1, 8>), grid, dim3(512), 0, stream, a);
+  if (a.row_blocks == 1) hipLaunchKernelGGL((attn_rows_q4_kernel<D, 1, 16>), grid, dim3(1024), 0, stream, a);
   else if (a.row_blocks == 2) hipLaunchKernelGGL((attn_rows_q4_kernel<D, 2, 8>), grid, dim3(512), 0, stream, a);
   else return hipErrorInvalidValue;
   return hipGetLastError();

@@ -61,9 +61,9 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   // ---- work item: the row tiles of one key range side by side, then its KV heads: they share its codes, and the
   // heads the cache lines (a head's codes of a token are 64 or 32 bytes), in an XCD's L2
   const int L = xcd_remap(blockIdx.x, gridDim.x);
-  const int rt = a.n_rt - 1 - L % a.n_rt;    // longest first
-  const int kv = (L / a.n_rt) % a.Hkv;
-  const int part = L / (a.n_rt * a.Hkv);
+  const int group = a.by_rt(L), part = a.by_kv(group);
+  const int rt = a.n_rt - 1 - (L - group * a.n_rt);      // longest first
+  const int kv = group - part * a.Hkv;
 
   if (tid == 0) odd_s = 0;
   int incl, shift, win;
@@ -74,17 +74,17 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   const int wrow0 = rt * BM + wave * 32;
   const bool wave_active = wrow0 < NR;
   const int my_row = min(wrow0 + l32, NR - 1);
-  const int tok = my_row / g, head = kv * g + my_row % g;
+  const int tok = a.by_g(my_row), head = kv * g + my_row - tok * g;
   bf16x8 qf[RB][NKS];
   WaveTile<D>::load_q(qf[0], a.q + ((int64_t)tok * a.Hq + head) * D + hh * 8);
 
   // ---- tiles: sink, store, tail up to the row tile's last row
   const int tail0 = a.T - a.Lq;              // tail key `tail0 + t` is row t's last
-  const int first_lim = tail0 + min(wrow0, NR - 1) / g, last_lim = tail0 + min(wrow0 + 31, NR - 1) / g;
+  const int first_lim = tail0 + a.by_g(min(wrow0, NR - 1)), last_lim = tail0 + a.by_g(min(wrow0 + 31, NR - 1));
   const int nb_s = (a.S + BN - 1) / BN, nb_sg = nb_s + (G + BN - 1) / BN;
-  const int n_tiles = nb_sg + (tail0 + (min((rt + 1) * BM, NR) - 1) / g) / BN + 1;
-  const int t_lo = (int)((int64_t)n_tiles * part / a.parts);
-  const int t_hi = (int)((int64_t)n_tiles * (part + 1) / a.parts);
+  const int n_tiles = nb_sg + (tail0 + a.by_g(min((rt + 1) * BM, NR) - 1)) / BN + 1;
+  const int per_part = a.by_parts(n_tiles + a.parts - 1);
+  const int t_lo = min(per_part * part, n_tiles), t_hi = min(t_lo + per_part, n_tiles);
   const int t_end = wave_active ? min(t_hi, nb_sg + last_lim / BN + 1) : t_lo;      // the wave's last tile
   // the lane's last visible key in tile t, and whether some lane of the wave does not see all of the tile
   auto lim_of = [&](int t) __attribute__((always_inline)) {
@@ -223,12 +223,13 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
 #pragma unroll
     for (int n = 0; n < NLD; ++n) {
       u32x4 x = *(lds_u4)(uintptr_t)(at + n * 1024);
+      u16x2 most{0, 0};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool lo = (x[i] & 0x7F80u) == 0x7F80u, hi = (x[i] & 0x7F800000u) == 0x7F800000u;
-        odd |= lo | hi;
-        x[i] &= (lo ? 0xFFFF0000u : ~0u) & (hi ? 0xFFFFu : ~0u);
+        largest_exponents(most, x[i]);
+        x[i] = finite_or_zero(x[i]);
       }
+      odd |= not_finite(most);
       *(lds_u4)(uintptr_t)(at + n * 1024) = x;
     }
   };

@@ -292,6 +292,10 @@ int vico_gather_attn_q4(const void* q, int32_t q_len, const void* tail_k, const 
   a.Lq = sh.Lq; a.T = sh.T; a.S = sh.S; a.cap = sh.cap; a.n_segs = sh.n_segs;
   a.Hq = sh.Hq; a.Hkv = sh.Hkv; a.D = sh.D;
   a.parts = sh.parts; a.n_rt = sh.n_rt; a.row_blocks = sh.row_blocks;
+  a.by_g = FastDiv::by(a.Hq / a.Hkv);
+  a.by_rt = FastDiv::by(a.n_rt);
+  a.by_kv = FastDiv::by(a.Hkv);
+  a.by_parts = FastDiv::by(a.parts);
   a.out_f32 = out_dtype == VICO_DTYPE_F32;
   const double scale = softmax_scale > 0.f ? double(softmax_scale) : 1.0 / sqrt(double(head_dim));
   a.scale_log2 = (float)(scale * 1.4426950408889634);

@@ -148,6 +148,20 @@ struct LoadQ4Args {
   int cap, n_segs, out_rows, row_elems;
 };
 
+// Division of numbers below 2^31 by a number known on the host: a product and a shift where the hardware would take
+// some twenty instructions, one after the other.
+struct FastDiv {
+  uint32_t m, s;
+  static FastDiv by(int d) {
+    uint32_t l = 0;
+    while ((uint64_t(1) << l) < (uint64_t)d) ++l;
+    return FastDiv{(uint32_t)((((uint64_t(1) << l) - (uint64_t)d) << 32) / (uint64_t)d + 1), l};
+  }
+  __host__ __device__ int operator()(int n) const {
+    return (int)(((uint32_t)(((uint64_t)m * (uint32_t)n) >> 32) + (uint32_t)n) >> s);
+  }
+};
+
 // Keys as in GatherArgs, the store in 4 bits; row tiles and parts as in RowsArgs.
 struct RowsQ4Args {
   const uint16_t* q;
@@ -168,6 +182,7 @@ struct RowsQ4Args {
   int Lq, T, S, cap, n_segs;
   int Hq, Hkv, D;
   int parts, n_rt, row_blocks;
+  FastDiv by_g, by_rt, by_kv, by_parts;     // Hq / Hkv, n_rt, Hkv, parts
   int out_f32;
   float scale_log2;
 };

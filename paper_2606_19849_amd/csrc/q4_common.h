@@ -129,7 +129,7 @@ struct Segments {
     slot0 = i + __builtin_amdgcn_readlane(shift, s);
     return __builtin_amdgcn_readlane(incl, s) - i;
   }
-  // slot of key i0 + lane % n (n: 32 or 64); a key past the last, `total` - 1, has its slot and real = false
+  // slot of key i0 + lane % n (n: a power of two); a key past the last, `total` - 1, has its slot and real = false
   __device__ __forceinline__ int slot_of_lane(int i0, int n, int total, bool& real) const {
     const int i = i0 + (int)(threadIdx.x & (n - 1)), end = min(i0 + n, total);
     int s = find(i0), slot = 0, last = 0, begin = i0;

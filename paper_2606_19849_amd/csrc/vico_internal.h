@@ -123,6 +123,20 @@ struct RowsArgs {
   AppendArgs app;
 };
 
+// Division of numbers below 2^31 by a number known on the host: a product and a shift where the hardware would take
+// some twenty instructions, one after the other.
+struct FastDiv {
+  uint32_t m, s;
+  static FastDiv by(int d) {
+    uint32_t l = 0;
+    while ((uint64_t(1) << l) < (uint64_t)d) ++l;
+    return FastDiv{(uint32_t)((((uint64_t(1) << l) - (uint64_t)d) << 32) / (uint64_t)d + 1), l};
+  }
+  __host__ __device__ int operator()(int n) const {
+    return (int)(((uint32_t)(((uint64_t)m * (uint32_t)n) >> 32) + (uint32_t)n) >> s);
+  }
+};
+
 // ---- the 4-bit store (q4_common.h)
 struct AppendQ4Args {
   const uint16_t* kc;      // [C][row_elems]
@@ -146,20 +160,8 @@ struct LoadQ4Args {
   uint16_t* v;
   int32_t* out_count;      // may be null
   int cap, n_segs, out_rows, row_elems;
-};
-
-// Division of numbers below 2^31 by a number known on the host: a product and a shift where the hardware would take
-// some twenty instructions, one after the other.
-struct FastDiv {
-  uint32_t m, s;
-  static FastDiv by(int d) {
-    uint32_t l = 0;
-    while ((uint64_t(1) << l) < (uint64_t)d) ++l;
-    return FastDiv{(uint32_t)((((uint64_t(1) << l) - (uint64_t)d) << 32) / (uint64_t)d + 1), l};
-  }
-  __host__ __device__ int operator()(int n) const {
-    return (int)(((uint32_t)(((uint64_t)m * (uint32_t)n) >> 32) + (uint32_t)n) >> s);
-  }
+  int per_wave;             // rows of a wave, and the divisor row_elems / 8: set by the launch
+  FastDiv by_units;
 };
 
 // Keys as in GatherArgs, the store in 4 bits; row tiles and parts as in RowsArgs.

@@ -326,10 +326,19 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
     bf16_block(sink ? l->sink_k : l->tail_k, sink ? l->sink_v : l->tail_v, rows, row0, lim,
                row0 + BK - 1 > (sink ? rows - 1 : tail_first), !sink);
   }
-  for (int b = first_g; b < last_g; b += NW) {
-    Codes x;
-    load_codes((b - nb_s) * BK, x);
-    q4_block((b - nb_s) * BK, x);
+  if constexpr (NW >= 16) {
+    for (int b = first_g; b < last_g; b += NW) {
+      Codes x;
+      load_codes((b - nb_s) * BK, x);
+      q4_block((b - nb_s) * BK, x);
+    }
+  } else {                                 // (one place for the loads: the code is fetched anew by each launch)
+    Codes next;
+    for (int b = first_g - NW; b < last_g; b += NW) {
+      const Codes now = next;
+      if (b + NW < last_g) load_codes((b + NW - nb_s) * BK, next);
+      if (b >= first_g) q4_block((b - nb_s) * BK, now);
+    }
   }
 
   // ---- merge of the waves: O^T lane (n, j) holds row n, dims VE*(4j+i) + e

@@ -80,7 +80,7 @@ int check_gather_q4_shape(int32_t Lq, int32_t T, int32_t S, int32_t cap, int32_t
   const int64_t gathered = n_segs == 0 ? 0 : std::min<int64_t>(hint > 0 ? hint : cap, int64_t(n_segs) * cap);
   const int64_t keys = S + gathered + T;
   int64_t most;
-  if (rows >= 128) {
+  if (rows >= 256) {
     sh->tile = 1;
     sh->n_rt = (int)((rows + kBlockM - 1) / kBlockM);
     int64_t cost;

@@ -141,7 +141,7 @@ int vico_kv_load_q4(const void* store_k, const void* store_v, const void* scale_
  *   keys_hint      expected total segment length (0: not known); sets how the
  *                  work is split and which kernel runs
  *   workspace      at least the bytes that vico_gather_plan_q4 reports for the
- *                  same arguments (below 48 MB with num_splits = 0)
+ *                  same arguments (at most 48 MiB with num_splits = 0)
  * num_segments * store_slots + sink_len + tail_len <= 2^30; q, sink, tail and
  * out are below 2^31 bytes, the store may be longer.  The table is
  * clipped to the store on the device as for vico_gather_attn.

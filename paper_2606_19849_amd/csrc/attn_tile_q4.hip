@@ -122,7 +122,9 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   };
   // Codes.  Consecutive tiles in one segment are a run: their loads share the per-lane offsets, and the bases move
   // on.  A wave's chunks differ by RPL rows, and K's units by an exclusive or of the lowest bit.
-  uint32_t kc[NLD], vc[NLD], ks[NLD], vs[NLD];
+  struct Codes {
+    uint32_t kc[NLD], vc[NLD], ks[NLD], vs[NLD];
+  };
   uint32_t k_off[NLD], v_off, ks_off, vs_off;
   {
     int rk, uk, rv, uv;
@@ -137,12 +139,12 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   const uint8_t *run_k = nullptr, *run_v = nullptr, *run_ks = nullptr, *run_vs = nullptr;
   int run_left = 0;                          // tiles left in the run, all below t_hi
   constexpr int NLOAD = 4 * NLD;
-  auto load_run = [&](auto job) __attribute__((always_inline)) {
+  auto load_run = [&](auto job, Codes& x) __attribute__((always_inline)) {
     constexpr int n = decltype(job)::value / 4, what = decltype(job)::value % 4;
-    if constexpr (what == 0) kc[n] = __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(run_k, BN * cbytes), k_off[n], 0, 0);
-    if constexpr (what == 1) vc[n] = __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(run_v, BN * cbytes), v_off + n * RPL * cbytes, 0, 0);
-    if constexpr (what == 2) ks[n] = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(run_ks, BN * sbytes), ks_off + n * RPL * sbytes, 0, 0);
-    if constexpr (what == 3) vs[n] = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(run_vs, BN * sbytes), vs_off + n * RPL * sbytes, 0, 0);
+    if constexpr (what == 0) x.kc[n] = __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(run_k, BN * cbytes), k_off[n], 0, 0);
+    if constexpr (what == 1) x.vc[n] = __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(run_v, BN * cbytes), v_off + n * RPL * cbytes, 0, 0);
+    if constexpr (what == 2) x.ks[n] = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(run_ks, BN * sbytes), ks_off + n * RPL * sbytes, 0, 0);
+    if constexpr (what == 3) x.vs[n] = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(run_vs, BN * sbytes), vs_off + n * RPL * sbytes, 0, 0);
   };
   auto advance_run = [&]() __attribute__((always_inline)) {
     run_k += BN * cbytes;
@@ -153,15 +155,15 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   };
   // codes in the registers to the buffers at `boff`: job 2n: K, 2n + 1: V
   constexpr int NCVT = 2 * NLD;
-  auto convert = [&](auto job, uint32_t boff) __attribute__((always_inline)) {
+  auto convert = [&](auto job, uint32_t boff, const Codes& x) __attribute__((always_inline)) {
     constexpr int n = decltype(job)::value / 2;
     const uint32_t at = lds0 + boff + my_part + (uint32_t)(lane * 16 + n * 1024);
-    if constexpr (decltype(job)::value % 2 == 0) *(lds_u4)(uintptr_t)(at + kKBase) = q4_eight(kc[n], q4_scale(ks[n]));
-    else *(lds_u4)(uintptr_t)at = q4_eight(vc[n], q4_scale(vs[n]));
+    if constexpr (decltype(job)::value % 2 == 0) *(lds_u4)(uintptr_t)(at + kKBase) = q4_eight(x.kc[n], q4_scale(x.ks[n]));
+    else *(lds_u4)(uintptr_t)at = q4_eight(x.vc[n], q4_scale(x.vs[n]));
   };
 
   // sends the loads of tile t: codes and scale bytes to registers, bf16 rows to their buffers at `boff`
-  auto send = [&](int t, uint32_t boff) __attribute__((always_inline)) {
+  auto send = [&](int t, uint32_t boff, Codes& x) __attribute__((always_inline)) {
     if (t >= t_hi) return;
     if (t >= nb_s && t < nb_sg) {
       const int i0 = (t - nb_s) * BN;
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
         run_vs = a.vs + (int64_t)slot0 * sbytes;
       }
       if (run_left > 0) {
-        unrolled<NLOAD>(load_run);
+        unrolled<NLOAD>([&](auto job) __attribute__((always_inline)) { load_run(job, x); });
         advance_run();
       } else {
         bool real;
@@ -186,12 +188,12 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
           place(n, k_row, k_unit, v_row, v_unit);
           const int64_t sk = __shfl(slot, k_row, 64), sv = __shfl(slot, v_row, 64);
           const bool ok = __shfl((int)real, v_row, 64);
-          kc[n] = *(const __attribute__((address_space(1))) uint32_t*)((gptr)a.k4 + sk * cbytes + kv * (D / 2) + k_unit * 4);
-          ks[n] = *(const __attribute__((address_space(1))) uint8_t*)((gptr)a.ks + sk * sbytes + kv * (D / kQ4Group) + k_unit / 4);
+          x.kc[n] = *(const __attribute__((address_space(1))) uint32_t*)((gptr)a.k4 + sk * cbytes + kv * (D / 2) + k_unit * 4);
+          x.ks[n] = *(const __attribute__((address_space(1))) uint8_t*)((gptr)a.ks + sk * sbytes + kv * (D / kQ4Group) + k_unit / 4);
           const uint32_t w = *(const __attribute__((address_space(1))) uint32_t*)((gptr)a.v4 + sv * cbytes + kv * (D / 2) + v_unit * 4);
           const uint32_t b = *(const __attribute__((address_space(1))) uint8_t*)((gptr)a.vs + sv * sbytes + kv * (D / kQ4Group) + v_unit / 4);
-          vc[n] = ok ? w : 0;
-          vs[n] = ok ? b : 127;
+          x.vc[n] = ok ? w : 0;
+          x.vs[n] = ok ? b : 127;
         }
       }
       return;
@@ -211,10 +213,10 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   };
   // tile t into its buffers at `boff`: converted from the registers, or landed
   bool odd = false;                          // a value of the tail that is not finite
-  auto finish = [&](int t, uint32_t boff) __attribute__((always_inline)) {
+  auto finish = [&](int t, uint32_t boff, const Codes& x) __attribute__((always_inline)) {
     if (t >= t_hi) return;
     if (t >= nb_s && t < nb_sg) {
-      unrolled<NCVT>([&](auto job) __attribute__((always_inline)) { convert(job, boff); });
+      unrolled<NCVT>([&](auto job) __attribute__((always_inline)) { convert(job, boff, x); });
       return;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -222,20 +224,21 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
     const uint32_t at = lds0 + boff + my_part + (uint32_t)(lane * 16);
 #pragma unroll
     for (int n = 0; n < NLD; ++n) {
-      u32x4 x = *(lds_u4)(uintptr_t)(at + n * 1024);
+      u32x4 y = *(lds_u4)(uintptr_t)(at + n * 1024);
       u16x2 most{0, 0};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        largest_exponents(most, x[i]);
-        x[i] = finite_or_zero(x[i]);
+        largest_exponents(most, y[i]);
+        y[i] = finite_or_zero(y[i]);
       }
       odd |= not_finite(most);
-      *(lds_u4)(uintptr_t)(at + n * 1024) = x;
+      *(lds_u4)(uintptr_t)(at + n * 1024) = y;
     }
   };
   // what this wave wrote is there, and every other wave's
   auto meet = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
+  Codes codes;                               // of the tile after the last one in LDS
   f32x16 o[RB][NDB];
   float m_run[RB] = {-INFINITY}, l_run[RB] = {0.f}, neg_m[RB] = {INFINITY};
 #pragma unroll
@@ -247,11 +250,14 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   v_nx += lds0;
   v_rd = v_nx + (NB - 1) * TBY;
   if (t_lo < t_hi) {
-    send(t_lo, 0);
-    finish(t_lo, 0);
-    send(t_lo + 1, TBY);
-    finish(t_lo + 1, TBY);
-    send(t_lo + 2, 2 * TBY);
+    {
+      Codes c0, c1;                          // three tiles on the way together: one memory latency before the first step
+      send(t_lo, 0, c0);
+      send(t_lo + 1, TBY, c1);
+      send(t_lo + 2, 2 * TBY, codes);
+      finish(t_lo, 0, c0);
+      finish(t_lo + 1, TBY, c1);
+    }
     // the pipeline's first P V multiplies zero probabilities with the last 16 rows of the last V buffer (tile t_lo + 3
     // goes there after the first barrier of the loop)
     if (tid < RBY) *(lds_u4)(uintptr_t)(lds0 + (NB - 1) * TBY + 48 * RBY + tid * 16) = u32x4{0, 0, 0, 0};
@@ -289,15 +295,15 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
         // tile t + 2 is codes in the registers and t + 3 the run's next: one piece of that work a slot
         const bool in_run = run_left > 0 && t + 2 >= nb_s;
         if (!in_run) {
-          finish(t + 2, fill);
-          send(t + 3, (fill + TBY) & kWrap);
+          finish(t + 2, fill, codes);
+          send(t + 3, (fill + TBY) & kWrap, codes);
         }
         wt.template half<0, 16, 32>(s1, s0, p0, p1, [&](auto slot) __attribute__((always_inline)) {
           constexpr int s = decltype(slot)::value;
           if constexpr (s < NCVT + NLOAD) {
             if (in_run) {
-              if constexpr (s < NCVT) convert(slot, fill);
-              else load_run(std::integral_constant<int, s - NCVT>{});
+              if constexpr (s < NCVT) convert(slot, fill, codes);
+              else load_run(std::integral_constant<int, s - NCVT>{}, codes);
             }
           }
         });
@@ -309,8 +315,8 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
     }
     for (; t < t_hi; ++t) {                  // tiles that this wave's rows do not see: it brings its share
       meet();
-      finish(t + 2, (boff + 2 * TBY) & kWrap);
-      send(t + 3, (boff + 3 * TBY) & kWrap);
+      finish(t + 2, (boff + 2 * TBY) & kWrap, codes);
+      send(t + 3, (boff + 3 * TBY) & kWrap, codes);
       boff = (boff + TBY) & kWrap;
     }
   }

@@ -44,16 +44,26 @@ struct GatherQ4Shape {
   int64_t ws_bytes;
 };
 
-// Parts of the 256-row kernel: the count with the least time, in units of 0.1 us.  A round of work-groups takes
-// 5 us to start and end and 1.5 us a 64-key tile; a merge 4 us and the partials' way to memory and back.
-int tile_parts(int64_t groups, int64_t tiles, int64_t row_bytes, int64_t* cost) {
+// Packed rows of a KV head from which the 256-row kernel runs.
+constexpr int64_t kTileRows = 256;
+
+constexpr int64_t kAutoWorkspace = int64_t(48) << 20;     // most bytes that a split picked by the library needs
+
+// Parts of the 256-row kernel: the count with the least time, in units of 0.1 us.  A round of work-groups takes 5 us to
+// start and end and 1.6 us a 64-key tile (64 tiles more a work-group, 101.6 us); a merge 4 us and the partials' way to
+// memory and back.
+//
+// Equal shares of all tiles of all row tiles, one a CU, which keep every CU busy to the end, were no gain: 1024 rows over
+// 8192 keys, us, shares / parts: 7B heads 146.6 / 145.0 (224 work-groups: the chip runs at its power limit), 777 rows 118
+// / 130, 3B heads over 2000 keys 79 / 46, small heads 51 / 40 (more partials, more starts).
+int tile_parts(int64_t groups, int64_t tiles, int64_t part_bytes) {
   int best = 1;
-  *cost = INT64_MAX;
-  for (int p = 1; p <= kMaxGatherParts && p <= tiles; ++p) {
+  int64_t least = INT64_MAX;
+  for (int p = 1; p <= kMaxGatherParts && p <= tiles && (p == 1 || p * part_bytes <= kAutoWorkspace); ++p) {
     const int64_t rounds = (groups * p + kNumCUs - 1) / kNumCUs;
-    const int64_t c = rounds * (50 + 15 * ((tiles + p - 1) / p)) + (p > 1 ? 40 + p * row_bytes / 200000 : 0);
-    if (c < *cost) {
-      *cost = c;
+    const int64_t c = rounds * (50 + 16 * ((tiles + p - 1) / p)) + (p > 1 ? 40 + p * part_bytes / 200000 : 0);
+    if (c < least) {
+      least = c;
       best = p;
     }
   }
@@ -78,13 +88,12 @@ int check_gather_q4_shape(int32_t Lq, int32_t T, int32_t S, int32_t cap, int32_t
   if (Lq == 0) return VICO_OK;
   const int64_t rows = int64_t(Hq / Hkv) * Lq;
   const int64_t gathered = n_segs == 0 ? 0 : std::min<int64_t>(hint > 0 ? hint : cap, int64_t(n_segs) * cap);
-  const int64_t keys = S + gathered + T;
+  const int64_t keys = S + gathered + T, part_o = int64_t(4) * Hq * Lq * D, part_lse = int64_t(4) * Hq * Lq;
   int64_t most;
-  if (rows >= 256) {
-    sh->tile = 1;
+  sh->tile = rows >= kTileRows;
+  if (sh->tile) {
     sh->n_rt = (int)((rows + kBlockM - 1) / kBlockM);
-    int64_t cost;
-    most = tile_parts(int64_t(Hkv) * sh->n_rt, (keys + kKeyTile - 1) / kKeyTile, int64_t(4) * Hq * Lq * D, &cost);
+    most = tile_parts(int64_t(Hkv) * sh->n_rt, (keys + kKeyTile - 1) / kKeyTile, part_o + part_lse + 256);
   } else {
     sh->row_blocks = rows > 16 ? 2 : 1;
     sh->n_rt = (int)((rows + 16 * sh->row_blocks - 1) / (16 * sh->row_blocks));
@@ -92,7 +101,7 @@ int check_gather_q4_shape(int32_t Lq, int32_t T, int32_t S, int32_t cap, int32_t
     most = std::max<int64_t>(std::min<int64_t>(kNumCUs / (int64_t(Hkv) * sh->n_rt), (blocks + 7) / 8), 1);
   }
   sh->parts = (int)std::min<int64_t>(splits > 0 ? splits : most, kMaxGatherParts);
-  if (sh->parts > 1) sh->ws_bytes = align256(int64_t(4) * sh->parts * Hq * Lq * D) + int64_t(4) * sh->parts * Hq * Lq;
+  if (sh->parts > 1) sh->ws_bytes = align256(sh->parts * part_o) + sh->parts * part_lse;
   return VICO_OK;
 }
 

@@ -37,15 +37,6 @@ __device__ __forceinline__ uint32_t dpp(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, true);
 }
 
-// The kernel's arguments, read again from memory where they are used: what only the start, the end or the bf16
-// blocks need takes no scalar registers (and, spilled, no vector ones) in the store's loop.
-typedef const __attribute__((address_space(4))) RowsQ4Args* late_args;
-__device__ __forceinline__ late_args late() {
-  late_args p = (late_args)__builtin_amdgcn_kernarg_segment_ptr();
-  asm volatile("" : "+s"(p));
-  return p;
-}
-
 // A row tile's state and block bodies; D dims a head, NRB blocks of 16 rows.
 template <int D, int NRB, int NW>
 __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) {

@@ -18,9 +18,10 @@
 //     the tile body's second half, in the shadow of its MFMAs.
 //   * A tile lies in one region (sink, store, tail); the regions' last tiles may
 //     be part-filled, with zeros that the mask hides.
-//   * Values of tail tokens that are not finite are zeros in LDS (0 times such a
-//     value would reach the rows that do not see it) and are added afterwards
-//     for the rows that do: such a row's result is that value whatever its weight.
+//   * Values that are not finite in a tail tile that the causal mask cuts are
+//     zeros in LDS (0 times such a value would reach the rows that do not see it)
+//     and are added afterwards for the rows that do: such a row's result is that
+//     value whatever its weight.
 
 #include <type_traits>
 
@@ -86,6 +87,8 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   const int per_part = a.by_parts(n_tiles + a.parts - 1);
   const int t_lo = min(per_part * part, n_tiles), t_hi = min(t_lo + per_part, n_tiles);
   const int t_end = wave_active ? min(t_hi, nb_sg + last_lim / BN + 1) : t_lo;      // the wave's last tile
+  // the first tail tile that the causal mask cuts for some row of the work-group
+  const int t_cut = nb_sg + (tail0 + a.by_g(rt * BM) + 1) / BN;
   // the lane's last visible key in tile t, and whether some lane of the wave does not see all of the tile
   auto lim_of = [&](int t) __attribute__((always_inline)) {
     return t < nb_s ? a.S - 1 - t * BN : t < nb_sg ? G - 1 - (t - nb_s) * BN : tail0 + tok - (t - nb_sg) * BN;
@@ -198,10 +201,11 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
       }
       return;
     }
+    const late_args l = late();
     const bool sink = t < nb_s;
-    const int row0 = (sink ? t : t - nb_sg) * BN, left = min((sink ? a.S : a.T) - row0, BN) * rbytes;
-    const char* const bk = (const char*)(sink ? a.sink_k : a.tail_k) + (int64_t)row0 * rbytes;
-    const char* const bv = (const char*)(sink ? a.sink_v : a.tail_v) + (int64_t)row0 * rbytes;
+    const int row0 = (sink ? t : t - nb_sg) * BN, left = min((sink ? l->S : l->T) - row0, BN) * rbytes;
+    const char* const bk = (const char*)(sink ? l->sink_k : l->tail_k) + (int64_t)row0 * rbytes;
+    const char* const bv = (const char*)(sink ? l->sink_v : l->tail_v) + (int64_t)row0 * rbytes;
 #pragma unroll
     for (int n = 0; n < NLD; ++n) {
       int k_row, k_unit, v_row, v_unit;
@@ -220,7 +224,7 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
       return;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (t < nb_s) return;
+    if (t < t_cut) return;
     const uint32_t at = lds0 + boff + my_part + (uint32_t)(lane * 16);
 #pragma unroll
     for (int n = 0; n < NLD; ++n) {
@@ -328,7 +332,7 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   if (__builtin_expect(odd_s != 0, 0)) {
     const int k0 = max(t_lo - nb_sg, 0) * BN, k1 = min(max(t_hi - nb_sg, 0) * BN, last_lim + 1);
     for (int k = k0; k < k1; ++k) {
-      const uint16_t* p = a.tail_v + ((int64_t)k * a.Hkv + kv) * D + hh * 4;
+      const uint16_t* p = late()->tail_v + ((int64_t)k * a.Hkv + kv) * D + hh * 4;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -343,10 +347,11 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
   const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == l_tot ? 0.f : l_tot;        // 0 for an empty row, NaN stays
   const float lse2 = l_tot > 0.f ? m_run[0] + __log2f(l_tot) : l_tot == l_tot ? -INFINITY : l_tot;
   if (wrow0 + l32 >= NR) return;
-  const bool partial = a.parts > 1;
-  if (partial || a.out_f32) {
-    float* op = partial ? a.ws_o + (((int64_t)part * a.Hq + head) * a.Lq + tok) * D
-                        : (float*)a.out + ((int64_t)tok * a.Hq + head) * D;
+  const late_args l = late();
+  const bool partial = l->parts > 1;
+  if (partial || l->out_f32) {
+    float* op = partial ? l->ws_o + (((int64_t)part * l->Hq + head) * l->Lq + tok) * D
+                        : (float*)l->out + ((int64_t)tok * l->Hq + head) * D;
     op += hh * 4;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
@@ -357,7 +362,7 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
             f32x4{x[q4 * 4] * inv, x[q4 * 4 + 1] * inv, x[q4 * 4 + 2] * inv, x[q4 * 4 + 3] * inv};
       }
   } else {
-    __bf16* op = (__bf16*)a.out + ((int64_t)tok * a.Hq + head) * D + hh * 4;
+    __bf16* op = (__bf16*)l->out + ((int64_t)tok * l->Hq + head) * D + hh * 4;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -368,8 +373,8 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void attn_tile_q4_kernel(RowsQ4
       }
   }
   if (hh != 0) return;
-  if (partial) a.ws_lse[((int64_t)part * a.Hq + head) * a.Lq + tok] = lse2;
-  else if (a.lse) a.lse[(int64_t)head * a.Lq + tok] = lse2 * kLn2;
+  if (partial) l->ws_lse[((int64_t)part * l->Hq + head) * l->Lq + tok] = lse2;
+  else if (l->lse) l->lse[(int64_t)head * l->Lq + tok] = lse2 * kLn2;
 }
 
 }  // namespace

@@ -44,34 +44,59 @@ struct GatherQ4Shape {
   int64_t ws_bytes;
 };
 
-// Packed rows of a KV head from which the 256-row kernel runs.
-constexpr int64_t kTileRows = 256;
-
 constexpr int64_t kAutoWorkspace = int64_t(48) << 20;     // most bytes that a split picked by the library needs
+constexpr int64_t kTileMinRows = 128;                     // fewer packed rows of a KV head never take the 256-row kernel
 
-// Parts of the 256-row kernel: the count with the least time, in units of 0.1 us.  A round of work-groups takes 5 us to
-// start and end and 1.6 us a 64-key tile (64 tiles more a work-group, 101.6 us); a merge 4 us and the partials' way to
-// memory and back.
+// One way to run a call: kernel, row tiles, key-range parts, and its time in
+// ns: rounds of work-groups over the CUs, each a start (launch,
+// table, first keys, the waves' merge or the output) and its keys, 32 or 64 at a
+// time; then the merge of the parts (another launch, and more work above 16
+// parts), which also sends the partial results to memory and back (2 MB a us).
 //
-// Equal shares of all tiles of all row tiles, one a CU, which keep every CU busy to the end, were no gain: 1024 rows over
-// 8192 keys, us, shares / parts: 7B heads 146.6 / 145.0 (224 work-groups: the chip runs at its power limit), 777 rows 118
-// / 130, 3B heads over 2000 keys 79 / 46, small heads 51 / 40 (more partials, more starts).
-int tile_parts(int64_t groups, int64_t tiles, int64_t part_bytes) {
-  int best = 1;
-  int64_t least = INT64_MAX;
-  for (int p = 1; p <= kMaxGatherParts && p <= tiles && (p == 1 || p * part_bytes <= kAutoWorkspace); ++p) {
-    const int64_t rounds = (groups * p + kNumCUs - 1) / kNumCUs;
-    const int64_t c = rounds * (50 + 16 * ((tiles + p - 1) / p)) + (p > 1 ? 40 + p * part_bytes / 200000 : 0);
-    if (c < least) {
-      least = c;
-      best = p;
+// The rates, fitted to calls on otherwise idle CUs, all keys in one part, us for
+// 64 / 1024 / 8192 / 65536 keys: 16-row tiles, one row of the 7B heads 6.1 / 9.6 /
+// 41.4 / 319, of heads of size 64 (2048, 32768 keys) 8.6 / 80; 32-row tiles, 28 rows
+// (256, 1024, 16384 keys) 9.0 / 12.5 / 91, heads of size 64 6.4 / 8.6 / 61; 256-row
+// tiles 101.6 for 64 tiles more.
+//
+// Rows against 256-row kernel, each at its best, us: 7B heads, 224 rows, 2048 /
+// 20000 keys 13 / 21 and 23 / 34; 700 rows, 8192 / 20000 keys 32 / 36 and 62 / 50;
+// 1050 rows, 2048 / 8192 keys 20 / 31 and 51 / 41; 3B heads, 1600 rows, 8192 / 20000
+// keys 32 / 38 and 62 / 53; small heads, 1024 rows, 20000 keys 26 / 32.
+struct Q4Plan {
+  int tile, row_blocks, n_rt, parts;
+  int64_t cost;
+};
+
+struct Q4Cost {
+  int64_t groups, blocks, start, block, part_bytes;      // work-groups of one part, 32- or 64-key blocks
+  int64_t operator()(int64_t parts) const {
+    const int64_t rounds = (groups * parts + kNumCUs - 1) / kNumCUs;
+    return rounds * (start + block * ((blocks + parts - 1) / parts)) +
+           (parts > 1 ? (parts > 16 ? 4200 : 3500) + parts * part_bytes / 2000 : 0);
+  }
+};
+
+// The parts with the least time: those that fill the CUs once, or fewer by halves.
+Q4Plan best_parts(const Q4Cost& cost, int tile, int row_blocks, int n_rt, int splits) {
+  if (splits > 0) {
+    const int p = std::min(splits, kMaxGatherParts);
+    return Q4Plan{tile, row_blocks, n_rt, p, cost(p)};
+  }
+  Q4Plan best{tile, row_blocks, n_rt, 1, cost(1)};
+  const int64_t most = std::min(std::min<int64_t>(kNumCUs / cost.groups, kMaxGatherParts),
+                                std::min(cost.blocks, (kAutoWorkspace - 256) / cost.part_bytes));
+  for (int64_t p = most; p > 1; p /= 2) {
+    const int64_t c = cost(p);
+    if (c < best.cost) {
+      best.parts = (int)p;
+      best.cost = c;
     }
   }
   return best;
 }
 
-// Validates the shape arguments and plans: row tiles of 16 or 32 packed rows, and as many key-range parts as keep
-// the grid within one round of the CUs and leave each of a work-group's eight waves a block.
+// Validates the shape arguments and plans.
 int check_gather_q4_shape(int32_t Lq, int32_t T, int32_t S, int32_t cap, int32_t n_segs, int64_t hint, int32_t Hq,
                           int32_t Hkv, int32_t D, int32_t splits, GatherQ4Shape* sh) {
   if (Lq < 0 || T < Lq || S < 0 || cap < 0 || n_segs < 0 || n_segs > kMaxSegments || hint < 0 || splits < 0)
@@ -89,18 +114,22 @@ int check_gather_q4_shape(int32_t Lq, int32_t T, int32_t S, int32_t cap, int32_t
   const int64_t rows = int64_t(Hq / Hkv) * Lq;
   const int64_t gathered = n_segs == 0 ? 0 : std::min<int64_t>(hint > 0 ? hint : cap, int64_t(n_segs) * cap);
   const int64_t keys = S + gathered + T, part_o = int64_t(4) * Hq * Lq * D, part_lse = int64_t(4) * Hq * Lq;
-  int64_t most;
-  sh->tile = rows >= kTileRows;
-  if (sh->tile) {
-    sh->n_rt = (int)((rows + kBlockM - 1) / kBlockM);
-    most = tile_parts(int64_t(Hkv) * sh->n_rt, (keys + kKeyTile - 1) / kKeyTile, part_o + part_lse + 256);
-  } else {
-    sh->row_blocks = rows > 16 ? 2 : 1;
-    sh->n_rt = (int)((rows + 16 * sh->row_blocks - 1) / (16 * sh->row_blocks));
-    const int64_t blocks = (keys + kRowsBlock - 1) / kRowsBlock;
-    most = std::max<int64_t>(std::min<int64_t>(kNumCUs / (int64_t(Hkv) * sh->n_rt), (blocks + 7) / 8), 1);
+  const int64_t blocks = (keys + kRowsBlock - 1) / kRowsBlock, tiles = (keys + kKeyTile - 1) / kKeyTile;
+  const bool d128 = D == 128;
+  const int rb = rows > 16 ? 2 : 1, n_rt = (int)((rows + 16 * rb - 1) / (16 * rb));
+  Q4Cost c{int64_t(Hkv) * n_rt, blocks, rb == 1 ? 3800 : d128 ? 6000 : 4800,
+           rb == 1 ? (d128 ? 140 : 75) : (d128 ? 163 : 113), part_o + part_lse};
+  Q4Plan best = best_parts(c, 0, rb, n_rt, splits);
+  if (rows >= kTileMinRows) {
+    const int n256 = (int)((rows + kBlockM - 1) / kBlockM);
+    c.groups = int64_t(Hkv) * n256;
+    c.blocks = tiles;
+    c.start = 5000;
+    c.block = d128 ? 1600 : 1200;
+    const Q4Plan p = best_parts(c, 1, 0, n256, splits);
+    if (p.cost < best.cost) best = p;
   }
-  sh->parts = (int)std::min<int64_t>(splits > 0 ? splits : most, kMaxGatherParts);
+  sh->tile = best.tile; sh->row_blocks = best.row_blocks; sh->n_rt = best.n_rt; sh->parts = best.parts;
   if (sh->parts > 1) sh->ws_bytes = align256(sh->parts * part_o) + sh->parts * part_lse;
   return VICO_OK;
 }

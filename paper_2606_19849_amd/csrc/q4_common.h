@@ -34,6 +34,15 @@ __device__ __forceinline__ u32x4 q4_eight(uint32_t w, float scale) {
 
 __device__ __forceinline__ float q4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// The kernel's arguments, read again from memory where they are used: what only the start, the end or the bf16
+// blocks need takes no scalar registers (and, spilled, no vector ones) in the store's loop.
+typedef const __attribute__((address_space(4))) RowsQ4Args* late_args;
+__device__ __forceinline__ late_args late() {
+  late_args p = (late_args)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
 // Pairs of bf16 values that are not finite: the largest exponent fields of the pairs seen so far, and the pair with
 // zeros in their place.
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));

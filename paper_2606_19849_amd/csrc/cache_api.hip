@@ -282,6 +282,20 @@ int vico_gather_plan_q4(int32_t q_len, int32_t tail_len, int32_t sink_len, int32
   return VICO_OK;
 }
 
+int vico_gather_q4_route(int32_t q_len, int32_t tail_len, int32_t sink_len, int32_t store_slots, int32_t num_segments,
+                         int64_t keys_hint, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                         int32_t num_splits, int32_t* route_out) {
+  GatherQ4Shape sh;
+  const int st = check_gather_q4_shape(q_len, tail_len, sink_len, store_slots, num_segments, keys_hint, num_q_heads,
+                                       num_kv_heads, head_dim, num_splits, &sh);
+  if (st != VICO_OK) return st;
+  route_out[0] = sh.tile ? kRouteTile : kRouteRows;
+  route_out[1] = sh.parts;
+  route_out[2] = sh.Hkv * sh.n_rt * sh.parts;
+  route_out[3] = sh.tile ? kBlockM : 16 * sh.row_blocks;
+  return VICO_OK;
+}
+
 int vico_gather_attn_q4(const void* q, int32_t q_len, const void* tail_k, const void* tail_v, int32_t tail_len,
                         const void* sink_k, const void* sink_v, int32_t sink_len, const void* store_k,
                         const void* store_v, const void* scale_k, const void* scale_v, int32_t store_slots,

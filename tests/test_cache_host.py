@@ -153,6 +153,29 @@ def test_plan_reports_the_workspace():
         vico.vico_gather_plan_q4(3, 2, 0, 0, 0, 0, 8, 2, 64)
 
 
+def route(q_len, tail, S, slots, n_segs, hint, heads, splits=0):
+    out = (ctypes.c_int32 * 4)()
+    assert lib.vico_gather_q4_route(q_len, tail, S, slots, n_segs, ctypes.c_int64(hint), *heads, splits, out) == 0
+    return tuple(out)
+
+
+def test_which_kernel_runs():
+    """Few rows or few keys: the rows kernel; many rows over many keys, or more parts than its row tiles have room for:
+    256-row tiles.  The parts of the plan are those of the route."""
+    b7, small = (28, 4, 128), (8, 2, 64)
+    assert route(1, 64, 64, 200000, 32, 18000, b7) == (2, 64, 256, 16)
+    assert route(1, 64, 0, 0, 0, 0, b7)[:2] == (2, 1)
+    assert route(32, 32, 64, 200000, 32, 18000, b7) == (2, 9, 252, 32)
+    assert route(1024, 1024, 64, 8192, 2, 8192, b7) == (0, 2, 224, 256)
+    assert route(2048, 2048, 16, 200, 2, 200, b7)[::3] == (0, 256)
+    assert route(130, 130, 16, 300, 2, 300, b7, 16) == (0, 16, 256, 256)
+    assert route(257, 300, 16, 300, 2, 300, small, 64) == (0, 64, 640, 256)
+    for q_len in (1, 3, 17, 40, 200, 1000, 3000):
+        for hint in (0, 100, 5000, 200000):
+            parts, _ = vico.vico_gather_plan_q4(q_len, q_len, 64, 1 << 18, 32, hint, *b7)
+            assert route(q_len, q_len, 64, 1 << 18, 32, hint, b7)[1] == parts
+
+
 def test_host_tensors_and_wrong_shapes_are_refused():
     bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)   # noqa: E731
     u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)      # noqa: E731

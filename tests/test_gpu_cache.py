@@ -319,6 +319,32 @@ def test_attention_of_a_chunk_over_a_ring_window(heads, C, W):
     c.check(splits=2)
 
 
+@pytest.mark.parametrize("heads", [(28, 4, 128), (8, 2, 64), (16, 1, 128)], ids=str)
+@pytest.mark.parametrize("splits", [16, 64])
+@pytest.mark.parametrize("q_len,tail,S,starts,lens", [
+    (130, 130, 16, [112, 0], [188, 112]), (257, 300, 0, [5, 100, 260], [31, 33, 40]), (150, 151, 100, [], []),
+    (140, 200, 64, list(range(0, 300, 2)), [2, 0, 3] * 50)])
+def test_attention_in_256_row_tiles(heads, splits, q_len, tail, S, starts, lens):
+    c = Case(q_len + S, *heads, q_len, tail, S, 300, starts, lens)
+    c.check(splits)
+    c.check(splits, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_a_large_chunk_without_parts(dtype):
+    """224 tiles of 256 rows, one work-group each; a few heads against the oracle."""
+    c = Case(20, 28, 4, 128, 2048, 2048, 16, 200, [75, 0], [125, 75])
+    o, l = c.run(0, dtype)
+    assert c.parts == 1
+    heads = [0, 13, 27]
+    ref, ref_lse = oracle.gather_attention(*c.args, heads=heads)
+    b = gather_bound(*c.args, heads=heads, parts=2)
+    if dtype == torch.float32:
+        check_f32(o[:, heads], ref, b, l[heads], ref_lse)
+    else:
+        check_bf16(o[:, heads], ref, b)
+
+
 def test_attention_scales_and_large_logits():
     c = Case(11, 8, 2, 64, 4, 30, 10, 200, [0], [200], sigma=12.0)
     c.check()
@@ -337,15 +363,15 @@ def test_attention_streams_and_repeats():
 @pytest.mark.parametrize("heads", [(8, 2, 64), (14, 2, 128)], ids=str)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("where", ["k", "v"])
-@pytest.mark.parametrize("q_len,tail", [(5, 9), (70, 90)])
-def test_what_is_masked_does_not_reach_a_row(heads, bad, where, q_len, tail):
+@pytest.mark.parametrize("q_len,tail,parts", [(5, 9, (1, 3)), (70, 90, (1, 3)), (140, 170, (1, 16))])
+def test_what_is_masked_does_not_reach_a_row(heads, bad, where, q_len, tail, parts):
     """Tail tokens that are not finite change the rows that see them and no others."""
     at = tail - q_len + 2                                  # first seen by row 2
     clean = Case(13, *heads, q_len, tail, 3, 100, [0], [77])
     def tweak(c):                                          # noqa: E306
         c.tail["kv".index(where)][at, 1, 3] = bad
     dirty = Case(13, *heads, q_len, tail, 3, 100, [0], [77], tweak=tweak)
-    for splits in (1, 3):
+    for splits in parts:
         a, la = clean.run(splits)
         b, lb = dirty.run(splits)
         g = heads[0] // heads[1]
@@ -376,15 +402,15 @@ def test_nan_of_the_store_reaches_every_row():
         assert np.isnan(o[:, 4:]).all() and np.isnan(l[4:]).all()
 
 
-@pytest.mark.parametrize("q_len,tail", [(2, 4), (60, 61)])
+@pytest.mark.parametrize("q_len,tail,parts", [(2, 4, (1, 3)), (60, 61, (1, 3)), (150, 151, (1, 16))])
 @pytest.mark.parametrize("S", [5, 64])
-def test_nan_of_the_sink_or_the_old_tail_reaches_every_row(q_len, tail, S):
+def test_nan_of_the_sink_or_the_old_tail_reaches_every_row(q_len, tail, parts, S):
     def tweak(c):
         c.sink[1][3, 0, 7] = float("nan")                  # KV head 0
         c.tail[1][0, 1, 9] = float("inf")                  # KV head 1: a token before every row
     c = Case(19, 8, 2, 64, q_len, tail, S, 100, [0], [77], tweak=tweak)
     clean = Case(19, 8, 2, 64, q_len, tail, S, 100, [0], [77])
-    for splits in (1, 3):
+    for splits in parts:
         (o, l), (a, la) = c.run(splits), clean.run(splits)
         assert np.isnan(o[:, :4, 7]).all() and np.all(o[:, 4:, 9] == np.inf) and np.array_equal(l, la)
         o[:, :4, 7], o[:, 4:, 9], a[:, :4, 7], a[:, 4:, 9] = 0, 0, 0, 0

@@ -18,7 +18,9 @@
 // pair a thread, into LDS, and its heads, q, k and v alike, D/16 lanes a head; a
 // lane holds 8 pairs (two 16-byte units), loaded before the angles are ready.
 // Two or four tokens a work-group leave fewer loads in flight at a time: 9.4 and
-// 11.6 us for 9.0 on that chunk.
+// 11.6 us for 9.0 on that chunk.  The next head is loaded after this one's
+// stores: loaded before its arithmetic it costs registers, and waves (78 for 73,
+// 0.2 us more).
 
 #include "attn_common.h"
 
@@ -77,9 +79,9 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
     x.xa = *(const u32x4*)(src + x.ea);
     x.xb = *(const u32x4*)(src + x.eb);
   };
-  Head next;
-  int i = tid / LPH;
-  if (i < heads) load(i, next);
+  Head x;
+  int head = tid / LPH;
+  if (head < heads) load(head, x);
 
   // ---- sines and cosines of the token's angles
   for (int p = tid; p < a.rot / 2; p += (int)blockDim.x) {
@@ -90,12 +92,11 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
   }
   __syncthreads();
 
-  for (; i < heads; i += step) {         // whole heads: the lanes of a head stay together
-    const Head x = next;
-    if (i + step < heads) load(i + step, next);
+  while (head < heads) {                 // whole heads: the lanes of a head stay together
     if (x.kind == 2) {
       *(u32x4*)(x.dst + x.ea) = x.xa;
       *(u32x4*)(x.dst + x.eb) = x.xb;
+      if ((head += step) < heads) load(head, x);
       continue;
     }
     float fa[8], fb[8];
@@ -146,6 +147,7 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
     }
     *(u32x4*)(x.dst + x.ea) = pack(fa);
     *(u32x4*)(x.dst + x.eb) = pack(fb);
+    if ((head += step) < heads) load(head, x);
   }
 }
 

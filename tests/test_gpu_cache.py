@@ -360,6 +360,57 @@ def test_attention_streams_and_repeats():
     assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("heads,q_len,splits", [((1024, 1024, 64), 1, 0), ((1024, 4, 64), 1, 2), ((1024, 2, 128), 2, 5),
+                                                ((200, 200, 128), 130, 1)], ids=str)
+def test_attention_of_very_many_heads(heads, q_len, splits):
+    Case(13, *heads, q_len, q_len + 3, 5, 90, [2, 70], [60, 11]).check(splits)
+
+
+def test_the_other_calls_with_very_many_heads():
+    check_rope(rope_case(8, 3, 1024, 1024, 64))
+    check_rope(rope_case(9, 2, 1024, 1, 128, axes=3))
+    st, x = empty_store(9, 1024, 128), normal(gen(30), 9, 1024, 128).to(DEV)
+    vico.vico_kv_append_q4(x, x.flip(0).contiguous(), *st, 4)
+    back = torch.empty_like(x), torch.empty_like(x)
+    vico.vico_kv_load_q4(*st, torch.tensor([4, 0], device=DEV), torch.tensor([5, 4], dtype=torch.int32, device=DEV), *back)
+    torch.cuda.synchronize()
+    order = [4, 5, 6, 7, 8, 0, 1, 2, 3]
+    assert np.array_equal(f64(back[0]), store_values(st)[0][order]) and torch.equal(back[0], back[1].flip(0))
+    # a group's largest magnitude is above 3.5 scales, and no value is further off than one
+    groups = lambda t: f64(t).reshape(9, 1024, 4, 32)   # noqa: E731
+    assert np.all(np.abs(groups(back[0]) - groups(x)) <= np.abs(groups(x)).max(-1, keepdims=True) / 3.5)
+
+
+def test_two_calls_at_once():
+    """The same table and store read from two streams, each with its own workspace: rows and 256-row kernel."""
+    a = Case(14, 28, 4, 128, 2, 70, 64, 20000, [0, 9000], [8000, 9000])
+    b = Case(15, 28, 4, 128, 300, 310, 64, 20000, [0, 9000], [8000, 9000])
+    sets = []
+    for c in (a, b):
+        parts, wb = vico.vico_gather_plan_q4(*c.sizes[:5], c.keys, *c.sizes[6:])
+        args = [t.to(DEV) for t in (c.q, *c.tail, *c.sink)] + list(a.store) + [t.to(DEV) for t in a.seg]
+        sets.append((args, torch.empty(c.q.shape, device=DEV), torch.empty(max(wb, 1), dtype=torch.uint8, device=DEV), c.keys))
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def call(i, stream):
+        args, out, ws, hint = sets[i]
+        vico.vico_gather_attn_q4(*args, out, workspace=ws, keys_hint=hint, stream=stream)
+
+    for i in range(2):
+        call(i, None)
+    torch.cuda.synchronize()
+    want = [s[1].clone() for s in sets]
+    for s in sets:
+        s[1].zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i in range(2):
+            call(i, streams[i])
+    torch.cuda.synchronize()
+    for s, w in zip(sets, want):
+        assert torch.equal(s[1], w)
+
+
 @pytest.mark.parametrize("heads", [(8, 2, 64), (14, 2, 128)], ids=str)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("where", ["k", "v"])

@@ -22,6 +22,18 @@
 // Probabilities are rounded to bf16 for the second product, as in the bf16
 // kernels; logits, softmax state and sums are fp32.
 //
+// What bounds it.  A decode step streams the store: 16 waves a CU, one 16-row
+// block each, have 16 blocks on the way, and 7B heads over 256 chunks (262k keys,
+// 143 MB) take 35.4 us, loads alone 34.4 (4.6 TB/s between the first load and the
+// last).  8 waves with the next block loaded ahead took 39; with the heads of a
+// key range on different XCDs 48: a token's codes are 64 bytes a head, and two
+// heads share a cache line.  Over 32 chunks the launch, the table, a memory latency
+// and the waves' merge are most of its 7.6 us.  Above 16 rows, two row
+// blocks a wave use each converted block twice, at 8 waves' registers: 224 rows
+// over 17.8k keys (a 32-token query, 7B heads) 21.3 us, against 30.4 with one row
+// block; what bounds those is issue, of conversion and softmax between the matrix
+// products (the matrix cores are busy for 18 % of the cycles), and the start.
+//
 // A masked key's probability is 0, but 0 times a NaN or an infinity is not: in
 // a block that the causal mask cuts, such values of V are zeros and are added at
 // the end for the rows that see them (whatever its weight, such a value is the

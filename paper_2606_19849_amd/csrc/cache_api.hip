@@ -47,11 +47,11 @@ struct GatherQ4Shape {
 constexpr int64_t kAutoWorkspace = int64_t(48) << 20;     // most bytes that a split picked by the library needs
 constexpr int64_t kTileMinRows = 128;                     // fewer packed rows of a KV head never take the 256-row kernel
 
-// One way to run a call: kernel, row tiles, key-range parts, and its time in
-// ns: rounds of work-groups over the CUs, each a start (launch,
-// table, first keys, the waves' merge or the output) and its keys, 32 or 64 at a
-// time; then the merge of the parts (another launch, and more work above 16
-// parts), which also sends the partial results to memory and back (2 MB a us).
+// One way to run a call: kernel, row tiles, key-range parts, and its time in ns:
+// rounds of work-groups over the CUs, each a start (launch, table, first keys, the
+// waves' merge or the output) and its keys, 32 or 64 at a time; then the merge of
+// the parts (another launch, and more work above 16 parts) with the partial
+// results' way to memory and back (2 MB a us).
 //
 // The rates, fitted to calls on otherwise idle CUs, all keys in one part, us for
 // 64 / 1024 / 8192 / 65536 keys: 16-row tiles, one row of the 7B heads 6.1 / 9.6 /

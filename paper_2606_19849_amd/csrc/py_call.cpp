@@ -96,6 +96,7 @@ struct Args {
   void* stream() {
     PyObject* o = next();
     if (o == Py_None) return ok ? (void*)c10::hip::getCurrentHIPStream().stream() : nullptr;
+    --i;
     return (void*)(uintptr_t)integer();
   }
 };

@@ -620,6 +620,25 @@ def test_both_paths_of_the_binding_give_the_same(monkeypatch):
         assert np.array_equal(a, b)
 
 
+def test_a_stream_handle_takes_the_short_path():
+    """Plain calls with a stream are answered by the C++ part of the binding, on that stream."""
+    import paper_2606_19849_amd._binding as binding
+    calls, s = binding._fast(), torch.cuda.Stream()
+    st, k = empty_store(8, 2, 64), normal(gen(19), 4, 2, 64).to(DEV)
+    out = [torch.zeros_like(k) for _ in range(4)]
+    seg = torch.zeros(1, dtype=torch.int64, device=DEV), torch.full((1,), 4, dtype=torch.int32, device=DEV)
+    pos, freq = torch.arange(4, dtype=torch.int32, device=DEV)[None], torch.rand(32, generator=gen(20)).to(DEV)
+    torch.cuda.synchronize()
+    h = s.cuda_stream
+    assert calls.append_q4(k, k, *st, 0, h) == 0
+    assert calls.load_q4(*st, *seg, out[0], out[1], None, h) == 0
+    assert calls.gather_q4(k[:1], k, k, None, None, *st, *seg, out[2][:1], None, 4, 1, 0.0, h, None) == 0
+    assert calls.qk_norm_rope(k, k, pos, freq, out[2], out[3], None, None, None, None, 1e-6, 0, 0, 0, 0, h) == 0
+    s.synchronize()
+    assert np.array_equal(f64(out[0]), store_values(st)[0][:4]) and torch.equal(out[0], out[1])
+    assert torch.equal(out[2], out[3]) and bool(out[2].any())
+
+
 def test_refusals_of_the_binding():
     bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device=DEV)   # noqa: E731
     st = empty_store(8, 2, 64)

@@ -24,13 +24,13 @@
 //
 // What bounds it.  A decode step streams the store: 16 waves a CU, one 16-row
 // block each, have 16 blocks on the way, and 7B heads over 256 chunks (262k keys,
-// 143 MB) take 35.4 us, loads alone 34.4 (4.6 TB/s between the first load and the
+// 143 MB) take 34.6 us, loads alone 34.4 (4.6 TB/s between the first load and the
 // last).  8 waves with the next block loaded ahead took 39; with the heads of a
 // key range on different XCDs 48: a token's codes are 64 bytes a head, and two
 // heads share a cache line.  Over 32 chunks the launch, the table, a memory latency
 // and the waves' merge are most of its 7.6 us.  Above 16 rows, two row
 // blocks a wave use each converted block twice, at 8 waves' registers: 224 rows
-// over 17.8k keys (a 32-token query, 7B heads) 21.3 us, against 30.4 with one row
+// over 17.8k keys (a 32-token query, 7B heads) 20.7 us, against 30.4 with one row
 // block; what bounds those is issue, of conversion and softmax between the matrix
 // products (the matrix cores are busy for 18 % of the cycles), and the start.
 //
@@ -322,8 +322,8 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
   };
 
   // ---- the wave's blocks: every NW-th of the part's.  (Loading the next block's codes while one is computed measured
-  // the same with 8 waves, 21.3 and 21.8 us on 224 rows over 17.8k keys, and does not fit 16 waves' registers: the
-  // other waves' loads fill the gap.)
+  // the same with 8 waves, 21.3 and 21.8 us on 224 rows over 17.8k keys, and so did two blocks at a time; neither fits
+  // 16 waves' registers.  The other waves' loads fill the gap.)
   const int end_g = nb_s + nb_g;
   auto step_to = [&](int b, int to) __attribute__((always_inline)) { return b + (max(to - b, 0) + NW - 1) / NW * NW; };
   const int first_g = step_to(b_lo + wave, nb_s), last_g = min(b_hi, end_g);
@@ -341,6 +341,11 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
     bf16_block(sink ? l->sink_k : l->tail_k, sink ? l->sink_v : l->tail_v, rows, row0, lim,
                row0 + BK - 1 > (sink ? rows - 1 : tail_first), !sink);
   }
+  // The waves of a SIMD go by age where they want the same slot: of 224 rows over 17.8k keys the older half ends at
+  // 14.5 us of 19, and the younger one goes on alone, at half the issue rate.  Turned round they end closer together:
+  // 23.0 -> 22.4 us a call, decode over 262k keys 40.0 -> 39.6.  Turned back after half or three quarters of the blocks:
+  // 22.4 and 22.1, but 40.9.
+  if (wave >= NW / 2) __builtin_amdgcn_s_setprio(1);
   for (int b = first_g; b < last_g; b += NW) {
     Codes x;
     load_codes((b - nb_s) * BK, x);

@@ -345,6 +345,15 @@ def test_a_large_chunk_without_parts(dtype):
         check_bf16(o[:, heads], ref, b)
 
 
+@pytest.mark.parametrize("heads", [(28, 4, 128), (8, 2, 64)], ids=str)
+@pytest.mark.parametrize("q_len", [1, 3, 11])
+def test_a_long_sink_and_tail(heads, q_len):
+    """Each wave has several bf16 blocks, before and after those of the store."""
+    c = Case(16, *heads, q_len, 1400, 700, 300, [5, 200], [150, 90])
+    c.check(splits=1)
+    c.check(splits=2)
+
+
 def test_attention_scales_and_large_logits():
     c = Case(11, 8, 2, 64, 4, 30, 10, 200, [0], [200], sigma=12.0)
     c.check()

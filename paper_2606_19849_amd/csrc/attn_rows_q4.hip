@@ -187,11 +187,6 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
   };
 
   // ---- rows row0 .. row0 + 31 of a bf16 tensor with `rows` (rows past it read as zero); lim counts from row0
-  // Sixteen waves have no registers for V beside K: it waits in the wave's part of the merge buffer, each lane's
-  // 16 bytes where it will read them.
-  constexpr bool kStageV = D == 128 && NRB == 1;
-  char* const v_stage = (char*)&o_s[wave][0][0];
-  static_assert(!kStageV || sizeof(o_s[0]) >= 8 * 1024, "a block's V in the wave's part of the merge buffer");
   bool odd = false;                                // a value of the tail that is not finite
   auto bf16_block = [&](const uint16_t* bk, const uint16_t* bv, int rows, int row0, const int (&lim)[NRB],
                         bool masked, bool tail) __attribute__((always_inline)) {
@@ -200,9 +195,7 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
     const rsrc_t rv = make_rsrc((const char*)bv + (int64_t)row0 * rbytes, left);
     const uint32_t k_off = (uint32_t)(ka * rbytes + kv * D * 2 + j * DPL * 2);
     const uint32_t v_off = (uint32_t)(8 * j * rbytes + kv * D * 2 + n * VE * 2);
-    // K and V on the way together: a wave with such a block is the last of its work-group
     bf16x8 pf[NRB];
-    vrow_t vr[8];
     {
       u32x4 kr[2][NKS];
 #pragma unroll
@@ -210,17 +203,13 @@ __global__ __launch_bounds__(NW * 64, 1) void attn_rows_q4_kernel(RowsQ4Args a) 
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks)
           kr[h][ks] = __builtin_amdgcn_raw_buffer_load_b128(rk, k_off + h * 4 * rbytes + ks * 16, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (kStageV) load_lds16(rv, (lds_void*)(v_stage + i * 1024), v_off + i * rbytes);
-        else if constexpr (VE == 8) vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, v_off + i * rbytes, 0, 0);
-        else vr[i] = __builtin_amdgcn_raw_buffer_load_b64(rv, v_off + i * rbytes, 0, 0);
-      }
       probabilities(kr, pf, lim, masked);
     }
-    if constexpr (kStageV) {
+    vrow_t vr[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) vr[i] = *(const vrow_t*)(v_stage + i * 1024 + lane * 16);
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (VE == 8) vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, v_off + i * rbytes, 0, 0);
+      else vr[i] = __builtin_amdgcn_raw_buffer_load_b64(rv, v_off + i * rbytes, 0, 0);
     }
     if (masked && tail) {
       u16x2 most{0, 0};

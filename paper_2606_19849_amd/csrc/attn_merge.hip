@@ -24,6 +24,7 @@ namespace {
 constexpr int kMergeThreads = 256;
 constexpr int kFewParts = 16;    // up to here one thread per (row, 4 columns) loads all parts
 constexpr int kPartsPerThread = 8;   // many parts: parts one thread loads (64 parts over 8 part groups)
+constexpr float kDropped = -1.f;     // many parts: weight of a part that is left out
 
 // With an append requested, the blocks past `merge_blocks` copy the chunk's
 // K/V into the ring instead of merging: this launch runs after every read of
@@ -38,7 +39,7 @@ __device__ __forceinline__ bool append_block(const AttnArgs& a, int merge_blocks
 
 // The log-sum-exp of a row whose weights are NaN: NaN where the caller asks for it.
 __device__ __forceinline__ float lse_or_nan(float lse, float sum, const AttnArgs& a) {
-  return a.nan_lse && sum != sum ? sum : lse;
+  return a.keep_nan && sum != sum ? sum : lse;
 }
 
 // Few parts, many rows (chunk prefill splits): one thread per (head, row,
@@ -119,7 +120,9 @@ __global__ __launch_bounds__(kMergeThreads) void attn_merge_kernel(AttnArgs a, i
     float sum = w;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    w_s[r][lane] = w;
+    // a part that saw no key is left out, its O slot may hold anything; one whose weight is 0 in fp32 counts where the
+    // caller asks for it, 0 times a NaN or an infinity being the row's result
+    w_s[r][lane] = ls == -INFINITY || (!a.keep_nan && w == 0.f) ? kDropped : w;
     if (lane == 0) {
       inv_s[r] = sum > 0.f ? 1.f / sum : 0.f;
       lse_s[r] = lse_or_nan(sum > 0.f ? (m_use + __log2f(sum)) * kLn2 : -INFINITY, sum, a);
@@ -142,16 +145,16 @@ __global__ __launch_bounds__(kMergeThreads) void attn_merge_kernel(AttnArgs a, i
 #pragma unroll
     for (int i = 0; i < kPartsPerThread; ++i) {
       // unconditional loads (a part past the last, or one that saw no key and
-      // left its slot unwritten, reads a slot in range and gets weight 0; the
-      // select below drops whatever it holds)
+      // left its slot unwritten, reads a slot in range; the select below
+      // drops whatever it holds)
       const int p = pg + i * PG;
       const int pc = min(p, a.splits - 1);
-      w[i] = p < a.splits ? w_s[r][p] : 0.f;
+      w[i] = p < a.splits ? w_s[r][p] : kDropped;
       v[i] = *(const f32x4*)(a.ws_o + (pc * stride + hr) * D + dq * 4);
     }
 #pragma unroll
     for (int i = 0; i < kPartsPerThread; ++i)
-      if (pg + i * PG < a.splits) acc += w[i] != 0.f ? w[i] * v[i] : f32x4{0.f, 0.f, 0.f, 0.f};
+      acc += w[i] < 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : w[i] * v[i];          // a NaN weight counts
   }
   acc_s[tid] = acc;
   __syncthreads();

@@ -356,7 +356,7 @@ int vico_gather_attn_q4(const void* q, int32_t q_len, const void* tail_k, const 
     AttnArgs m{};
     m.out = a.out; m.lse = a.lse; m.ws_o = a.ws_o; m.ws_lse = a.ws_lse;
     m.C = a.Lq; m.Hq = a.Hq; m.Hkv = a.Hkv; m.D = a.D;
-    m.splits = a.parts; m.out_f32 = a.out_f32; m.nan_lse = 1;
+    m.splits = a.parts; m.out_f32 = a.out_f32; m.keep_nan = 1;
     e = launch_merge(m, (hipStream_t)stream);
   }
   return status_of(e);

@@ -54,7 +54,8 @@ struct AttnArgs {
   int app_p0;          // first ring slot written = hist_len mod R
   int app_blocks;      // > 0: extra work-groups of the attention launch that append (no split; the
                        // written slots are outside the window)
-  int nan_lse;              // merge: the log-sum-exp of a row with NaN logits is NaN (0: -inf)
+  int keep_nan;        // merge: 1: the log-sum-exp of a row with NaN logits is NaN, and a NaN or an infinity of a part
+                       // counts whatever the part's weight; 0: -inf, and of many parts not where the weight is 0
 };
 
 // Short-query attention over gathered key segments: query rows are the last

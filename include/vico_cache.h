@@ -51,7 +51,8 @@ extern "C" {
  * vico_qk_norm_rope -- norms of queries and keys for each head, with the
  * position rotation in the same pass; optionally the values' copy.
  *
- * For token t and each head, in fp32, rounded to bf16 once at the end:
+ * For token t and each head, in fp32 (the norm of finite inputs of any size),
+ * rounded to bf16 once at the end:
  *     x' = x * weight / sqrt(mean(x^2) + eps)        (x' = x where the weight is NULL)
  *     y0 = x0' cos a - x1' sin a,  y1 = x1' cos a + x0' sin a
  * for the rotary_dim / 2 pairs (x0, x1) of the head's first rotary_dim

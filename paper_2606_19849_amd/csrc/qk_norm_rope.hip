@@ -54,6 +54,31 @@ __device__ __forceinline__ void weights(const void* w, int f32, int at, float (&
   }
 }
 
+// The norm of a head whose squares leave fp32 (a mean below 2^-100 has lost some of them, an infinite one all): x and
+// the squares scaled by powers of two.  Returns the factor that is still to be applied.
+template <int LPH>
+__device__ __forceinline__ float scaled_norm(float (&fa)[8], float (&fb)[8], float mean, float eps) {
+  const bool tiny = mean < 1.f;
+  const float up = tiny ? 0x1p100f : 1.f, down = tiny ? 1.f : 0x1p-70f, sc = up * down;
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    fa[i] *= up;                         // exact: at most 2^-46 before
+    fb[i] *= up;
+    const float u = fa[i] * down, v = fb[i] * down;
+    ss = __builtin_fmaf(u, u, __builtin_fmaf(v, v, ss));
+  }
+#pragma unroll
+  for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
+  const float r = 1.f / sqrtf(ss * (1.f / (16 * LPH)) + eps * sc * sc);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    fa[i] *= r;
+    fb[i] *= r;
+  }
+  return down;
+}
+
 template <int D>
 __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) {
   constexpr int LPH = D / 16;            // lanes of a head
@@ -112,7 +137,10 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
       for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(fa[i], fa[i], __builtin_fmaf(fb[i], fb[i], ss));
 #pragma unroll
       for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
-      const float r = 1.f / sqrtf(ss * (1.f / D) + a.eps);
+      const float mean = ss * (1.f / D) + a.eps;
+      float r = 1.f / sqrtf(mean);
+      // (alike in all lanes of a head)
+      if (__builtin_expect(!(mean >= 0x1p-100f && mean < INFINITY), 0)) r = scaled_norm<LPH>(fa, fb, mean, a.eps);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         fa[i] = fa[i] * r * wa[i];

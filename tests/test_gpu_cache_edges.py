@@ -40,3 +40,55 @@ def test_a_value_of_vanishing_weight_that_is_not_finite(heads, where, bad):
         hit[9 if where == "tail" else slice(0, 32)] = True
         assert np.array_equal(o[:, :g], a[:, :g]) and np.array_equal(o[:, g:, ~hit], a[:, g:, ~hit])
         assert np.array_equal(l, la)
+
+
+# ---------------------------------------------------------------- norms over the whole range of bf16
+
+def normed(x, Hq, w, eps, adjacent=False):
+    """(result, definition, E) of test_gpu_cache.check_rope for q and k of x [T, heads, D] with weights w."""
+    T, heads, D = x.shape
+    pos, freq = torch.arange(T, dtype=torch.int32) * 37, (1e4 ** (-torch.arange(D // 2, dtype=torch.float64) / D)).float()
+    q, k = x.to(DEV).split((Hq, heads - Hq), 1)
+    out = [torch.empty(T, h, D, dtype=torch.bfloat16, device=DEV) for h in (Hq, heads - Hq)]
+    vico.vico_qk_norm_rope(q, k, pos.to(DEV), freq.to(DEV), *out, q_weight=w.to(DEV), k_weight=w.to(DEV), eps=eps,
+                           flags=vico.VICO_ROPE_ADJACENT * adjacent)
+    torch.cuda.synchronize()
+    res = []
+    for y, xs in ((out[0], x[:, :Hq]), (out[1], x[:, Hq:])):
+        n = rope.head_norm(f64(xs), f64(w), eps)
+        pair = (lambda a: a.reshape(*a.shape[:2], -1, 2)) if adjacent else (
+            lambda a: a.reshape(*a.shape[:2], 2, -1).swapaxes(-1, -2))
+        E = np.repeat(np.abs(pair(n)).sum(-1), 2, -1) if adjacent else np.tile(np.abs(pair(n)).sum(-1), 2)
+        res.append((f64(y), rope.rotate(n, pos.numpy()[None], f64(freq), None, adjacent), E))
+    return res
+
+
+@pytest.mark.parametrize("D,adjacent", [(64, False), (128, True)])
+@pytest.mark.parametrize("eps", [0.0, 1e-35, 1e-6, 1e-2, 1e12])
+@pytest.mark.parametrize("size", [1e-38, 1e-25, 1e-16, 1.0, 1e18, 1e19, 1e25, 1e38])
+def test_norm_of_any_size(D, adjacent, eps, size):
+    """Squares that leave fp32 on either side; eps above, beside and below them."""
+    g = gen(31)
+    x = (torch.randn(5, 6, D, generator=g, dtype=torch.float64).clamp(-3, 3) * size).to(torch.bfloat16)
+    w = 1 + 0.3 * torch.randn(D, generator=g)
+    check_rope(normed(x, 4, w, eps, adjacent))
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-6])
+def test_norm_of_unlike_elements(eps):
+    """One element sets the norm, the others are far below it, in heads of every size side by side."""
+    x = normal(gen(32), 8, 6, 128, sigma=1.0)
+    for t in range(8):
+        x[t, :, t] = (-1.0) ** t * 10.0 ** (5 * t)         # 1 .. 1e35
+        x[t, 5] = (x[t, 5].double() * 1e-30).to(torch.bfloat16)
+    check_rope(normed(x, 4, torch.ones(128), eps))
+
+
+def test_norm_of_zeros():
+    x = normal(gen(33), 4, 4, 64)
+    x[1], x[2, 3] = 0, 0
+    (q, _, _), (k, _, _) = normed(x, 2, torch.ones(64), 1e-6)
+    assert np.all(q[1] == 0) and np.all(k[1:3, 1] == 0) and np.all(np.isfinite(k))
+    with np.errstate(invalid="ignore"):
+        (q, ref, _), (k, _, _) = normed(x, 2, torch.ones(64), 0.0)
+    assert np.isnan(q[1]).all() and np.isnan(ref[1]).all() and np.isnan(k[2, 1]).all() and np.isfinite(k[2, 0]).all()

@@ -431,7 +431,12 @@ def _rows_of_heads(name, t):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
 
-def _check_store(store_k, store_v, scale_k, scale_v, heads, head_dim):
+def _check_store(store_k, store_v, scale_k, scale_v, heads, head_dim, optional=False):
+    """The slots of the 4-bit store; optional: 0 for one that is not there."""
+    if optional and store_k is store_v is scale_k is scale_v is None:
+        return 0
+    if any(t is None for t in (store_k, store_v, scale_k, scale_v)):
+        raise ValueError("store_k, store_v, scale_k, scale_v: " + ("all or none" if optional else "all are needed"))
     for n, t in (("store_k", store_k), ("store_v", store_v), ("scale_k", scale_k), ("scale_v", scale_v)):
         _dev_tensor(n, t, torch.uint8, 3)
     R = store_k.shape[0]
@@ -439,6 +444,7 @@ def _check_store(store_k, store_v, scale_k, scale_v, heads, head_dim):
                         ("scale_k", scale_k, head_dim // 32), ("scale_v", scale_v, head_dim // 32)):
         _shape(n, t, (R, heads, width))
     _here(store_k=store_k, store_v=store_v, scale_k=scale_k, scale_v=scale_v)
+    return R
 
 
 def vico_qk_norm_rope(q, k, positions, inv_freq, q_out, k_out, v=None, v_out=None, q_weight=None, k_weight=None,
@@ -553,7 +559,7 @@ def vico_gather_plan_q4(q_len, tail_len, sink_len, store_slots, num_segments, ke
 def vico_gather_attn_q4(q, tail_k, tail_v, sink_k, sink_v, store_k, store_v, scale_k, scale_v, seg_start, seg_len, out,
                         lse=None, workspace=None, keys_hint: int = 0, num_splits: int = 0, softmax_scale: float = 0.0,
                         stream=None) -> None:
-    """vico_gather_attn over a store in 4 bits (vico_gather_attn_q4)."""
+    """vico_gather_attn over a store in 4 bits (vico_gather_attn_q4); its four arrays may be None, as sink and segments may."""
     st = (_calls or _fast()).gather_q4(q, tail_k, tail_v, sink_k, sink_v, store_k, store_v, scale_k, scale_v, seg_start,
                                        seg_len, out, lse, keys_hint, num_splits, softmax_scale, _handle(stream), workspace)
     if st is not None:
@@ -577,7 +583,7 @@ def vico_gather_attn_q4(q, tail_k, tail_v, sink_k, sink_v, store_k, store_v, sca
         _dev_tensor("seg_start", seg_start, torch.int64, 1)
         _dev_tensor("seg_len", seg_len, torch.int32, 1)
         _shape("seg_len", seg_len, seg_start.shape)
-    _check_store(store_k, store_v, scale_k, scale_v, Hkv, D)
+    R = _check_store(store_k, store_v, scale_k, scale_v, Hkv, D, optional=True)
     if not (out.is_cuda and out.is_contiguous() and out.dtype in (torch.bfloat16, torch.float32)):
         raise ValueError("out: expected a contiguous bfloat16 or float32 CUDA tensor")
     _shape("out", out, q.shape)
@@ -592,6 +598,6 @@ def vico_gather_attn_q4(q, tail_k, tail_v, sink_k, sink_v, store_k, store_v, sca
     odt = VICO_DTYPE_F32 if out.dtype == torch.float32 else VICO_DTYPE_BF16
     st = load_library().vico_gather_attn_q4(
         _ptr(q), Lq, _ptr(tail_k), _ptr(tail_v), T, _ptr(sink_k), _ptr(sink_v), S, _ptr(store_k), _ptr(store_v),
-        _ptr(scale_k), _ptr(scale_v), store_k.shape[0], _ptr(seg_start), _ptr(seg_len), n_segs, int(keys_hint), Hq, Hkv, D,
+        _ptr(scale_k), _ptr(scale_v), R, _ptr(seg_start), _ptr(seg_len), n_segs, int(keys_hint), Hq, Hkv, D,
         float(softmax_scale), _ptr(out), odt, _ptr(lse), int(num_splits), _ptr(workspace), wb, _stream(stream))
     _check(st, "vico_gather_attn_q4")

@@ -297,9 +297,11 @@ bool same_shape(const at::Tensor* a, const at::Tensor* b) { return a->sizes() ==
 // the store's arrays: codes of [slots][heads][dim / 2], scales of [slots][heads][dim / 32]
 struct Store {
   const at::Tensor *k, *v, *ks, *vs;
-  explicit Store(Args& in)
-      : k(in.tensor(at::kByte, 3)), v(in.tensor(at::kByte, 3)), ks(in.tensor(at::kByte, 3)), vs(in.tensor(at::kByte, 3)) {}
-  bool fits(int64_t heads, int64_t dim) const {
+  explicit Store(Args& in, bool optional = false)
+      : k(in.tensor(at::kByte, 3, optional)), v(in.tensor(at::kByte, 3, optional)), ks(in.tensor(at::kByte, 3, optional)),
+        vs(in.tensor(at::kByte, 3, optional)) {}
+  bool fits(int64_t heads, int64_t dim) const {      // all four arrays, or none where that is allowed
+    if (!k || !v || !ks || !vs) return !k && !v && !ks && !vs;
     return shape3(k, k->size(0), heads, dim / 2) && same_shape(k, v) && shape3(ks, k->size(0), heads, dim / 32) &&
            same_shape(ks, vs) && here(k, v, ks, vs);
   }
@@ -386,7 +388,7 @@ PyObject* gather_q4(PyObject* const* args, Py_ssize_t n) {
   Args in{args, n};
   const at::Tensor *q = in.tensor(at::kBFloat16, 3), *tk = in.tensor(at::kBFloat16, 3), *tv = in.tensor(at::kBFloat16, 3);
   const at::Tensor *sk = in.tensor(at::kBFloat16, 3, true), *sv = in.tensor(at::kBFloat16, 3, true);
-  const Store s(in);
+  const Store s(in, true);
   const at::Tensor *ss = in.tensor(at::kLong, 1, true), *sl = in.tensor(at::kInt, 1, true);
   const at::Tensor* out = in.output();
   const at::Tensor* lse = in.tensor(at::kFloat, 2, true);

@@ -92,3 +92,33 @@ def test_norm_of_zeros():
     with np.errstate(invalid="ignore"):
         (q, ref, _), (k, _, _) = normed(x, 2, torch.ones(64), 0.0)
     assert np.isnan(q[1]).all() and np.isnan(ref[1]).all() and np.isnan(k[2, 1]).all() and np.isfinite(k[2, 0]).all()
+
+
+# ---------------------------------------------------------------- a stream that has no store yet
+
+@pytest.mark.parametrize("segs", [None, 2])
+@pytest.mark.parametrize("stream", [False, True])
+def test_attention_without_a_store(segs, stream, monkeypatch):
+    """As vico_gather_attn takes it: None, with or without a table; through both paths of the binding."""
+    import paper_2606_19849_amd._binding as binding
+    g = gen(34)
+    q, tk, tv, sk, sv = (normal(g, n, h, 64) for n, h in ((3, 8), (9, 2), (9, 2), (70, 2), (70, 2)))
+    table = (None, None) if segs is None else (torch.tensor([0, 5], device=DEV), torch.tensor([7, 3], dtype=torch.int32, device=DEV))
+    args = tuple(map(f64, (q, tk, tv, sk, sv))) + (np.zeros((0, 2, 64)),) * 2 + ([], [])
+    ref, ref_lse = oracle.gather_attention(*args)
+    dev = [t.to(DEV) for t in (q, tk, tv, sk, sv)]
+
+    class Never:
+        def __getattr__(self, name):
+            return lambda *a: None
+
+    for calls in (binding._fast(), Never()):
+        monkeypatch.setattr(binding, "_calls", calls)
+        out, lse = torch.empty(3, 8, 64, device=DEV), torch.empty(8, 3, device=DEV)
+        torch.cuda.synchronize()
+        vico.vico_gather_attn_q4(*dev, None, None, None, None, *table, out, lse=lse, num_splits=1,
+                                 stream=torch.cuda.Stream() if stream else None)
+        torch.cuda.synchronize()
+        check_f32(f64(out), ref, gather_bound(*args), f64(lse), ref_lse)
+        with pytest.raises(ValueError, match="all or none"):
+            vico.vico_gather_attn_q4(*dev, torch.zeros(4, 2, 32, dtype=torch.uint8, device=DEV), None, None, None, *table, out)

@@ -26,7 +26,10 @@
  *   scale_k, scale_v  [R][num_kv_heads][head_dim / 32] uint8
  * A code's highest bit is the sign, the others select 0, .5, 1, 1.5, 2, 3, 4,
  * 6.  Every 32 elements of a head share a scale byte b: the values are
- * code * 2^(b - 127), or all NaN for b = 255.  Writing a group with largest
+ * code * 2^(b - 127), or all NaN for b = 255.  The calls write b in [4, 252],
+ * and 255.  Other bytes are read as well (an array of zeros reads as zeros):
+ * subnormal values are exact too, and values from 2^128 on (b = 253: 4 and 6;
+ * b = 254: 2 and more) are infinities.  Writing a group with largest
  * magnitude m takes the smallest power of two s with m <= 7 s (the largest
  * element, if it becomes 6 s, is then no further off than half a step), kept
  * in [2^-123, 2^125]; values become x / s to the nearest code, ties to the
@@ -108,7 +111,8 @@ int vico_kv_append_q4(const void* k_chunk, const void* v_chunk, int32_t chunk_le
 
 /*
  * vico_kv_load_q4 -- segments of the 4-bit store as bf16 (exactly: a value has
- * two significant bits), one after the other in table order.
+ * two significant bits; from 2^128 on an infinity), one after the other in
+ * table order.
  *
  *   seg_start, seg_len  the table as for vico_gather_attn: int64 / int32 device
  *                  arrays of num_segments <= 2048 entries, clipped to [0, store_slots)

@@ -6,7 +6,8 @@
 // elements share a power of two 2^(byte - 127), byte 255 makes them all NaN.
 // The matrix cores' own conversion (v_cvt_scalef32_pk_bf16_fp4) turns two
 // codes and their scale into two bf16 values, exactly: a value has two
-// significant bits.
+// significant bits.  The append writes bytes 4 .. 252 and 255; of the others, 0
+// to 3 make exact subnormals, 253 and 254 infinities of values from 2^128 on.
 #pragma once
 
 #include "attn_common.h"

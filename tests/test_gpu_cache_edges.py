@@ -122,3 +122,37 @@ def test_attention_without_a_store(segs, stream, monkeypatch):
         check_f32(f64(out), ref, gather_bound(*args), f64(lse), ref_lse)
         with pytest.raises(ValueError, match="all or none"):
             vico.vico_gather_attn_q4(*dev, torch.zeros(4, 2, 32, dtype=torch.uint8, device=DEV), None, None, None, *table, out)
+
+
+# ---------------------------------------------------------------- scale bytes that the append never writes
+
+def test_load_of_every_scale_byte_and_code():
+    """256 slots, one for each scale byte, all 16 codes in either half of a byte: exact, subnormals too; from 2^128 on an
+    infinity."""
+    codes = torch.arange(16, dtype=torch.uint8).repeat(256, 1, 2)
+    codes = codes | (15 - codes) << 4
+    scales = torch.arange(256, dtype=torch.uint8).view(256, 1, 1).expand(256, 1, 2).contiguous()
+    st = [t.to(DEV) for t in (codes, codes.flip(-1).contiguous(), scales, scales)]
+    out = [torch.empty(256, 1, 64, dtype=torch.bfloat16, device=DEV) for _ in "kv"]
+    vico.vico_kv_load_q4(*st, torch.tensor([0], device=DEV), torch.tensor([256], dtype=torch.int32, device=DEV), *out)
+    torch.cuda.synchronize()
+    for o, want in zip(out, store_values(st)):
+        want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)
+        o = f64(o)
+        assert np.array_equal(o, want, equal_nan=True) and np.array_equal(np.signbit(o[:255]), np.signbit(want[:255]))
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 64), (14, 2, 128)], ids=str)
+def test_attention_over_slots_of_zeros_and_of_subnormal_values(heads):
+    """Slots that nobody has written, in arrays of zeros, are keys and values of zero; bytes 0 to 3 with any codes are as
+    small as makes no difference to the derived bounds."""
+    def tweak(c):
+        for t in c.store:
+            t[20:40] = 0
+        for t in c.store[2:]:
+            t[50:80] = torch.arange(30, dtype=torch.uint8, device=DEV).view(30, 1, 1) % 4
+    c = Case(35, *heads, 3, 9, 4, 100, [0], [95], tweak=tweak)
+    for splits in (0, 1, 3):
+        c.check(splits)
+    c = Case(36, *heads, 300, 310, 4, 100, [0], [95], tweak=tweak)
+    c.check(16)

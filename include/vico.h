@@ -104,7 +104,8 @@ int vico_kv_append(const void* k_chunk, const void* v_chunk, int32_t chunk_len,
  *   out            [chunk_len][num_q_heads][head_dim], out_dtype BF16 (rounded to
  *                  nearest even) or F32
  *   lse_out        NULL or [num_q_heads][chunk_len] fp32: natural-log sum of
- *                  exp(scale * q.k) over the visible keys of each row
+ *                  exp(scale * q.k) over the visible keys of each row (-infinity,
+ *                  with NaN in out, for a row with a NaN or +infinity among them)
  *   num_splits     0: the library picks the schedule; n > 0 splits every row
  *                  tile's key range into n parts (clamped to the number of key
  *                  tiles and to 16); VICO_SPLIT_BALANCED gives every work-group an equal

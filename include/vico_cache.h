@@ -154,7 +154,10 @@ int vico_kv_load_q4(const void* store_k, const void* store_v, const void* scale_
  * Arithmetic: the store's values as bf16 (exact), bf16 MFMA products with fp32
  * accumulation, fp32 online softmax, probabilities rounded to bf16 for the P.V
  * product.  A NaN or an infinity in a tail key or value reaches the rows that
- * see it and no other.
+ * see it, as one or the other and whatever its weight, and no other row.  (An
+ * infinite key whose logit is -infinity has none.)  lse_out is NaN for a row
+ * with a NaN or +infinity among its logits, where vico_gather_attn writes
+ * -infinity: who merges both must take such a row from its output.
  */
 int vico_gather_attn_q4(const void* q, int32_t q_len, const void* tail_k, const void* tail_v, int32_t tail_len,
                         const void* sink_k, const void* sink_v, int32_t sink_len, const void* store_k,

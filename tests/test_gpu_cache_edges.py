@@ -156,3 +156,28 @@ def test_attention_over_slots_of_zeros_and_of_subnormal_values(heads):
         c.check(splits)
     c = Case(36, *heads, 300, 310, 4, 100, [0], [95], tweak=tweak)
     c.check(16)
+
+
+# ---------------------------------------------------------------- the log-sum-exp of a row that is NaN
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("q_len,pad,splits", [(1, 0, 1), (1, 0, 3), (1, 0, 20), (40, 70, 1), (40, 70, 3), (40, 70, 20),
+                                              (300, 0, 1), (300, 0, 16)])
+def test_log_sum_exp_of_nan_rows(q_len, pad, splits, bad):
+    """NaN over the 4-bit store, -inf over the bf16 one, as the headers say; the outputs are NaN in both.  Query heads of
+    the other KV head keep theirs."""
+    q = normal(gen(40), q_len, 8, 64, sigma=1.0).abs().to(DEV)
+    tail = [normal(gen(41 + i), q_len + 3, 2, 64).to(DEV) for i in range(2)]
+    tail[0][0, 1] = bad                                    # a token that every row sees; logits of +inf where bad is
+    seg = torch.zeros(1 + pad, dtype=torch.int64, device=DEV), torch.zeros(1 + pad, dtype=torch.int32, device=DEV)
+    seg[1][0] = 700
+    bf16 = [normal(gen(44 + i), 800, 2, 64).to(DEV) for i in range(2)]
+    q4 = empty_store(800, 2, 64)
+    vico.vico_kv_append_q4(*bf16, *q4, 0)
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+    for call, store, want in ((vico.vico_gather_attn_q4, q4, np.nan), (vico.vico_gather_attn, bf16, -np.inf)):
+        out, lse = torch.empty(q_len, 8, 64, device=DEV), torch.empty(8, q_len, device=DEV)
+        call(q, *tail, None, None, *store, *seg, out, lse=lse, workspace=ws, keys_hint=700, num_splits=splits)
+        torch.cuda.synchronize()
+        assert torch.isnan(out[:, 4:]).all() and torch.isfinite(out[:, :4]).all() and torch.isfinite(lse[:4]).all()
+        assert np.array_equal(f64(lse[4:]), np.full((4, q_len), want), equal_nan=True)

@@ -7,10 +7,10 @@ import torch
 
 import oracle
 import paper_2606_19849_amd as vico
-from oracle import kv4, rope
-from tests._bounds import U8, gather_bound
-from tests._gpu import check_bf16, check_f32
-from tests.test_gpu_cache import DEV, Case, check_rope, empty_store, f64, gen, normal, store_values
+from oracle import rope
+from tests._bounds import gather_bound
+from tests._gpu import check_f32
+from tests.test_gpu_cache import DEV, Case, check_rope, empty_store, f64, gen, normal, rope_case, store_values
 
 pytestmark = pytest.mark.gpu
 
@@ -181,3 +181,33 @@ def test_log_sum_exp_of_nan_rows(q_len, pad, splits, bad):
         torch.cuda.synchronize()
         assert torch.isnan(out[:, 4:]).all() and torch.isfinite(out[:, :4]).all() and torch.isfinite(lse[:4]).all()
         assert np.array_equal(f64(lse[4:]), np.full((4, q_len), want), equal_nan=True)
+
+
+# ---------------------------------------------------------------- strides and rotated widths
+
+def test_rope_of_tokens_far_apart():
+    """Token strides of 2^30 elements: offsets beyond 32 bits, in elements and in bytes."""
+    T, Hq, Hkv, D, stride = 4, 3, 2, 64, 1 << 30
+    buf = torch.empty((T - 1) * stride + (Hq + 2 * Hkv) * D, dtype=torch.bfloat16, device=DEV)
+    x = normal(gen(50), T, Hq + 2 * Hkv, D)
+    rows = buf.as_strided((T, Hq + 2 * Hkv, D), (stride, D, 1))
+    rows.copy_(x)
+    q, k, v = rows.split((Hq, Hkv, Hkv), 1)
+    out = [torch.empty(T, h, D, dtype=torch.bfloat16, device=DEV) for h in (Hq, Hkv, Hkv)]
+    w, pos, freq = torch.ones(D), torch.arange(T, dtype=torch.int32) * 1000, (1e4 ** (-torch.arange(32) / 32.0)).float()
+    vico.vico_qk_norm_rope(q, k, pos.to(DEV), freq.to(DEV), out[0], out[1], v=v, v_out=out[2], q_weight=w.to(DEV))
+    torch.cuda.synchronize()
+    assert torch.equal(out[2].cpu(), x[:, Hq + Hkv:])
+    res = []
+    for y, xs, wi in ((out[0], x[:, :Hq], f64(w)), (out[1], x[:, Hq:Hq + Hkv], None)):
+        n = rope.head_norm(f64(xs), wi, 1e-6)
+        E = np.tile(np.abs(n[..., :32]) + np.abs(n[..., 32:]), 2)
+        res.append((f64(y), rope.rotate(n, pos.numpy()[None], f64(freq)), E))
+    check_rope(res)
+
+
+@pytest.mark.parametrize("D,rot", [(64, 48), (128, 48), (128, 80), (128, 112)])
+@pytest.mark.parametrize("kw", [dict(), dict(adjacent=True), dict(axes=3), dict(axes=3, strided=True)],
+                         ids=lambda k: "-".join(k) or "plain")
+def test_rope_of_other_widths(D, rot, kw):
+    check_rope(rope_case(rot + D, 13, 5, 2, D, rot=rot, **kw))

@@ -20,17 +20,20 @@
 //     bytes of a quad's 4 lanes cover the quad's 8 keys; a DPP step broadcasts
 //     each.
 // Probabilities are rounded to bf16 for the second product, as in the bf16
-// kernels; logits, softmax state and sums are fp32.
+// kernels: its operands are 16-bit, and a second term for the rest would double
+// it.  Each is off by 2^-8 of itself at most, a result by 2^-8 of the weighted mean
+// of |v|: over the norm 2.1e-3 to 2.3e-3 from 64 bits, with the bf16 output's own
+// 1.7e-3, for 1.7e-3 with fp32 ones.  Logits, softmax state and sums are fp32.
 //
-// What bounds it.  A decode step streams the store: 16 waves a CU, one 16-row
+// What bounds it (the kernel alone, medians of a trace).  A decode step streams the store: 16 waves a CU, one 16-row
 // block each, have 16 blocks on the way, and 7B heads over 256 chunks (262k keys,
-// 143 MB) take 34.6 us, loads alone 34.4 (4.6 TB/s between the first load and the
+// 143 MB) take 35.4 us, loads alone 34.4 (4.6 TB/s between the first load and the
 // last).  8 waves with the next block loaded ahead took 39; with the heads of a
 // key range on different XCDs 48: a token's codes are 64 bytes a head, and two
 // heads share a cache line.  Over 32 chunks the launch, the table, a memory latency
-// and the waves' merge are most of its 7.6 us.  Above 16 rows, two row
+// and the waves' merge are most of its 7.9 us.  Above 16 rows, two row
 // blocks a wave use each converted block twice, at 8 waves' registers: 224 rows
-// over 17.8k keys (a 32-token query, 7B heads) 20.7 us, against 30.4 with one row
+// over 17.8k keys (a 32-token query, 7B heads) 21.1 us, against 30.4 with one row
 // block; what bounds those is issue, of conversion and softmax between the matrix
 // products (the matrix cores are busy for 18 % of the cycles), and the start.
 //

@@ -24,8 +24,8 @@
 //     value whatever its weight.
 // It is bound by the matrix cores, as the chunk prefill is, and by what goes
 // between their instructions.  1024 tokens over 8192 store keys, 7B heads, 128.7
-// GFLOP: 140 us a call, 920 TFLOP/s, with the merge of its two parts (7 us).  173
-// with all of the conversion and the loads between two barriers, 156 in the slots;
+// GFLOP: 140 to 145 us a call by the box, 885 to 920 TFLOP/s, with the merge of its
+// two parts (7 us).  173 with all of the conversion and the loads between two barriers, 156 in the slots;
 // a copy for timing that does neither took 149 us traced for 166.  Equal shares of
 // the tiles for every CU (224 work-groups leave 32 idle) took 146.6 for 145: a row
 // tile's keys then come in more parts.

@@ -62,7 +62,9 @@ constexpr int64_t kTileMinRows = 128;                     // fewer packed rows o
 // Rows against 256-row kernel, each at its best, us: 7B heads, 224 rows, 2048 /
 // 20000 keys 13 / 21 and 23 / 34; 700 rows, 8192 / 20000 keys 32 / 36 and 62 / 50;
 // 1050 rows, 2048 / 8192 keys 20 / 31 and 51 / 41; 3B heads, 1600 rows, 8192 / 20000
-// keys 32 / 38 and 62 / 53; small heads, 1024 rows, 20000 keys 26 / 32.
+// keys 32 / 38 and 62 / 53; small heads, 1024 rows, 20000 keys 26 / 32.  Both are
+// far from a matrix product's rate there (8.5 us of work for 700 rows over 8192 keys): the
+// rows kernel converts the codes for every 32 rows, the other has few row tiles.
 struct Q4Plan {
   int tile, row_blocks, n_rt, parts;
   int64_t cost;

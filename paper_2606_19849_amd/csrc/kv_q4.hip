@@ -14,8 +14,9 @@
 // Both kernels move bytes, 2.53 a value, and are bound by memory or, for one
 // chunk, by the launch.  A thread takes units of 8 elements: 16 bytes on the bf16
 // side, 4 of codes; four lanes share a group (amax and the scale byte by two DPP
-// steps).  7B heads, traced: append of 2048 tokens (5.3 MB) 3.5 us, of 77 tokens (3B
-// heads) 2.6; load of 32 chunks, 17.6k rows (45.5 MB), 8.4 us, 5.4 TB/s.
+// steps).  7B heads, medians of a trace: append of 2048 tokens (5.3 MB) 3.5 us, of 77
+// tokens (3B heads) 2.6; load of 32 chunks, 17.6k rows (45.5 MB), 8.4 to 9.4 us by the
+// box, 4.9 to 5.4 TB/s.
 
 #include <algorithm>
 

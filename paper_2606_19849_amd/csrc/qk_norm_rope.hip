@@ -13,14 +13,15 @@
 // The operator moves four bytes for every element and computes little, so it
 // is bound by memory and, for few tokens, by the launch -- as long as a
 // token's angles are not computed for each of its heads: fp64 products, sines
-// and cosines of 64 pairs for 32 heads each took 16 us of a 2048-token chunk (7B
-// heads).  A work-group takes one token, computes its sines and cosines once, one
+// and cosines of 64 pairs for 32 heads each took 16.4 us a call for a 2048-token
+// chunk (7B heads, 38 MB), computed once 10.7 (traced kernel: median 11.1 to 11.4,
+// least 10.0).  A work-group takes one token, computes its sines and cosines once, one
 // pair a thread, into LDS, and its heads, q, k and v alike, D/16 lanes a head; a
 // lane holds 8 pairs (two 16-byte units), loaded before the angles are ready.
-// Two or four tokens a work-group leave fewer loads in flight at a time: 9.4 and
-// 11.6 us for 9.0 on that chunk.  The next head is loaded after this one's
-// stores: loaded before its arithmetic it costs registers, and waves (78 for 73,
-// 0.2 us more).
+// The next head is loaded after this one's stores: loaded before its arithmetic it
+// costs registers, and waves (0.2 us more).  That chunk again and again in a
+// graph, the same inputs / eight in turn: 9.8 / 12.9 us; two tokens a work-group,
+// as a variant of this kernel, 9.1 / 12.2, four 10.2 / 13.8.
 
 #include "attn_common.h"
 

@@ -9,9 +9,11 @@ chunks) and attention of short queries or decode steps over the retrieved
 chunks complete the query path; temporal token dropping thins each chunk's
 tokens before they reach the LLM.  Head norms with the position rotation make
 the attention's inputs from the projection, and a store of keys and values in 4
-bits serves the query path of long streams.  All arithmetic runs in the
-hand-written HIP kernels of libvico.so (C ABI in include/vico.h and
-include/vico_cache.h); this package only marshals arguments.
+bits serves the query path of long streams.  Many streams, and the questions
+that branch off them, share one pool of pages with attention over it.  All
+arithmetic runs in the hand-written HIP kernels of libvico.so (C ABI in
+include/vico.h, vico_cache.h and vico_pages.h); this package only marshals
+arguments.
 """
 from ._binding import (
     VICO_DTYPE_BF16,
@@ -44,6 +46,15 @@ from ._binding import (
     vico_kv_load_q4,
     vico_gather_plan_q4,
     vico_gather_attn_q4,
+    vico_paged_append,
+    vico_paged_attn,
+    vico_paged_attn_plan,
+    vico_pages_fork,
+    vico_pages_free,
+    vico_pages_reserve,
+    vico_pages_compact,
+    vico_pages_workspace_bytes,
+    vico_pages_copy,
 )
 
 __all__ = [
@@ -77,4 +88,13 @@ __all__ = [
     "vico_kv_load_q4",
     "vico_gather_plan_q4",
     "vico_gather_attn_q4",
+    "vico_paged_append",
+    "vico_paged_attn",
+    "vico_paged_attn_plan",
+    "vico_pages_fork",
+    "vico_pages_free",
+    "vico_pages_reserve",
+    "vico_pages_compact",
+    "vico_pages_workspace_bytes",
+    "vico_pages_copy",
 ]

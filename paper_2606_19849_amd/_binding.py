@@ -1,4 +1,4 @@
-"""Binding of libvico (include/vico.h, include/vico_cache.h): argument marshalling only.
+"""Binding of libvico (include/vico.h, vico_cache.h, vico_pages.h): argument marshalling only.
 
 Calls with plain arguments go through _vico_call (csrc/py_call.cpp), which
 checks and passes them in C++; it answers None for anything else, and the
@@ -68,6 +68,17 @@ _SIGNATURES = {
                                    _i64, _i32, _i32, _i32, _f32, _vp, _i32, _vp, _i32, _vp, _i64, _vp]),
     "vico_status_str": (ctypes.c_char_p, [_i32]),
     "vico_last_hip_error": (_i32, []),
+    "vico_paged_append": (_i32, [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _i32, _i32, _vp]),
+    "vico_paged_attn": (_i32, [_vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _i32, _i64, _i64,
+                               _i32, _i32, _i32, _f32, _i32, _vp, _i32, _vp, _i32, _vp, _i64, _vp]),
+    "vico_paged_attn_plan": (_i32, [_i32, _i32, _i32, _i32, _i32, _i32, _i64, _i64, _i32, _i32, _i32, _i32,
+                                    ctypes.POINTER(_i32), ctypes.POINTER(_i64)]),
+    "vico_pages_fork": (_i32, [_vp, _i32, _i32, _vp, _i32, _i32, _vp, _vp, _vp]),
+    "vico_pages_free": (_i32, [_vp, _i32, _i32, _vp, _i32, _i32, _vp, _vp, _vp]),
+    "vico_pages_reserve": (_i32, [_vp, _i32, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "vico_pages_compact": (_i32, [_vp, _i32, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _i64, _vp]),
+    "vico_pages_workspace_bytes": (_i64, [_i32, _i32]),
+    "vico_pages_copy": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _i32, _vp, _vp]),
 }
 
 CALL_PATH = os.path.join(PKG, "_vico_call.so")
@@ -410,7 +421,7 @@ def vico_temporal_drop(frames, tau: float, keep, out_index, out_count, sim=None,
 # ---------------------------------------------------------------- include/vico_cache.h
 
 def _here(**tensors):
-    """The calls of vico_cache.h run on the current device: tensors of another one are refused."""
+    """The calls of vico_cache.h and vico_pages.h run on the current device: tensors of another one are refused."""
     current = torch.cuda.current_device()
     for n, t in tensors.items():
         if t is not None and t.device.index != current:
@@ -601,3 +612,202 @@ def vico_gather_attn_q4(q, tail_k, tail_v, sink_k, sink_v, store_k, store_v, sca
         _ptr(scale_k), _ptr(scale_v), R, _ptr(seg_start), _ptr(seg_len), n_segs, int(keys_hint), Hq, Hkv, D,
         float(softmax_scale), _ptr(out), odt, _ptr(lse), int(num_splits), _ptr(workspace), wb, _stream(stream))
     _check(st, "vico_gather_attn_q4")
+
+
+# ---------------------------------------------------------------- include/vico_pages.h
+
+def _check_ints(**tensors):
+    """int32 device arrays of one dimension: (tensor, entries)."""
+    for n, (t, want) in tensors.items():
+        _dev_tensor(n, t, torch.int32, 1)
+        _shape(n, t, (want,))
+
+
+def _check_pools(k_pages, v_pages, ndim=4):
+    for n, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+        _dev_tensor(n, t, torch.bfloat16, ndim)
+    _shape("v_pages", v_pages, k_pages.shape)
+
+
+def _check_table(page_table, page_refs):
+    """Rows and entries of a row of the page table, pages of the pool."""
+    _dev_tensor("page_table", page_table, torch.int32, 2)
+    _dev_tensor("page_refs", page_refs, torch.int32, 1)
+    _here(page_table=page_table, page_refs=page_refs)
+    return page_table.shape[0], page_table.shape[1], page_refs.shape[0]
+
+
+def _memory(workspace):
+    if workspace is None:
+        return 0
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor")
+    _here(workspace=workspace)
+    return workspace.numel() * workspace.element_size()
+
+
+def vico_paged_append(k, v, q_start, seq_len, k_pages, v_pages, page_table, stream=None) -> None:
+    """Every sequence's new tokens into its pages (vico_paged_append).
+
+    k, v bf16 [total, Hkv, D]; q_start int32 [num_seqs + 1], seq_len int32 [num_seqs]; k_pages, v_pages bf16
+    [num_pages, page_size, Hkv, D]; page_table int32 [num_seqs, max_pages]."""
+    st = (_calls or _fast()).paged_append(k, v, q_start, seq_len, k_pages, v_pages, page_table, _handle(stream))
+    if st is not None:
+        return _check(st, "vico_paged_append")
+    _dev_bf16("k", k)
+    _dev_bf16("v", v)
+    _shape("v", v, k.shape)
+    _check_pools(k_pages, v_pages)
+    total, Hkv, D = k.shape
+    N, P = k_pages.shape[:2]
+    _shape("k_pages", k_pages, (N, P, Hkv, D))
+    _dev_tensor("page_table", page_table, torch.int32, 2)
+    B, width = page_table.shape
+    _check_ints(q_start=(q_start, B + 1), seq_len=(seq_len, B))
+    _here(k=k, v=v, q_start=q_start, seq_len=seq_len, k_pages=k_pages, v_pages=v_pages, page_table=page_table)
+    st = load_library().vico_paged_append(_ptr(k), _ptr(v), total, _ptr(q_start), _ptr(seq_len), B, _ptr(k_pages),
+                                          _ptr(v_pages), N, P, _ptr(page_table), width, Hkv, D, _stream(stream))
+    _check(st, "vico_paged_append")
+
+
+def vico_paged_attn_plan(num_seqs, total_q, max_q_len, page_size, max_pages, sink_len, window, keys_hint, num_q_heads,
+                         num_kv_heads, head_dim, num_splits=0):
+    """(most parts, workspace_bytes) of vico_paged_attn for these arguments."""
+    ns, wb = _i32(0), _i64(0)
+    st = load_library().vico_paged_attn_plan(num_seqs, total_q, max_q_len, page_size, max_pages, sink_len, int(window),
+                                             int(keys_hint), num_q_heads, num_kv_heads, head_dim, num_splits,
+                                             ctypes.byref(ns), ctypes.byref(wb))
+    _check(st, "vico_paged_attn_plan")
+    return ns.value, wb.value
+
+
+def vico_paged_attn(q, q_start, seq_len, k_pages, v_pages, page_table, out, lse=None, sink_len: int = 0,
+                    window: int = VICO_FULL_HISTORY, max_q_len=None, keys_hint: int = 0, num_splits: int = 0,
+                    softmax_scale: float = 0.0, flags: int = 0, workspace=None, stream=None) -> None:
+    """Attention of every sequence's new tokens over its pages (vico_paged_attn); writes `out` (and `lse`).
+
+    q bf16 [total, Hq, D], the other tensors as for vico_paged_append; max_q_len: at least the new tokens of any one
+    sequence (None: all of q's rows)."""
+    st = (_calls or _fast()).paged_attn(q, q_start, seq_len, k_pages, v_pages, page_table, out, lse, sink_len, window,
+                                        q.shape[0] if max_q_len is None else max_q_len, keys_hint, num_splits,
+                                        softmax_scale, flags, workspace, _handle(stream))
+    if st is not None:
+        return _check(st, "vico_paged_attn")
+    _dev_bf16("q", q)
+    _check_pools(k_pages, v_pages)
+    total, Hq, D = q.shape
+    N, P, Hkv = k_pages.shape[:3]
+    _shape("k_pages", k_pages, (N, P, Hkv, D))
+    _dev_tensor("page_table", page_table, torch.int32, 2)
+    B, width = page_table.shape
+    _check_ints(q_start=(q_start, B + 1), seq_len=(seq_len, B))
+    if not (out.is_cuda and out.is_contiguous() and out.dtype in (torch.bfloat16, torch.float32)):
+        raise ValueError("out: expected a contiguous bfloat16 or float32 CUDA tensor")
+    _shape("out", out, q.shape)
+    if lse is not None:
+        _dev_tensor("lse", lse, torch.float32, 2)
+        _shape("lse", lse, (Hq, total))
+    _here(q=q, q_start=q_start, seq_len=seq_len, k_pages=k_pages, v_pages=v_pages, page_table=page_table, out=out, lse=lse)
+    wb = _memory(workspace)
+    odt = VICO_DTYPE_F32 if out.dtype == torch.float32 else VICO_DTYPE_BF16
+    st = load_library().vico_paged_attn(
+        _ptr(q), _ptr(q_start), _ptr(seq_len), B, total, total if max_q_len is None else int(max_q_len), _ptr(k_pages),
+        _ptr(v_pages), N, P, _ptr(page_table), width, int(sink_len), int(window), int(keys_hint), Hq, Hkv, D,
+        float(softmax_scale), int(flags), _ptr(out), odt, _ptr(lse), int(num_splits), _ptr(workspace), wb, _stream(stream))
+    _check(st, "vico_paged_attn")
+
+
+def vico_pages_fork(page_table, page_refs, seq_len, parent, page_size: int, stream=None) -> None:
+    """Row b of the page table becomes a branch of row parent[b], or empty for -1 (vico_pages_fork).
+
+    page_table int32 [num_seqs, max_pages], page_refs int32 [num_pages], seq_len and parent int32 [num_seqs]."""
+    st = (_calls or _fast()).pages_fork(page_table, page_refs, seq_len, parent, page_size, _handle(stream))
+    if st is not None:
+        return _check(st, "vico_pages_fork")
+    B, width, N = _check_table(page_table, page_refs)
+    _check_ints(seq_len=(seq_len, B), parent=(parent, B))
+    _here(seq_len=seq_len, parent=parent)
+    st = load_library().vico_pages_fork(_ptr(page_table), B, width, _ptr(page_refs), N, int(page_size), _ptr(seq_len),
+                                        _ptr(parent), _stream(stream))
+    _check(st, "vico_pages_fork")
+
+
+def vico_pages_free(page_table, page_refs, first, last, page_size: int, stream=None) -> None:
+    """Pages wholly in positions [first[b], last[b]) of row b are given back (vico_pages_free)."""
+    st = (_calls or _fast()).pages_free(page_table, page_refs, first, last, page_size, _handle(stream))
+    if st is not None:
+        return _check(st, "vico_pages_free")
+    B, width, N = _check_table(page_table, page_refs)
+    _check_ints(first=(first, B), last=(last, B))
+    _here(first=first, last=last)
+    st = load_library().vico_pages_free(_ptr(page_table), B, width, _ptr(page_refs), N, int(page_size), _ptr(first),
+                                        _ptr(last), _stream(stream))
+    _check(st, "vico_pages_free")
+
+
+def vico_pages_workspace_bytes(num_seqs: int, num_pages: int) -> int:
+    """Workspace bytes of vico_pages_reserve and vico_pages_compact."""
+    b = load_library().vico_pages_workspace_bytes(num_seqs, num_pages)
+    if b < 0:
+        raise VicoError(int(b), "vico_pages_workspace_bytes")
+    return int(b)
+
+
+def vico_pages_reserve(page_table, page_refs, seq_len, q_start, page_size: int, moves, granted, workspace,
+                       stream=None) -> None:
+    """Pages of its own for every sequence's new tokens (vico_pages_reserve).
+
+    moves int32 [num_seqs, 2] and granted int32 [num_seqs] are written; workspace: vico_pages_workspace_bytes bytes."""
+    st = (_calls or _fast()).pages_reserve(page_table, page_refs, seq_len, q_start, page_size, moves, granted, workspace,
+                                           _handle(stream))
+    if st is not None:
+        return _check(st, "vico_pages_reserve")
+    B, width, N = _check_table(page_table, page_refs)
+    _check_ints(seq_len=(seq_len, B), q_start=(q_start, B + 1), granted=(granted, B))
+    _dev_tensor("moves", moves, torch.int32, 2)
+    _shape("moves", moves, (B, 2))
+    _here(seq_len=seq_len, q_start=q_start, granted=granted, moves=moves)
+    wb = _memory(workspace)
+    st = load_library().vico_pages_reserve(_ptr(page_table), B, width, _ptr(page_refs), N, int(page_size), _ptr(seq_len),
+                                           _ptr(q_start), _ptr(moves), _ptr(granted), _ptr(workspace), wb, _stream(stream))
+    _check(st, "vico_pages_reserve")
+
+
+def vico_pages_compact(page_table, page_refs, moves, count, workspace, stream=None) -> None:
+    """The pages in use to the pool's low end (vico_pages_compact).
+
+    moves int32 [at least num_pages / 2, 2] and count int32 [1] are written; workspace as for vico_pages_reserve."""
+    st = (_calls or _fast()).pages_compact(page_table, page_refs, moves, count, workspace, _handle(stream))
+    if st is not None:
+        return _check(st, "vico_pages_compact")
+    B, width, N = _check_table(page_table, page_refs)
+    _dev_tensor("moves", moves, torch.int32, 2)
+    _shape("moves", moves, (moves.shape[0], 2))
+    _check_ints(count=(count, 1))
+    _here(moves=moves, count=count)
+    wb = _memory(workspace)
+    st = load_library().vico_pages_compact(_ptr(page_table), B, width, _ptr(page_refs), N, _ptr(moves), moves.shape[0],
+                                           _ptr(count), _ptr(workspace), wb, _stream(stream))
+    _check(st, "vico_pages_compact")
+
+
+def vico_pages_copy(k_pages, v_pages, moves, count=None, stream=None) -> None:
+    """Page moves[i][0] to page moves[i][1] in every layer (vico_pages_copy).
+
+    k_pages, v_pages bf16 [num_pages, page_size, Hkv, D], with the layers as a first dimension where there are several."""
+    st = (_calls or _fast()).pages_copy(k_pages, v_pages, moves, count, _handle(stream))
+    if st is not None:
+        return _check(st, "vico_pages_copy")
+    if k_pages.dim() not in (4, 5):
+        raise ValueError("k_pages: expected 4 or 5 dimensions")
+    _check_pools(k_pages, v_pages, k_pages.dim())
+    _dev_tensor("moves", moves, torch.int32, 2)
+    _shape("moves", moves, (moves.shape[0], 2))
+    if count is not None:
+        _check_ints(count=(count, 1))
+    _here(k_pages=k_pages, v_pages=v_pages, moves=moves, count=count)
+    L = k_pages.shape[0] if k_pages.dim() == 5 else 1
+    N, P, Hkv, D = k_pages.shape[-4:]
+    st = load_library().vico_pages_copy(_ptr(k_pages), _ptr(v_pages), L, N, P, Hkv, D, _ptr(moves), moves.shape[0],
+                                        _ptr(count), _stream(stream))
+    _check(st, "vico_pages_copy")

@@ -1,0 +1,150 @@
+// The cache in pages (include/vico_pages.h): arguments and device helpers that
+// its kernels share.
+#pragma once
+
+#include "vico_internal.h"
+
+namespace vico {
+
+constexpr int kMaxPages = 1 << 21;
+constexpr int kMaxSeqs = 4096;
+constexpr int kMaxMoves = 1 << 24;
+constexpr int kPageBlock = 512;                       // pages that one count covers: eight words of 64 flags
+constexpr int kMaxPageBlocks = kMaxPages / kPageBlock;
+
+// ---- tables
+struct PagesArgs {
+  int32_t* table;           // [B][width]
+  int32_t* refs;            // [N]
+  int32_t* seq_len;         // [B]
+  const int32_t* parent;    // fork
+  const int32_t* first;     // free
+  const int32_t* last;
+  const int32_t* q_start;   // reserve
+  int32_t* moves;           // reserve, compact
+  int32_t* granted;         // reserve
+  int32_t* count;           // compact
+  uint64_t* flags;          // workspace: a bit for each page; reserve: free, compact: in use
+  uint64_t* flags1;         // workspace: pages held once (reserve)
+  int32_t* blocks;          // workspace: flags counted, kPageBlock pages each
+  int32_t* need;            // workspace: pages that each row wants (reserve)
+  int B, width, N, n_blocks, page_shift, max_moves;
+};
+hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_free(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t stream);
+
+// ---- contents
+struct PagesCopyArgs {
+  uint16_t* k;              // [layers][N][page_units * 8 elements]
+  uint16_t* v;
+  const int32_t* moves;     // [n_moves][2]
+  const int32_t* count;     // may be null
+  int n_moves, layers, N;
+  int page_units;           // 16-byte units of a page
+  int pieces;               // pieces that a page is copied in: set by the launch
+};
+hipError_t launch_pages_copy(const PagesCopyArgs& a, hipStream_t stream);
+
+struct PagedAppendArgs {
+  const uint16_t* k;        // [total][row_units * 8 elements]
+  const uint16_t* v;
+  uint16_t* k_pages;
+  uint16_t* v_pages;
+  const int32_t* q_start;
+  const int32_t* seq_len;
+  const int32_t* table;
+  int B, total, N, width, page_shift;
+  int row_units;            // 16-byte units of a token's row
+  FastDiv by_units;
+  int per_wave;             // tokens of a wave: set by the launch
+};
+hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream);
+
+// ---- attention
+constexpr int kPagedParts = 64;       // most key-range parts of a row tile (rows kernel)
+constexpr int kPagedTileParts = 16;   // and of a 256-row tile
+struct PagedAttnArgs {
+  const uint16_t* q;
+  const int32_t* q_start;
+  const int32_t* seq_len;
+  const uint16_t* k_pages;
+  const uint16_t* v_pages;
+  const int32_t* table;
+  void* out;
+  float* lse;               // may be null
+  float* ws_o;              // partial results of row tiles: [slot][rows][D] fp32, and their log2-sum-exps [slot][rows]
+  float* ws_lse;
+  int B, total, max_q, N, width, page_shift;
+  int S;
+  int64_t W;                // < 0: the whole history
+  int Hq, Hkv, D;
+  int bidir, out_f32;
+  float scale_log2;
+  int rows_most;            // packed rows of a sequence up to which the rows kernel takes it
+  int n_rt, row_blocks;     // rows kernel: row tiles of 16 * row_blocks rows of a sequence
+  int parts, per_part;      // rows kernel: parts at most, 32-key blocks of a part at least
+  int tile_slots;           // 256-row kernel: work-groups that share the key ranges
+  int tile_splits;          // its parts: 0: those that fill the slots
+  FastDiv by_g, by_rt, by_parts, by_kv;
+};
+hipError_t launch_paged_rows(const PagedAttnArgs& a, hipStream_t stream);
+hipError_t launch_paged_tile(const PagedAttnArgs& a, hipStream_t stream);
+
+// What a sequence's rows are and see.  Numbers from device memory are brought
+// into range here: whatever the arrays hold, rows lie in [0, total) and positions in
+// [0, width * page_size).
+struct Sequence {
+  int q0, n;                // its first row, its rows
+  int H;                    // tokens before them
+  int sink, first;          // visible before the new tokens: [0, sink) and [first, H), sink <= first
+};
+template <class A>
+__device__ __forceinline__ int rows_of(const A& a, int b, int& q0) {
+  q0 = min(max(a.q_start[b], 0), a.total);
+  return min(max(a.q_start[b + 1], q0), a.total) - q0;
+}
+__device__ __forceinline__ Sequence sequence(const PagedAttnArgs& a, int b) {
+  Sequence s;
+  s.n = min(rows_of(a, b, s.q0), a.max_q);
+  s.H = min(max(a.seq_len[b], 0), a.width << a.page_shift);
+  s.first = a.W < 0 || a.W >= s.H ? 0 : s.H - (int)a.W;
+  s.sink = min(a.S, s.first);
+  return s;
+}
+// A row's last position: token t of the sequence's chunk.
+__device__ __forceinline__ int last_position(const PagedAttnArgs& a, const Sequence& s, int t) {
+  return min(s.H + (a.bidir ? s.n - 1 : t), (a.width << a.page_shift) - 1);
+}
+// Blocks of BN positions (a power of two): those of the sink, then those from the window on; the first block after the
+// sink's, and how many there are up to position `last`.
+template <int BN>
+struct KeyBlocks {
+  int of_sink, from;
+  __device__ __forceinline__ explicit KeyBlocks(const Sequence& s)
+      : of_sink((s.sink + BN - 1) / BN), from(max(s.first / BN, (s.sink + BN - 1) / BN)) {}
+  __device__ __forceinline__ int upto(int last) const { return max(last / BN + 1 - from, 0) + of_sink; }
+  __device__ __forceinline__ int position(int i) const { return (i < of_sink ? i : i - of_sink + from) * BN; }
+};
+// Parts of a sequence's key range on the rows kernel, and 32-key blocks of one.
+__device__ __forceinline__ int parts_of(const PagedAttnArgs& a, int blocks, int& per) {
+  per = max(a.per_part, a.by_parts(blocks + a.parts - 1));
+  return max((blocks + per - 1) / per, 1);
+}
+
+// The sequence that row t of the calls' tensors belongs to (every lane of a wave
+// asks for the same t), B where none does: the number of entries q_start[1 .. B]
+// that are <= t, 64 at a time.
+__device__ __forceinline__ int sequence_of(const int32_t* q_start, int B, int t, int lane) {
+  int lo = 0, step = 1;
+  while (step * 64 < B) step *= 64;
+  for (; step > 0; step /= 64) {
+    const int i = lo + (lane + 1) * step;
+    const bool passed = i <= B && q_start[i] <= t;
+    lo += step * __builtin_popcountll(__builtin_amdgcn_ballot_w64(passed));
+  }
+  return lo;
+}
+
+}  // namespace vico

@@ -1,0 +1,317 @@
+// Host side of include/vico_pages.h: argument validation, launch planning and
+// error mapping, as vico_api.hip does it for vico.h.
+
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "vico_pages.h"
+#include "pages.h"
+#include "host_util.h"
+
+using namespace vico;
+
+namespace {
+
+struct Region {
+  const void* p;
+  int64_t bytes;
+};
+
+// Whether a written region meets any other region, written or read.
+template <int NW, int NR>
+bool collide(const Region (&w)[NW], const Region (&r)[NR]) {
+  for (int i = 0; i < NW; ++i) {
+    if (!w[i].p) continue;
+    for (int k = 0; k < NR; ++k)
+      if (r[k].p && overlaps(w[i].p, w[i].bytes, r[k].p, r[k].bytes)) return true;
+    for (int k = i + 1; k < NW; ++k)
+      if (w[k].p && overlaps(w[i].p, w[i].bytes, w[k].p, w[k].bytes)) return true;
+  }
+  return false;
+}
+
+bool heads_ok(int32_t Hq, int32_t Hkv) { return Hq >= 1 && Hkv >= 1 && Hq <= kMaxHeads && Hkv <= kMaxHeads; }
+
+// The table's sizes; page_size 0: the call has none.
+bool table_ok(int32_t B, int32_t width, int32_t N, int32_t page_size) {
+  if (B < 0 || B > kMaxSeqs || width < 0 || N < 0 || N > kMaxPages) return false;
+  if (int64_t(B) * width > kMaxKeys || width > kMaxKeys / 16) return false;
+  if (page_size == 0) return true;
+  return page_size >= 16 && page_size <= 1024 && (page_size & (page_size - 1)) == 0 && int64_t(width) * page_size <= kMaxKeys;
+}
+int shift_of(int32_t page_size) { return __builtin_ctz((unsigned)page_size); }
+int64_t pool_bytes(int64_t N, int64_t page_size, int64_t Hkv, int64_t D) { return N * page_size * Hkv * D * 2; }
+
+int status_of(hipError_t e) { return e == hipSuccess ? VICO_OK : record_hip_failure(e); }
+
+int page_blocks(int32_t N) { return (N + kPageBlock - 1) / kPageBlock; }
+int64_t table_workspace(int32_t B, int32_t N) {
+  const int64_t words = int64_t(page_blocks(N)) * (kPageBlock / 64);
+  return 2 * align256(words * 8) + align256(int64_t(page_blocks(N)) * 4) + align256(int64_t(B) * 4);
+}
+void use_workspace(PagesArgs* a, void* workspace) {
+  const int64_t words = int64_t(a->n_blocks) * (kPageBlock / 64);
+  char* p = (char*)workspace;
+  a->flags = (uint64_t*)p;
+  p += align256(words * 8);
+  a->flags1 = (uint64_t*)p;
+  p += align256(words * 8);
+  a->blocks = (int32_t*)p;
+  p += align256(int64_t(a->n_blocks) * 4);
+  a->need = (int32_t*)p;
+}
+
+// ---- attention: which sequences take which kernel, and how their keys are split.
+constexpr int kPagedRowsMost = 1 << 30;
+
+struct PagedPlan {
+  int rows_most, n_rt, row_blocks, parts, per_part;
+  bool rows, tile;
+  int64_t rows_ws, ws_bytes;
+};
+
+int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size, int32_t width, int32_t S, int64_t W,
+                      int64_t hint, int32_t Hq, int32_t Hkv, int32_t D, int32_t splits, PagedPlan* pl) {
+  if (total < 0 || max_q < 0 || S < 0 || W < VICO_FULL_HISTORY || hint < 0 || splits < 0) return VICO_ERR_INVALID_ARG;
+  if (!heads_ok(Hq, Hkv) || Hq % Hkv != 0) return VICO_ERR_INVALID_ARG;
+  if (D != 64 && D != 128) return VICO_ERR_UNSUPPORTED;
+  if (page_size == 0 || !table_ok(B, width, 0, page_size)) return VICO_ERR_INVALID_ARG;
+  if (total > kMaxChunk || int64_t(total) * Hq * D * 4 >= kMaxTensorBytes) return VICO_ERR_INVALID_ARG;
+  *pl = PagedPlan{};
+  const int n = std::min(max_q, total), g = Hq / Hkv;
+  if (n == 0 || B == 0) return VICO_OK;
+  const int64_t cap = int64_t(width) * page_size, rows = int64_t(g) * n;
+  int64_t keys = std::min(hint > 0 ? hint : cap, cap);
+  if (W != VICO_FULL_HISTORY) keys = std::min(keys, S + W + n);
+  pl->rows_most = kPagedRowsMost;
+  pl->rows = true;
+  const int64_t few = std::min<int64_t>(rows, pl->rows_most);
+  pl->row_blocks = few > 16 ? 2 : 1;
+  pl->n_rt = (int)((few + 16 * pl->row_blocks - 1) / (16 * pl->row_blocks));
+  const int64_t groups = int64_t(B) * Hkv * pl->n_rt, blocks = keys / kRowsBlock + 1;
+  const int64_t target = (B == 1 ? 2 : 4) * kNumCUs;
+  pl->parts = splits > 0 ? std::min(splits, kPagedParts)
+                         : (int)std::max<int64_t>(std::min(std::min<int64_t>(kPagedParts, target / groups), blocks / 8), 1);
+  if (groups * pl->parts > kMaxKeys) return VICO_ERR_INVALID_ARG;
+  pl->per_part = splits > 0 ? 1 : (int)((blocks + pl->parts - 1) / pl->parts);
+  if (pl->parts > 1) pl->rows_ws = align256(groups * pl->parts * 16 * pl->row_blocks * D * 4) + align256(groups * pl->parts * 16 * pl->row_blocks * 4);
+  pl->ws_bytes = pl->rows_ws;
+  return VICO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int vico_paged_append(const void* k, const void* v, int32_t total_tokens, const int32_t* q_start,
+                      const int32_t* seq_len, int32_t num_seqs, void* k_pages, void* v_pages, int32_t num_pages,
+                      int32_t page_size, const int32_t* page_table, int32_t max_pages, int32_t num_kv_heads,
+                      int32_t head_dim, void* stream) {
+  if (total_tokens < 0 || total_tokens > kMaxChunk || !heads_ok(num_kv_heads, num_kv_heads)) return VICO_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return VICO_ERR_UNSUPPORTED;
+  if (page_size == 0 || !table_ok(num_seqs, max_pages, num_pages, page_size)) return VICO_ERR_INVALID_ARG;
+  const int64_t row = int64_t(num_kv_heads) * head_dim * 2, bytes = row * total_tokens;
+  if (bytes >= kMaxTensorBytes) return VICO_ERR_INVALID_ARG;
+  if (total_tokens == 0 || num_seqs == 0 || max_pages == 0 || num_pages == 0) return VICO_OK;
+  if (!k || !v || !q_start || !seq_len || !k_pages || !v_pages || !page_table) return VICO_ERR_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned_to(q_start, 4) ||
+      !aligned_to(seq_len, 4) || !aligned_to(page_table, 4))
+    return VICO_ERR_MISALIGNED;
+  const int64_t pool = pool_bytes(num_pages, page_size, num_kv_heads, head_dim);
+  const Region w[] = {{k_pages, pool}, {v_pages, pool}};
+  const Region r[] = {{k, bytes}, {v, bytes}, {q_start, int64_t(num_seqs + 1) * 4}, {seq_len, int64_t(num_seqs) * 4},
+                      {page_table, int64_t(num_seqs) * max_pages * 4}};
+  if (collide(w, r)) return VICO_ERR_INVALID_ARG;
+  PagedAppendArgs a{};
+  a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
+  a.k_pages = (uint16_t*)k_pages; a.v_pages = (uint16_t*)v_pages;
+  a.q_start = q_start; a.seq_len = seq_len; a.table = page_table;
+  a.B = num_seqs; a.total = total_tokens; a.N = num_pages; a.width = max_pages; a.page_shift = shift_of(page_size);
+  a.row_units = (int)(row / 16);
+  a.by_units = FastDiv::by(a.row_units);
+  return status_of(launch_paged_append(a, (hipStream_t)stream));
+}
+
+int vico_paged_attn_plan(int32_t num_seqs, int32_t total_q, int32_t max_q_len, int32_t page_size, int32_t max_pages,
+                         int32_t sink_len, int64_t window, int64_t keys_hint, int32_t num_q_heads,
+                         int32_t num_kv_heads, int32_t head_dim, int32_t num_splits, int32_t* num_splits_out,
+                         int64_t* workspace_bytes_out) {
+  PagedPlan pl;
+  const int st = check_paged_shape(num_seqs, total_q, max_q_len, page_size, max_pages, sink_len, window, keys_hint,
+                                   num_q_heads, num_kv_heads, head_dim, num_splits, &pl);
+  if (st != VICO_OK) return st;
+  if (num_splits_out) *num_splits_out = std::max(pl.parts, 1);
+  if (workspace_bytes_out) *workspace_bytes_out = pl.ws_bytes;
+  return VICO_OK;
+}
+
+int vico_paged_attn(const void* q, const int32_t* q_start, const int32_t* seq_len, int32_t num_seqs, int32_t total_q,
+                    int32_t max_q_len, const void* k_pages, const void* v_pages, int32_t num_pages, int32_t page_size,
+                    const int32_t* page_table, int32_t max_pages, int32_t sink_len, int64_t window, int64_t keys_hint,
+                    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float softmax_scale, int32_t flags,
+                    void* out, int32_t out_dtype, float* lse_out, int32_t num_splits, void* workspace,
+                    int64_t workspace_bytes, void* stream) {
+  PagedPlan pl;
+  const int st = check_paged_shape(num_seqs, total_q, max_q_len, page_size, max_pages, sink_len, window, keys_hint,
+                                   num_q_heads, num_kv_heads, head_dim, num_splits, &pl);
+  if (st != VICO_OK) return st;
+  if (out_dtype != VICO_DTYPE_BF16 && out_dtype != VICO_DTYPE_F32) return VICO_ERR_UNSUPPORTED;
+  if (flags & ~VICO_ATTN_BIDIRECTIONAL) return VICO_ERR_INVALID_ARG;
+  if (isnan(softmax_scale) || isinf(softmax_scale) || workspace_bytes < 0) return VICO_ERR_INVALID_ARG;
+  if (num_pages < 0 || num_pages > kMaxPages) return VICO_ERR_INVALID_ARG;
+  if (num_seqs == 0 || total_q == 0 || max_q_len == 0) return VICO_OK;
+  // a pool or a table without an entry leaves every row without keys, and the kernels without an address to read
+  if (num_pages == 0 || max_pages == 0) return VICO_ERR_CAPACITY;
+  if (!q || !q_start || !seq_len || !k_pages || !v_pages || !page_table || !out) return VICO_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || (workspace && !aligned16(workspace)) ||
+      !aligned_to(q_start, 4) || !aligned_to(seq_len, 4) || !aligned_to(page_table, 4) || !aligned_to(lse_out, 4))
+    return VICO_ERR_MISALIGNED;
+  if (pl.ws_bytes > 0 && (!workspace || workspace_bytes < pl.ws_bytes)) return VICO_ERR_WORKSPACE;
+  const int64_t rows = int64_t(total_q) * num_q_heads, pool = pool_bytes(num_pages, page_size, num_kv_heads, head_dim);
+  const Region w[] = {{out, rows * head_dim * (out_dtype == VICO_DTYPE_F32 ? 4 : 2)}, {lse_out, rows * 4},
+                      {pl.ws_bytes > 0 ? workspace : nullptr, pl.ws_bytes}};
+  const Region r[] = {{q, rows * head_dim * 2}, {k_pages, pool}, {v_pages, pool}, {q_start, int64_t(num_seqs + 1) * 4},
+                      {seq_len, int64_t(num_seqs) * 4}, {page_table, int64_t(num_seqs) * max_pages * 4}};
+  if (collide(w, r)) return VICO_ERR_INVALID_ARG;
+
+  PagedAttnArgs a{};
+  a.q = (const uint16_t*)q; a.q_start = q_start; a.seq_len = seq_len;
+  a.k_pages = (const uint16_t*)k_pages; a.v_pages = (const uint16_t*)v_pages; a.table = page_table;
+  a.out = out; a.lse = lse_out;
+  a.B = num_seqs; a.total = total_q; a.max_q = max_q_len; a.N = num_pages; a.width = max_pages;
+  a.page_shift = shift_of(page_size);
+  a.S = sink_len; a.W = window;
+  a.Hq = num_q_heads; a.Hkv = num_kv_heads; a.D = head_dim;
+  a.bidir = (flags & VICO_ATTN_BIDIRECTIONAL) != 0;
+  a.out_f32 = out_dtype == VICO_DTYPE_F32;
+  const double scale = softmax_scale > 0.f ? double(softmax_scale) : 1.0 / sqrt(double(head_dim));
+  a.scale_log2 = (float)(scale * 1.4426950408889634);
+  a.rows_most = pl.rows_most; a.n_rt = pl.n_rt; a.row_blocks = pl.row_blocks;
+  a.parts = pl.parts; a.per_part = pl.per_part;
+  a.by_g = FastDiv::by(a.Hq / a.Hkv);
+  a.by_kv = FastDiv::by(a.Hkv);
+  hipError_t e = hipSuccess;
+  if (pl.rows) {
+    a.by_rt = FastDiv::by(a.n_rt);
+    a.by_parts = FastDiv::by(a.parts);
+    if (a.parts > 1) {
+      a.ws_o = (float*)workspace;
+      a.ws_lse = (float*)((char*)workspace + align256(int64_t(a.B) * a.Hkv * a.n_rt * a.parts * 16 * a.row_blocks * a.D * 4));
+    }
+    e = launch_paged_rows(a, (hipStream_t)stream);
+  }
+  return status_of(e);
+}
+
+int64_t vico_pages_workspace_bytes(int32_t num_seqs, int32_t num_pages) {
+  if (!table_ok(num_seqs, 0, num_pages, 0)) return VICO_ERR_INVALID_ARG;
+  return table_workspace(num_seqs, num_pages);
+}
+
+int vico_pages_fork(int32_t* page_table, int32_t num_seqs, int32_t max_pages, int32_t* page_refs, int32_t num_pages,
+                    int32_t page_size, int32_t* seq_len, const int32_t* parent, void* stream) {
+  if (page_size == 0 || !table_ok(num_seqs, max_pages, num_pages, page_size)) return VICO_ERR_INVALID_ARG;
+  if (num_seqs == 0) return VICO_OK;
+  if (max_pages == 0 || num_pages == 0) return VICO_ERR_CAPACITY;
+  if (!page_table || !page_refs || !seq_len || !parent) return VICO_ERR_INVALID_ARG;
+  if (!aligned_to(page_table, 4) || !aligned_to(page_refs, 4) || !aligned_to(seq_len, 4) || !aligned_to(parent, 4))
+    return VICO_ERR_MISALIGNED;
+  const Region w[] = {{page_table, int64_t(num_seqs) * max_pages * 4}, {page_refs, int64_t(num_pages) * 4},
+                      {seq_len, int64_t(num_seqs) * 4}};
+  const Region r[] = {{parent, int64_t(num_seqs) * 4}};
+  if (collide(w, r)) return VICO_ERR_INVALID_ARG;
+  PagesArgs a{};
+  a.table = page_table; a.refs = page_refs; a.seq_len = seq_len; a.parent = parent;
+  a.B = num_seqs; a.width = max_pages; a.N = num_pages; a.page_shift = shift_of(page_size);
+  return status_of(launch_pages_fork(a, (hipStream_t)stream));
+}
+
+int vico_pages_free(int32_t* page_table, int32_t num_seqs, int32_t max_pages, int32_t* page_refs, int32_t num_pages,
+                    int32_t page_size, const int32_t* first, const int32_t* last, void* stream) {
+  if (page_size == 0 || !table_ok(num_seqs, max_pages, num_pages, page_size)) return VICO_ERR_INVALID_ARG;
+  if (num_seqs == 0 || max_pages == 0) return VICO_OK;
+  if (num_pages == 0) return VICO_ERR_CAPACITY;
+  if (!page_table || !page_refs || !first || !last) return VICO_ERR_INVALID_ARG;
+  if (!aligned_to(page_table, 4) || !aligned_to(page_refs, 4) || !aligned_to(first, 4) || !aligned_to(last, 4))
+    return VICO_ERR_MISALIGNED;
+  const Region w[] = {{page_table, int64_t(num_seqs) * max_pages * 4}, {page_refs, int64_t(num_pages) * 4}};
+  const Region r[] = {{first, int64_t(num_seqs) * 4}, {last, int64_t(num_seqs) * 4}};
+  if (collide(w, r)) return VICO_ERR_INVALID_ARG;
+  PagesArgs a{};
+  a.table = page_table; a.refs = page_refs; a.first = first; a.last = last;
+  a.B = num_seqs; a.width = max_pages; a.N = num_pages; a.page_shift = shift_of(page_size);
+  return status_of(launch_pages_free(a, (hipStream_t)stream));
+}
+
+int vico_pages_reserve(int32_t* page_table, int32_t num_seqs, int32_t max_pages, int32_t* page_refs,
+                       int32_t num_pages, int32_t page_size, const int32_t* seq_len, const int32_t* q_start,
+                       int32_t* moves, int32_t* granted, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (page_size == 0 || !table_ok(num_seqs, max_pages, num_pages, page_size) || workspace_bytes < 0) return VICO_ERR_INVALID_ARG;
+  if (num_seqs == 0) return VICO_OK;
+  if (max_pages == 0 || num_pages == 0) return VICO_ERR_CAPACITY;
+  if (!page_table || !page_refs || !seq_len || !q_start || !moves || !granted) return VICO_ERR_INVALID_ARG;
+  if (!aligned_to(page_table, 4) || !aligned_to(page_refs, 4) || !aligned_to(seq_len, 4) || !aligned_to(q_start, 4) ||
+      !aligned_to(moves, 8) || !aligned_to(granted, 4) || (workspace && !aligned16(workspace)))
+    return VICO_ERR_MISALIGNED;
+  const int64_t ws = table_workspace(num_seqs, num_pages);
+  if (!workspace || workspace_bytes < ws) return VICO_ERR_WORKSPACE;
+  const Region w[] = {{page_table, int64_t(num_seqs) * max_pages * 4}, {page_refs, int64_t(num_pages) * 4},
+                      {moves, int64_t(num_seqs) * 8}, {granted, int64_t(num_seqs) * 4}, {workspace, ws}};
+  const Region r[] = {{seq_len, int64_t(num_seqs) * 4}, {q_start, int64_t(num_seqs + 1) * 4}};
+  if (collide(w, r)) return VICO_ERR_INVALID_ARG;
+  PagesArgs a{};
+  a.table = page_table; a.refs = page_refs; a.seq_len = const_cast<int32_t*>(seq_len); a.q_start = q_start;
+  a.moves = moves; a.granted = granted;
+  a.B = num_seqs; a.width = max_pages; a.N = num_pages; a.page_shift = shift_of(page_size); a.n_blocks = page_blocks(num_pages);
+  use_workspace(&a, workspace);
+  return status_of(launch_pages_reserve(a, (hipStream_t)stream));
+}
+
+int vico_pages_compact(int32_t* page_table, int32_t num_seqs, int32_t max_pages, int32_t* page_refs,
+                       int32_t num_pages, int32_t* moves, int32_t max_moves, int32_t* count, void* workspace,
+                       int64_t workspace_bytes, void* stream) {
+  if (!table_ok(num_seqs, max_pages, num_pages, 0) || max_moves < 0 || max_moves > kMaxMoves || workspace_bytes < 0)
+    return VICO_ERR_INVALID_ARG;
+  if (max_moves < num_pages / 2) return VICO_ERR_CAPACITY;
+  if (num_pages == 0) return VICO_ERR_CAPACITY;
+  if (!page_refs || !count || (max_moves > 0 && !moves) || (int64_t(num_seqs) * max_pages > 0 && !page_table)) return VICO_ERR_INVALID_ARG;
+  if (!aligned_to(page_table, 4) || !aligned_to(page_refs, 4) || !aligned_to(moves, 8) || !aligned_to(count, 4) ||
+      (workspace && !aligned16(workspace)))
+    return VICO_ERR_MISALIGNED;
+  const int64_t ws = table_workspace(num_seqs, num_pages);
+  if (!workspace || workspace_bytes < ws) return VICO_ERR_WORKSPACE;
+  const Region w[] = {{page_table, int64_t(num_seqs) * max_pages * 4}, {page_refs, int64_t(num_pages) * 4},
+                      {moves, int64_t(max_moves) * 8}, {count, 4}, {workspace, ws}};
+  const Region r[] = {{nullptr, 0}};
+  if (collide(w, r)) return VICO_ERR_INVALID_ARG;
+  PagesArgs a{};
+  a.table = page_table; a.refs = page_refs; a.moves = moves; a.count = count;
+  a.B = num_seqs; a.width = max_pages; a.N = num_pages; a.n_blocks = page_blocks(num_pages); a.max_moves = max_moves;
+  use_workspace(&a, workspace);
+  return status_of(launch_pages_compact(a, (hipStream_t)stream));
+}
+
+int vico_pages_copy(void* k_pages, void* v_pages, int32_t num_layers, int32_t num_pages, int32_t page_size,
+                    int32_t num_kv_heads, int32_t head_dim, const int32_t* moves, int32_t num_moves,
+                    const int32_t* count, void* stream) {
+  if (num_layers < 0 || num_layers > 4096 || num_moves < 0 || num_moves > kMaxMoves || !heads_ok(num_kv_heads, num_kv_heads))
+    return VICO_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return VICO_ERR_UNSUPPORTED;
+  if (page_size == 0 || !table_ok(0, 0, num_pages, page_size)) return VICO_ERR_INVALID_ARG;
+  if (num_layers == 0 || num_pages == 0 || num_moves == 0) return VICO_OK;
+  if (!k_pages || !v_pages || !moves) return VICO_ERR_INVALID_ARG;
+  if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned_to(moves, 8) || !aligned_to(count, 4)) return VICO_ERR_MISALIGNED;
+  const int64_t pool = pool_bytes(num_pages, page_size, num_kv_heads, head_dim);
+  const Region w[] = {{k_pages, pool * num_layers}, {v_pages, pool * num_layers}};
+  const Region r[] = {{moves, int64_t(num_moves) * 8}, {count, 4}};
+  if (collide(w, r)) return VICO_ERR_INVALID_ARG;
+  PagesCopyArgs a{};
+  a.k = (uint16_t*)k_pages; a.v = (uint16_t*)v_pages; a.moves = moves; a.count = count;
+  a.n_moves = num_moves; a.layers = num_layers; a.N = num_pages;
+  a.page_units = page_size * num_kv_heads * (head_dim / 8);
+  return status_of(launch_pages_copy(a, (hipStream_t)stream));
+}
+
+}  // extern "C"

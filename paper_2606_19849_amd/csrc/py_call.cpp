@@ -18,6 +18,7 @@
 #include <c10/hip/HIPStream.h>
 
 #include "vico_cache.h"
+#include "vico_pages.h"
 
 namespace {
 
@@ -286,7 +287,7 @@ PyObject* temporal_drop(PyObject* const* args, Py_ssize_t n) {
   });
 }
 
-// The calls of vico_cache.h take tensors of the current device only.
+// The calls of vico_cache.h and vico_pages.h take tensors of the current device only.
 template <class... T>
 bool here(const T*... t) {
   const int dev = c10::hip::current_device();
@@ -414,10 +415,129 @@ PyObject* gather_q4(PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// ---- the cache in pages.  A pool of pages: [pages][tokens of a page][heads][dim], or with the layers before it.
+bool shape1(const at::Tensor* t, int64_t a) { return t->size(0) == a; }
+bool shape2(const at::Tensor* t, int64_t a, int64_t b) { return t->size(0) == a && t->size(1) == b; }
+
+// k, v, q_start, seq_len, k_pages, v_pages, page_table, stream
+PyObject* paged_append(PyObject* const* args, Py_ssize_t n) {
+  Args in{args, n};
+  const at::Tensor *k = in.tensor(at::kBFloat16, 3), *v = in.tensor(at::kBFloat16, 3);
+  const at::Tensor *qs = in.tensor(at::kInt, 1), *len = in.tensor(at::kInt, 1);
+  const at::Tensor *kp = in.tensor(at::kBFloat16, 4), *vp = in.tensor(at::kBFloat16, 4), *pt = in.tensor(at::kInt, 2);
+  void* stream = in.stream();
+  if (!in.ok || !same_shape(k, v) || !same_shape(kp, vp) || kp->size(2) != k->size(1) || kp->size(3) != k->size(2)) Py_RETURN_NONE;
+  if (!shape1(len, pt->size(0)) || !shape1(qs, pt->size(0) + 1) || !here(k, v, qs, len, kp, vp, pt)) Py_RETURN_NONE;
+  if (!fits(k) || !fits(kp) || !fits(pt)) Py_RETURN_NONE;
+  void *const a = wptr(kp), *const b = wptr(vp);
+  return called(in, [&] {
+    return vico_paged_append(ptr(k), ptr(v), size(k, 0), (const int32_t*)ptr(qs), (const int32_t*)ptr(len), size(pt, 0), a, b,
+                             size(kp, 0), size(kp, 1), (const int32_t*)ptr(pt), size(pt, 1), size(k, 1), size(k, 2), stream);
+  });
+}
+
+// q, q_start, seq_len, k_pages, v_pages, page_table, out, lse, sink_len, window, max_q_len, keys_hint, num_splits,
+// softmax_scale, flags, workspace, stream
+PyObject* paged_attn(PyObject* const* args, Py_ssize_t n) {
+  Args in{args, n};
+  const at::Tensor *q = in.tensor(at::kBFloat16, 3), *qs = in.tensor(at::kInt, 1), *len = in.tensor(at::kInt, 1);
+  const at::Tensor *kp = in.tensor(at::kBFloat16, 4), *vp = in.tensor(at::kBFloat16, 4), *pt = in.tensor(at::kInt, 2);
+  const at::Tensor* out = in.output();
+  const at::Tensor* lse = in.tensor(at::kFloat, 2, true);
+  const int32_t sink = in.int32();
+  const int64_t window = in.integer();
+  const int32_t most = in.int32();
+  const int64_t hint = in.integer();
+  const int32_t splits = in.int32();
+  const float scale = in.real();
+  const int32_t flags = in.int32();
+  const at::Tensor* ws = in.memory(true);
+  void* stream = in.stream();
+  if (!in.ok || !same_shape(out, q) || !same_shape(kp, vp) || kp->size(3) != q->size(2)) Py_RETURN_NONE;
+  if (!shape1(len, pt->size(0)) || !shape1(qs, pt->size(0) + 1) || (lse && !shape2(lse, q->size(1), q->size(0)))) Py_RETURN_NONE;
+  if (!here(q, qs, len, kp, vp, pt, out, lse, ws) || !fits(q) || !fits(kp) || !fits(pt)) Py_RETURN_NONE;
+  void *const o = wptr(out), *const l = wptr(lse), *const w = wptr(ws);
+  return called(in, [&] {
+    return vico_paged_attn(ptr(q), (const int32_t*)ptr(qs), (const int32_t*)ptr(len), size(pt, 0), size(q, 0), most, ptr(kp),
+                           ptr(vp), size(kp, 0), size(kp, 1), (const int32_t*)ptr(pt), size(pt, 1), sink, window, hint,
+                           size(q, 1), size(kp, 2), size(q, 2), scale, flags, o,
+                           out->scalar_type() == at::kFloat ? VICO_DTYPE_F32 : VICO_DTYPE_BF16, (float*)l, splits, w, bytes(ws),
+                           stream);
+  });
+}
+
+// page_table, page_refs, two arrays of a number for each row, page_size, stream; the first array is written if FORK
+template <bool FORK>
+PyObject* pages_rows(PyObject* const* args, Py_ssize_t n) {
+  Args in{args, n};
+  const at::Tensor *pt = in.tensor(at::kInt, 2), *refs = in.tensor(at::kInt, 1), *x = in.tensor(at::kInt, 1), *y = in.tensor(at::kInt, 1);
+  const int32_t page = in.int32();
+  void* stream = in.stream();
+  if (!in.ok || !shape1(x, pt->size(0)) || !shape1(y, pt->size(0)) || !here(pt, refs, x, y) || !fits(pt)) Py_RETURN_NONE;
+  int32_t *const t = (int32_t*)wptr(pt), *const r = (int32_t*)wptr(refs), *const a = (int32_t*)(FORK ? wptr(x) : ptr(x));
+  return called(in, [&] {
+    return (FORK ? vico_pages_fork(t, size(pt, 0), size(pt, 1), r, size(refs, 0), page, a, (const int32_t*)ptr(y), stream)
+                 : vico_pages_free(t, size(pt, 0), size(pt, 1), r, size(refs, 0), page, a, (const int32_t*)ptr(y), stream));
+  });
+}
+PyObject* pages_fork(PyObject* const* args, Py_ssize_t n) { return pages_rows<true>(args, n); }
+PyObject* pages_free(PyObject* const* args, Py_ssize_t n) { return pages_rows<false>(args, n); }
+
+// page_table, page_refs, seq_len, q_start, page_size, moves, granted, workspace, stream
+PyObject* pages_reserve(PyObject* const* args, Py_ssize_t n) {
+  Args in{args, n};
+  const at::Tensor *pt = in.tensor(at::kInt, 2), *refs = in.tensor(at::kInt, 1), *len = in.tensor(at::kInt, 1), *qs = in.tensor(at::kInt, 1);
+  const int32_t page = in.int32();
+  const at::Tensor *mv = in.tensor(at::kInt, 2), *ok = in.tensor(at::kInt, 1);
+  const at::Tensor* ws = in.memory(true);
+  void* stream = in.stream();
+  if (!in.ok || !here(pt, refs, len, qs, mv, ok, ws) || !fits(pt)) Py_RETURN_NONE;
+  const int64_t B = pt->size(0);
+  if (!shape1(len, B) || !shape1(qs, B + 1) || !shape2(mv, B, 2) || !shape1(ok, B)) Py_RETURN_NONE;
+  void *const t = wptr(pt), *const r = wptr(refs), *const m = wptr(mv), *const g = wptr(ok), *const w = wptr(ws);
+  return called(in, [&] {
+    return vico_pages_reserve((int32_t*)t, size(pt, 0), size(pt, 1), (int32_t*)r, size(refs, 0), page, (const int32_t*)ptr(len),
+                              (const int32_t*)ptr(qs), (int32_t*)m, (int32_t*)g, w, bytes(ws), stream);
+  });
+}
+
+// page_table, page_refs, moves, count, workspace, stream
+PyObject* pages_compact(PyObject* const* args, Py_ssize_t n) {
+  Args in{args, n};
+  const at::Tensor *pt = in.tensor(at::kInt, 2), *refs = in.tensor(at::kInt, 1), *mv = in.tensor(at::kInt, 2), *cnt = in.tensor(at::kInt, 1);
+  const at::Tensor* ws = in.memory(true);
+  void* stream = in.stream();
+  if (!in.ok || mv->size(1) != 2 || !shape1(cnt, 1) || !here(pt, refs, mv, cnt, ws) || !fits(pt) || mv->size(0) != size(mv, 0))
+    Py_RETURN_NONE;
+  void *const t = wptr(pt), *const r = wptr(refs), *const m = wptr(mv), *const c = wptr(cnt), *const w = wptr(ws);
+  return called(in, [&] {
+    return vico_pages_compact((int32_t*)t, size(pt, 0), size(pt, 1), (int32_t*)r, size(refs, 0), (int32_t*)m, size(mv, 0),
+                              (int32_t*)c, w, bytes(ws), stream);
+  });
+}
+
+// k_pages, v_pages (with or without layers), moves, count, stream
+PyObject* pages_copy(PyObject* const* args, Py_ssize_t n) {
+  Args in{args, n};
+  const int dims = n > 0 && THPVariable_CheckExact(args[0]) && THPVariable_Unpack(args[0]).dim() == 5 ? 5 : 4, l = dims - 4;
+  const at::Tensor *kp = in.tensor(at::kBFloat16, dims), *vp = in.tensor(at::kBFloat16, dims), *mv = in.tensor(at::kInt, 2);
+  const at::Tensor* cnt = in.tensor(at::kInt, 1, true);
+  void* stream = in.stream();
+  if (!in.ok || !same_shape(kp, vp) || mv->size(1) != 2 || (cnt && !shape1(cnt, 1)) || !here(kp, vp, mv, cnt)) Py_RETURN_NONE;
+  if (!fits(kp) || mv->size(0) != size(mv, 0)) Py_RETURN_NONE;
+  void *const a = wptr(kp), *const b = wptr(vp);
+  return called(in, [&] {
+    return vico_pages_copy(a, b, l ? size(kp, 0) : 1, size(kp, l), size(kp, l + 1), size(kp, l + 2), size(kp, l + 3),
+                           (const int32_t*)ptr(mv), size(mv, 0), (const int32_t*)ptr(cnt), stream);
+  });
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(prefill),      FAST(gather),      FAST(gather_noalloc), FAST(kv_append), FAST(token_mean),
                          FAST(chunk_scores), FAST(topk_chunks), FAST(temporal_drop),
-                         FAST(qk_norm_rope), FAST(append_q4),   FAST(load_q4),        FAST(gather_q4), {nullptr, nullptr, 0, nullptr}};
+                         FAST(qk_norm_rope), FAST(append_q4),   FAST(load_q4),        FAST(gather_q4),
+                         FAST(paged_append), FAST(paged_attn),  FAST(pages_fork),     FAST(pages_free), FAST(pages_reserve),
+                         FAST(pages_compact), FAST(pages_copy), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_vico_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -11,6 +11,7 @@
 #pragma once
 
 #include "attn_common.h"
+#include "values.h"
 
 namespace vico {
 
@@ -42,17 +43,6 @@ __device__ __forceinline__ late_args late() {
   late_args p = (late_args)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(p));
   return p;
-}
-
-// Pairs of bf16 values that are not finite: the largest exponent fields of the pairs seen so far, and the pair with
-// zeros in their place.
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void largest_exponents(u16x2& most, uint32_t x) {
-  most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x & 0x7F807F80u));
-}
-__device__ __forceinline__ bool not_finite(u16x2 most) { return (most[0] == 0x7F80) | (most[1] == 0x7F80); }
-__device__ __forceinline__ uint32_t finite_or_zero(uint32_t x) {
-  return x & ((x & 0x7F80u) == 0x7F80u ? 0xFFFF0000u : ~0u) & ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFFu : ~0u);
 }
 
 // The segment table of a work-group of NT threads.  The lanes of every wave

@@ -1,0 +1,554 @@
+"""GPU parity of include/vico_pages.h: the table's calls and the copies exactly, attention within the derived
+per-element bounds of tests/_bounds.py (fp32 and bf16 outputs, the log-sum-exp)."""
+from __future__ import annotations
+
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_19849_amd as vico
+from oracle import pages
+from tests._pages import DEV, Cache, check, f64, i32
+
+pytestmark = pytest.mark.gpu
+
+H128, H7B, H3B, ODD = (4, 2, 128), (28, 4, 128), (16, 2, 128), (6, 2, 64)
+
+
+# ---------------------------------------------------------------- the table
+
+def bits(t):
+    return t.view(torch.int16)
+
+
+def random_state(seed, rows, page, N, width, share=0.4, most=1.0):
+    """A consistent table: rows of some length, some of them branches of others, and reserved pages past the length."""
+    r = random.Random(seed)
+    free = list(range(N))
+    r.shuffle(free)
+    table, refs, lens = [], [0] * N, []
+    for b in range(rows):
+        row = [-1] * width
+        if b and r.random() < share:
+            p = r.randrange(b)
+            keep = pages.pages_of(r.randint(0, lens[p]), page)
+            row[:keep] = table[p][:keep]
+            lens.append(max(min(lens[p], keep * page - r.randrange(page)), 0))
+        else:
+            tokens = min(r.randint(0, int(width * page * most)), len(free) * page)
+            for j in range(pages.pages_of(tokens, page)):
+                row[j] = free.pop()
+            lens.append(max(tokens - r.randrange(2 * page), 0))
+        for e in row:
+            if e >= 0:
+                refs[e] += 1
+        table.append(row)
+    return table, refs, lens
+
+
+def guarded(x, extra=8):
+    """The values on the device with a margin behind them, and the margin."""
+    t = torch.tensor(x, dtype=torch.int32)
+    raw = torch.full((t.numel() + extra,), 12345, dtype=torch.int32, device=DEV)
+    raw[:t.numel()] = t.flatten().to(DEV)
+    return raw[:t.numel()].view(t.shape), raw[t.numel():]
+
+
+TABLES = [(1, 16, 8, 4), (3, 16, 40, 9), (7, 64, 300, 70), (33, 16, 1500, 64), (65, 32, 5000, 130), (130, 16, 3000, 33),
+          (600, 16, 6000, 12)]
+
+
+@pytest.mark.parametrize("rows,page,N,width", TABLES)
+def test_fork(rows, page, N, width):
+    table, refs, lens = random_state(rows, rows, page, N, width)
+    r = random.Random(rows + 1)
+    parent = [r.choice([b, -1, r.randrange(rows), r.randrange(rows), -5, rows]) for b in range(rows)]
+    (t, m0), (f, m1), (s, m2) = guarded(table), guarded(refs), guarded(lens)
+    vico.vico_pages_fork(t, f, s, i32(parent), page)
+    want = pages.fork(table, refs, lens, parent, page)
+    assert t.tolist() == want[0] and f.tolist() == want[1] and s.tolist() == want[2]
+    assert all(torch.all(m == 12345) for m in (m0, m1, m2))
+
+
+def test_fork_of_many_rows():
+    rows, page, N, width = 4096, 16, 9000, 20
+    table, refs, lens = random_state(3, rows, page, N, width, most=0.2)
+    parent = [(b * 7 + 3) % rows for b in range(rows)]
+    t, f, s = i32(table), i32(refs), i32(lens)
+    vico.vico_pages_fork(t, f, s, i32(parent), page)
+    want = pages.fork(table, refs, lens, parent, page)
+    assert t.tolist() == want[0] and f.tolist() == want[1] and s.tolist() == want[2]
+
+
+@pytest.mark.parametrize("rows,page,N,width", TABLES)
+def test_free(rows, page, N, width):
+    table, refs, lens = random_state(rows + 5, rows, page, N, width)
+    r = random.Random(rows)
+    first = [r.choice([0, -3, r.randrange(width * page), page, 2 ** 31 - 1]) for _ in range(rows)]
+    last = [r.choice([0, -1, r.randrange(width * page), width * page, 2 ** 31 - 1]) for _ in range(rows)]
+    (t, m0), (f, m1) = guarded(table), guarded(refs)
+    vico.vico_pages_free(t, f, i32(first), i32(last), page)
+    want = pages.free(table, refs, first, last, page)
+    assert t.tolist() == want[0] and f.tolist() == want[1]
+    assert torch.all(m0 == 12345) and torch.all(m1 == 12345)
+
+
+def reserve(table, refs, lens, starts, page):
+    B, N = len(table), len(refs)
+    (t, m0), (f, m1) = guarded(table), guarded(refs)
+    (moves, m2), (granted, m3) = guarded([[99, 99]] * B), guarded([99] * B)
+    wb = vico.vico_pages_workspace_bytes(B, N)
+    ws = torch.full((wb + 64,), 171, dtype=torch.uint8, device=DEV)
+    vico.vico_pages_reserve(t, f, i32(lens), i32(starts), page, moves, granted, ws[:wb])
+    assert all(torch.all(m == 12345) for m in (m0, m1, m2, m3)) and torch.all(ws[wb:] == 171)
+    return t.tolist(), f.tolist(), moves.tolist(), granted.tolist()
+
+
+@pytest.mark.parametrize("most", [1, 40, 4000])
+@pytest.mark.parametrize("rows,page,N,width", TABLES)
+def test_reserve(rows, page, N, width, most):
+    table, refs, lens = random_state(rows + 9, rows, page, N, width, most=0.6)
+    r = random.Random(most)
+    n = [r.choice([0, 1, r.randint(0, most)]) for _ in range(rows)]
+    starts = np.cumsum([3] + n).tolist()
+    assert reserve(table, refs, lens, starts, page) == tuple(pages.reserve(table, refs, lens, starts, page))
+
+
+def test_reserve_without_enough_pages():
+    # four free pages; row 1 wants three, row 2 two, row 3 none, row 4 one, row 5 passes the table
+    table = [[0, -1, -1, -1], [1, -1, -1, -1], [2, -1, -1, -1], [3, -1, -1, -1], [4, -1, -1, -1], [5, -1, -1, -1]]
+    refs = [1] * 6 + [0] * 4
+    lens, n = [16, 16, 16, 3, 16, 60], [0, 48, 20, 13, 1, 5]
+    starts = np.cumsum([0] + n).tolist()
+    got = reserve(table, refs, lens, starts, 16)
+    assert got == tuple(pages.reserve(table, refs, lens, starts, 16))
+    assert got[3] == [1, 1, 0, 1, 0, 0]
+
+
+def test_reserve_replaces_what_both_branches_hold():
+    # rows 0 and 1 share a full page and a half-filled one; both go on
+    table, refs = [[2, 5, -1], [2, 5, -1]], [0, 0, 2, 0, 0, 2, 0]
+    got = reserve(table, refs, [24, 24], [0, 4, 20], 16)
+    assert got == ([[2, 0, -1], [2, 1, 3]], [1, 1, 2, 1, 0, 0, 0], [[5, 0], [5, 1]], [1, 1])
+
+
+@pytest.mark.parametrize("rows,page,N,width", TABLES + [(2, 16, 100000, 3000)])
+def test_compact(rows, page, N, width):
+    table, refs, _ = random_state(rows + 13, rows, page, N, width)
+    most = N // 2 + 3
+    (t, m0), (f, m1), (moves, m2), (count, m3) = guarded(table), guarded(refs), guarded([[99, 99]] * most), guarded([99])
+    ws = torch.full((vico.vico_pages_workspace_bytes(rows, N),), 171, dtype=torch.uint8, device=DEV)
+    vico.vico_pages_compact(t, f, moves, count, ws)
+    want = pages.compact(table, refs, most)
+    assert t.tolist() == want[0] and f.tolist() == want[1] and moves.tolist() == want[2] and count.item() == want[3]
+    assert all(torch.all(m == 12345) for m in (m0, m1, m2, m3))
+
+
+@pytest.mark.parametrize("full", [True, False])
+def test_compact_of_a_full_or_empty_pool(full):
+    N = 1025
+    refs, table = [int(full)] * N, [list(range(N)) if full else [-1] * N]
+    t, f, moves, count = i32(table), i32(refs), i32([[9, 9]] * (N // 2)), i32([9])
+    vico.vico_pages_compact(t, f, moves, count, torch.empty(vico.vico_pages_workspace_bytes(1, N), dtype=torch.uint8, device=DEV))
+    assert count.item() == 0 and t.tolist() == table and f.tolist() == refs and torch.all(moves == -1)
+
+
+# ---------------------------------------------------------------- contents
+
+@pytest.mark.parametrize("layers,N,page,Hkv,D", [(1, 9, 16, 1, 64), (3, 40, 64, 4, 128), (2, 12, 256, 2, 128), (1, 5, 1024, 3, 64)])
+def test_copy(layers, N, page, Hkv, D):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(N)
+    k, v = (torch.randint(-2 ** 15, 2 ** 15, (layers, N, page, Hkv, D), generator=g, device=DEV, dtype=torch.int16).view(torch.bfloat16)
+            for _ in "kv")
+    pairs = [[N - 1, 0], [-1, -1], [1, 2], [N, 3], [3, -1], [4, 4]]
+    for count in (None, 1, 0, 100, -3):
+        x, y = k.clone(), v.clone()
+        a, b = (t if layers > 1 else t[0] for t in (x, y))
+        vico.vico_pages_copy(a, b, i32(pairs), count=None if count is None else i32([count]))
+        n = len(pairs) if count is None else max(min(count, len(pairs)), 0)
+        for s, d in [p for p in pairs[:n] if 0 <= p[0] < N and 0 <= p[1] < N]:
+            k_, v_ = k.clone(), v.clone()
+        want = [t.clone() for t in (k, v)]
+        for s, d in pairs[:n]:
+            if 0 <= s < N and 0 <= d < N:
+                for w, t in zip(want, (k, v)):
+                    w[:, d] = t[:, s]
+        assert torch.equal(bits(x), bits(want[0])) and torch.equal(bits(y), bits(want[1]))
+
+
+@pytest.mark.parametrize("heads", [(1, 1, 64), (4, 4, 128), (3, 3, 64), (5, 5, 128)], ids=str)
+@pytest.mark.parametrize("seqs,page", [([(1, 0)], 16), ([(1, 15), (1, 16), (0, 4), (33, 40)], 16), ([(700, 3), (0, 0), (257, 130)], 64),
+                                       ([(1, b) for b in range(70)], 32), ([(b % 3, b) for b in range(300)], 16),
+                                       ([(2000, 1000)], 1024)], ids=lambda x: str(x)[:24])
+def test_append(heads, seqs, page):
+    c = Cache(len(seqs), seqs, heads=heads, page=page, drop={(1, 0)} if len(seqs) > 1 else ()).device()
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    rows = c.q_start[-1] + 3                      # rows behind the last sequence go nowhere
+    k, v = (torch.randint(-2 ** 15, 2 ** 15, (rows, c.Hkv, c.D), generator=g, device=DEV, dtype=torch.int16).view(torch.bfloat16)
+            for _ in "kv")
+    wk, wv = c.dk.clone(), c.dv.clone()
+    for b, n in enumerate(c.n):
+        for j in range(n):
+            page_, at = c.place(b, c.H[b] + j)
+            if 0 <= page_ < c.k.shape[0]:
+                wk[page_, at], wv[page_, at] = k[c.q_start[b] + j], v[c.q_start[b] + j]
+    vico.vico_paged_append(k, v, c.ds, c.dl, c.dk, c.dv, c.dt)
+    assert torch.equal(bits(c.dk), bits(wk)) and torch.equal(bits(c.dv), bits(wv))
+
+
+def test_append_past_the_table_goes_nowhere():
+    c = Cache(3, [(5, 14), (40, 0)], heads=(2, 2, 64), width=1).device()
+    wk = c.dk.clone()
+    k = torch.randn(c.q.shape[0], 2, 64, device=DEV).to(torch.bfloat16)
+    vico.vico_paged_append(k, k, c.ds, c.dl, c.dk, c.dv, c.dt)
+    for b, n in ((0, 2), (1, 16)):
+        for j in range(n):
+            page, at = c.place(b, c.H[b] + j)
+            wk[page, at] = k[c.q_start[b] + j]
+    assert torch.equal(bits(c.dk), bits(wk))
+
+
+# ---------------------------------------------------------------- attention
+
+SEQS = {
+    "one": [(1, 0)],
+    "decode": [(1, 200)],
+    "decodes": [(1, 0), (1, 15), (1, 16), (1, 31), (1, 700), (0, 9), (1, 64), (1, 63)],
+    "short": [(5, 33), (2, 0), (0, 0), (17, 480), (3, 47)],
+    "mixed": [(1, 90), (150, 77), (1, 1), (64, 0), (7, 300)],
+    "chunk": [(333, 190)],
+}
+MASKS = [dict(), dict(sink=5, window=40), dict(sink=40, window=17), dict(window=0), dict(sink=64, window=64)]
+
+
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("mask", MASKS, ids=str)
+@pytest.mark.parametrize("name", SEQS)
+def test_attention(name, mask, page):
+    heads = {16: ODD, 64: (4, 4, 128), 256: H128}[page]
+    c = Cache(len(name) + page, SEQS[name], heads=heads, page=page, **mask).device()
+    check(c, c.attention(), c.oracle())
+    check(c, c.attention(dtype=torch.bfloat16, splits=5, lse=False), c.oracle())
+
+
+@pytest.mark.parametrize("heads", [H7B, H3B, (1, 1, 64), (8, 1, 64), (9, 3, 128), (40, 2, 64)], ids=str)
+def test_attention_heads(heads):
+    for seqs in ([(1, 300), (1, 35)], [(9, 60), (70, 20)]):
+        c = Cache(sum(heads), seqs, heads=heads, page=32, sink=16, window=100).device()
+        check(c, c.attention(), c.oracle())
+
+
+@pytest.mark.parametrize("splits", [1, 2, 7, 33, 64, 1000])
+def test_attention_parts(splits):
+    for seqs in ([(1, 2500), (1, 7), (1, 900)], [(9, 1500), (40, 100)]):
+        c = Cache(splits, seqs, heads=H128, page=16).device()
+        check(c, c.attention(splits=splits), c.oracle())
+
+
+@pytest.mark.parametrize("hint", [1, 100, 1 << 20])
+def test_attention_hints(hint):
+    c = Cache(7, [(1, 1300), (30, 600), (1, 2)], heads=H128, page=64).device()
+    check(c, c.attention(hint=hint), c.oracle())
+
+
+@pytest.mark.parametrize("mask", MASKS[:3], ids=str)
+def test_attention_bidirectional(mask):
+    c = Cache(11, SEQS["mixed"], heads=H128, page=32, **mask).device()
+    check(c, c.attention(flags=vico.VICO_ATTN_BIDIRECTIONAL), c.oracle(bidirectional=True))
+
+
+def test_attention_scale_and_fewer_rows():
+    c = Cache(12, SEQS["short"], heads=ODD, page=16).device()
+    check(c, c.attention(scale=0.31), c.oracle(scale=float(np.float32(0.31))))
+    check(c, c.attention(max_q=3), c.oracle(max_q=3))
+
+
+def test_attention_past_the_table():
+    # positions that the table has no entry for: their keys are not seen, their rows see the rest
+    c = Cache(13, [(20, 40), (3, 100)], heads=ODD, page=16, width=3).device()
+    check(c, c.attention(), c.oracle())
+
+
+@pytest.mark.parametrize("seqs,drop", [([(1, 100)], {(0, 0)}), ([(1, 40)], {(0, 0), (0, 1), (0, 2)}), ([(70, 90), (1, 50)], {(0, 2), (1, 1), (0, 9)}),
+                                       ([(3, 13)], {(0, 0)})], ids=str)
+def test_attention_without_some_pages(seqs, drop):
+    c = Cache(14, seqs, heads=H128, page=16, drop=drop).device()
+    check(c, c.attention(), c.oracle())
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("seqs", [[(1, 70), (2, 33)], [(9, 60)], [(150, 77)], [(300, 200), (1, 5)]], ids=str)
+def test_values_that_are_not_finite(seqs, value):
+    for mask in (dict(), dict(sink=8, window=30)):
+        c = Cache(15, seqs, heads=H128, page=16, **mask)
+        zero = []
+        for b, (n, H) in enumerate(seqs):
+            lo = H - 30 if mask else 0
+            for p in {H + n - 1, H + n // 2, max(lo, 0), H - 1}:
+                zero.append((b, p, b % 2, p % 128))
+                page, at = c.place(b, p)
+                c.v[page, at, b % 2, p % 128] = value
+        c.device()
+        ref = c.oracle(zero=zero)
+        for splits in (0, 3):
+            out, lse = c.attention(splits=splits)
+            for b, p, h, d in zero:
+                for i in range(c.n[b]):
+                    t = c.q_start[b] + i
+                    if p <= c.H[b] + i:
+                        got = out[t, 2 * h:2 * h + 2, d]
+                        assert not torch.isfinite(got).any(), (b, p, i)
+                        out[t, 2 * h:2 * h + 2, d] = torch.tensor(ref[0][t, 2 * h:2 * h + 2, d], dtype=torch.float32, device=DEV)
+            check(c, (out, lse), ref)
+
+
+def test_nan_keys_stay_in_the_rows_that_see_them():
+    c = Cache(16, [(40, 50), (1, 30)], heads=H128, page=16)
+    page, at = c.place(0, 70)
+    c.k[page, at, 0, 3] = float("nan")
+    c.device()
+    for splits in (0, 4):
+        out, lse = c.attention(splits=splits)
+        clean = Cache(16, [(40, 50), (1, 30)], heads=H128, page=16).device()
+        clean.parts = c.parts
+        ref = clean.oracle()
+        assert torch.isnan(out[20:40, :2]).all() and torch.isnan(lse[:2, 20:40]).all()
+        out[20:40, :2] = torch.tensor(ref[0][20:40, :2], dtype=torch.float32, device=DEV)
+        lse[:2, 20:40] = torch.tensor(ref[1][:2, 20:40], dtype=torch.float32, device=DEV)
+        check(c, (out, lse), ref)
+
+
+def test_large_logits():
+    c = Cache(17, [(1, 400), (37, 100)], heads=H128, page=16, sigma=40.0).device()
+    out, lse = c.attention()
+    ref = c.oracle()
+    check(c, (out, lse), ref)
+
+
+def test_arrays_that_make_no_sense_stay_in_bounds():
+    """Lengths, starts and entries outside every range: rows that exist are written, nothing faults, no other row is."""
+    c = Cache(18, [(3, 20), (4, 50)], heads=H128, page=16).device()
+    big = 2 ** 31 - 1
+    for starts in ([-5, 3, 7], [0, 100, 200], [6, 3, 1], [0, big, -big - 1]):
+        for lens in ([-4, big], [big, -big - 1]):
+            c.ds, c.dl = i32(starts), i32(lens)
+            c.attention(max_q=9)
+            k = torch.zeros(9, 2, 128, dtype=torch.bfloat16, device=DEV)
+            vico.vico_paged_append(k, k, c.ds, c.dl, c.dk, c.dv, c.dt)
+            refs = torch.ones(c.k.shape[0], dtype=torch.int32, device=DEV)
+            ws = torch.empty(vico.vico_pages_workspace_bytes(2, c.k.shape[0]), dtype=torch.uint8, device=DEV)
+            moves, granted = i32([[0, 0], [0, 0]]), i32([0, 0])
+            vico.vico_pages_reserve(c.dt.clone(), refs, c.dl, c.ds, 16, moves, granted, ws)
+            vico.vico_pages_fork(c.dt.clone(), refs, c.dl.clone(), i32([1, 0]), 16)
+            torch.cuda.synchronize()
+
+
+def test_pool_past_the_32bit_offset_limit():
+    page, Hkv, D = 1024, 4, 128                    # 1 MiB a page
+    N = 4200
+    k, v = (torch.zeros(N, page, Hkv, D, dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    ids = [4199, 3, 2101, 4100]
+    g = torch.Generator()
+    g.manual_seed(5)
+    n, H, rows = 33, 3 * page + 100, 33
+    c = Cache(19, [(1, 1)], heads=H7B, page=page)
+    c.n, c.H, c.q_start, c.width, c.page = [n], [H], [0, n], 4, page
+    c.q = (torch.randn(n, 28, D, generator=g) * 2).to(torch.bfloat16)
+    c.k, c.v = ((torch.randn(4, page, Hkv, D, generator=g) * s).to(torch.bfloat16) for s in (2.0, 1.0))
+    c.table = [[0, 1, 2, 3]]
+    new_k, new_v = (x[3, 100:100 + n].contiguous().to(DEV) for x in (c.k, c.v))
+    c.k[3, 100:], c.v[3, 100:] = 0, 0
+    pairs = [[10 + i, ids[i]] for i in range(4)]
+    for i in range(4):
+        k[10 + i], v[10 + i] = c.k[i].to(DEV), c.v[i].to(DEV)
+    vico.vico_pages_copy(k, v, i32(pairs))
+    t, s, l = i32([ids]), i32([0, n]), i32([H])
+    vico.vico_paged_append(new_k, new_v, s, l, k, v, t)
+    c.k[3, 100:100 + n], c.v[3, 100:100 + n] = new_k.cpu(), new_v.cpu()
+    c.dk, c.dv, c.dq, c.dt, c.ds, c.dl = k, v, c.q.to(DEV), t, s, l
+    rows = [0, 17, 32]
+    out, lse = c.attention()
+    ref = c.oracle(max_q=None)
+    check(c, (out, lse), ref)
+
+
+# ---------------------------------------------------------------- together
+
+class Serving:
+    """Streams, questions that branch off them, and a dense copy of every sequence's tokens to compare with."""
+
+    def __init__(self, seed, rows, page=16, N=260, width=40, heads=H128, layers=2):
+        self.rng, self.page, self.heads, self.layers, self.rows = random.Random(seed), page, heads, layers, rows
+        self.g = torch.Generator(device=DEV)
+        self.g.manual_seed(seed)
+        shape = (layers, N, page, heads[1], heads[2])
+        self.k, self.v = (torch.full(shape, float("nan"), dtype=torch.bfloat16, device=DEV) for _ in "kv")
+        self.table, self.refs = i32([[-1] * width] * rows), torch.zeros(N, dtype=torch.int32, device=DEV)
+        self.lens = torch.zeros(rows, dtype=torch.int32, device=DEV)
+        self.dense = [[torch.empty(0, 2, *heads[1:], dtype=torch.bfloat16, device=DEV) for _ in range(layers)] for _ in range(rows)]
+        self.ws = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+        self.moves, self.granted = i32([[0, 0]] * rows), i32([0] * rows)
+
+    def fork(self, parent):
+        vico.vico_pages_fork(self.table, self.refs, self.lens, i32(parent), self.page)
+        none = [x[:0] for x in self.dense[0]]
+        self.dense = [none if p < 0 else self.dense[p] for p in parent]
+
+    def step(self, n, sink=0, window=-1):
+        starts = i32(np.cumsum([0] + n).tolist())
+        vico.vico_pages_reserve(self.table, self.refs, self.lens, starts, self.page, self.moves, self.granted, self.ws)
+        vico.vico_pages_copy(self.k, self.v, self.moves)
+        assert torch.all(self.granted == 1)
+        Hq, Hkv, D = self.heads
+        total = sum(n)
+        for layer in range(self.layers):
+            q, k, v = (torch.randn(total, h, D, generator=self.g, device=DEV).to(torch.bfloat16) for h in (Hq, Hkv, Hkv))
+            vico.vico_paged_append(k, v, starts, self.lens, self.k[layer], self.v[layer], self.table)
+            out = torch.empty(total, Hq, D, dtype=torch.float32, device=DEV)
+            vico.vico_paged_attn(q, starts, self.lens, self.k[layer], self.v[layer], self.table, out, sink_len=sink,
+                                 window=window, max_q_len=max(n), workspace=self.ws)
+            at = 0
+            for b, m in enumerate(n):
+                d = torch.cat([self.dense[b][layer], torch.stack([k[at:at + m], v[at:at + m]], 1)])
+                self.dense[b] = self.dense[b][:layer] + [d] + self.dense[b][layer + 1:]
+                if m:
+                    H = d.shape[0] - m
+                    pos = torch.arange(H + m, device=DEV)
+                    seen = (pos[None] <= H + torch.arange(m, device=DEV)[:, None]) & ((pos < sink) | (pos >= H - window) if window >= 0 else pos >= 0)
+                    kk, vv = (d[:, i].double().repeat_interleave(Hq // Hkv, 1).transpose(0, 1) for i in (0, 1))
+                    z = (q[at:at + m].double().transpose(0, 1) @ kk.transpose(1, 2).contiguous()) / D ** 0.5
+                    p = torch.softmax(z.masked_fill(~seen, -torch.inf), -1)
+                    want = (p @ vv.contiguous()).transpose(0, 1)
+                    # probabilities rounded to bf16 (2^-8 of the mean |v|, at most 5 here), fp32 sums below 2^-12
+                    bound = (2.0 ** -8 + 2.0 ** -12) * (p @ vv.abs().contiguous()).transpose(0, 1) + 1e-6
+                    assert torch.all((out[at:at + m].double() - want).abs() <= bound), (b, layer)
+                at += m
+        self.lens += i32(n)
+
+    def compact(self):
+        moves, count = i32([[0, 0]] * (self.refs.shape[0] // 2)), i32([0])
+        vico.vico_pages_compact(self.table, self.refs, moves, count, self.ws)
+        vico.vico_pages_copy(self.k, self.v, moves, count=count)
+        held = self.refs > 0
+        assert torch.all(held[:int(held.sum())])
+        # what is free may hold anything
+        self.k[:, ~held], self.v[:, ~held] = float("nan"), float("nan")
+
+    def consistent(self):
+        t = self.table.flatten()
+        assert torch.equal(torch.bincount(t[t >= 0].long(), minlength=self.refs.shape[0]).int(), self.refs)
+
+
+@pytest.mark.parametrize("seed,page", [(0, 16), (1, 32), (2, 64)])
+def test_streams_and_questions(seed, page):
+    s = Serving(seed, rows=5, page=page)
+    s.step([40, 7, 0, 0, 0])
+    s.step([33, 64, 0, 0, 0])
+    s.fork([0, 1, 0, 0, 1])                 # three questions
+    s.step([0, 0, 9, 1, 20])
+    s.step([25, 0, 1, 1, 1])                # the streams go on beside the answers
+    s.consistent()
+    s.compact()
+    s.step([1, 30, 1, 0, 1])
+    s.fork([0, 1, -1, 2, 3])                # reordered, one ended
+    s.consistent()
+    s.compact()
+    s.step([3, 2, 50, 1, 4])
+    s.consistent()
+
+
+def test_a_window_that_rolls_on():
+    s = Serving(4, rows=3, page=16, N=40, width=60)
+    sink, window = 20, 50
+    for i in range(9):
+        s.step([17, 33, i], sink=sink, window=window)
+        vico.vico_pages_free(s.table, s.refs, i32([sink] * 3), s.lens - window, 16)
+        s.consistent()
+        if i % 4 == 3:
+            s.compact()
+    assert int((s.refs > 0).sum()) <= 3 * 7
+
+
+def capture(f):
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        f()
+    return g
+
+
+def test_a_step_replays_as_a_graph():
+    c = Cache(21, [(1, 90), (150, 77), (1, 1)], heads=H128, page=16, sink=8, window=60).device()
+    eager = c.attention()
+    out, lse = torch.zeros_like(eager[0]), torch.zeros_like(eager[1])
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+    k, v = (torch.randn(c.q.shape[0], 2, 128, device=DEV).to(torch.bfloat16) for _ in "kv")
+    wb = vico.vico_pages_workspace_bytes(3, c.k.shape[0])
+    refs = torch.ones(c.k.shape[0], dtype=torch.int32, device=DEV)
+    moves, granted, parent, count = i32([[0, 0]] * 40), i32([0] * 3), i32([0, 0, -1]), i32([0])
+    table, lens, zero = c.dt.clone(), c.dl.clone(), i32([0] * 3)
+
+    def body():
+        vico.vico_paged_append(k, v, c.ds, c.dl, c.dk, c.dv, c.dt)
+        vico.vico_paged_attn(c.dq, c.ds, c.dl, c.dk, c.dv, c.dt, out, lse=lse, sink_len=8, window=60, max_q_len=150, workspace=ws)
+        vico.vico_pages_fork(table, refs, lens, parent, 16)
+        vico.vico_pages_free(table, refs, zero, lens, 16)
+        vico.vico_pages_reserve(table, refs, lens, c.ds, 16, moves[:3], granted, ws[:wb])
+        vico.vico_pages_compact(table, refs, moves, count, ws[:wb])
+        vico.vico_pages_copy(c.dk, c.dv, moves[:3], count=zero[:1])
+
+    state = [t.clone() for t in (table, refs, lens, c.dk, c.dv)]
+
+    def reset():
+        for t, s in zip((table, refs, lens, c.dk, c.dv), state):
+            t.copy_(s)
+        out.zero_()
+        torch.cuda.synchronize()
+
+    def result():
+        torch.cuda.synchronize()
+        return [t.clone() for t in (out, lse, table, refs, lens, moves, granted, count)] + [bits(c.dk).clone(), bits(c.dv).clone()]
+
+    body()
+    want = result()
+    reset()
+    g = capture(body)
+    for i in range(4):
+        reset()
+        g.replay()
+        for x, y in zip(result(), want):
+            assert torch.equal(torch.nan_to_num(x.float()), torch.nan_to_num(y.float()))
+        c.attention()                               # eager work between the replays
+
+
+def test_on_another_stream_and_twice_at_once():
+    a = Cache(22, [(1, 900), (40, 100)], heads=H128, page=16).device()
+    b = Cache(23, [(1, 700), (1, 40), (9, 300)], heads=H128, page=64).device()
+    ra, rb = a.oracle(), b.oracle()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    check(a, a.attention(stream=s), ra)
+    bufs = []
+    torch.cuda.synchronize()
+    for c, st in ((a, s), (b, t), (a, s), (b, t)):
+        rows = c.q.shape[0]
+        out, ws = torch.full((rows, c.Hq, c.D), 7.25, device=DEV), torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+        bufs.append((c, out, ws))
+    torch.cuda.synchronize()
+    for (c, out, ws), st in zip(bufs, (s, t, s, t)):
+        vico.vico_paged_attn(c.dq, c.ds, c.dl, c.dk, c.dv, c.dt, out, max_q_len=max(c.n), num_splits=4, workspace=ws, stream=st)
+    torch.cuda.synchronize()
+    for (c, out, _), ref in zip(bufs, (ra, rb, ra, rb)):
+        ref[3].parts = 4
+        check(c, (out, None), ref)
+
+
+def test_results_repeat():
+    c = Cache(24, [(1, 3000), (70, 500), (1, 80)], heads=H7B, page=16).device()
+    first = c.attention(dtype=torch.bfloat16)
+    for _ in range(3):
+        again = c.attention(dtype=torch.bfloat16)
+        assert torch.equal(bits(first[0]), bits(again[0])) and torch.equal(first[1], again[1])

@@ -31,7 +31,7 @@ def test_header_functions_are_exported_and_bound():
 
 TABLE_SIZES = [(dict(B=-1), -1), (dict(B=4097), -1), (dict(width=-1), -1), (dict(N=-1), -1), (dict(N=(1 << 21) + 1), -1),
                (dict(B=4096, width=1 << 19), -1)]
-PAGE_SIZES = [(dict(page=p), -1) for p in (0, 8, 24, 48, 2048, -16)] + [(dict(width=1 << 25, B=1), -1)]
+PAGE_SIZES = [(dict(page=p), -1) for p in (0, 8, 24, 48, 2048, -16)] + [(dict(width=(1 << 26) + 1, B=1), -1)]
 
 
 def _append(**kw):

@@ -1,0 +1,501 @@
+// Attention over the cache in pages, many query rows a sequence (gfx950): what
+// attn_rows_pages.hip computes, for sequences whose rows share every key often
+// enough to be bound by the matrix cores -- visual chunks, long queries.
+//
+// A work-group of 8 waves owns 256 packed (token, query head) rows of one KV head of
+// one sequence, 32 a wave, and walks 64-key tiles of its visible positions; the tile
+// body is PipeTile (attn_pipe.h), the software-pipelined one of the chunk prefill,
+// with K and V loaded straight to LDS three tiles ahead and one barrier a tile.
+//   * Tiles are aligned to positions, and a wave's share of a tile is 8 consecutive
+//     rows: they lie in one page whatever its size (16 tokens at least).  So a page
+//     costs a wave one number and two buffer resources a tile, all scalar.  A resource
+//     ends behind the last row that exists: rows past the sequence, and rows of a page
+//     that is none, read as zeros.
+//   * The page numbers of the part's tiles are in LDS, checked, two halves in turn: one
+//     is filled while the other is read, in the middle of it, so that no wait or
+//     barrier of its own is needed.
+//   * Between sink and window nothing is walked; rows that no row of the sequence sees in
+//     the two tiles there are read from outside the resource, as zeros.
+//   * Values that are not finite in tiles that the causal mask cuts are zeros in LDS (0
+//     times such a value would reach rows that do not see it) and are added afterwards for
+//     the rows that do.  Each wave looks at what it loaded, before the barrier that
+//     shows it to the others.
+// Which sequences these are stands in device memory, so every work-group counts the
+// row tiles of all sequences and finds its own; where they leave CUs idle, key ranges
+// are split and joined by the merge kernel.
+
+#include "attn_pipe.h"
+#include "pages.h"
+#include "values.h"
+
+namespace vico {
+namespace {
+
+typedef const __attribute__((address_space(4))) PagedAttnArgs* late_args;
+// the kernel's arguments, read again where they are used: what only the start and the end need takes no registers
+// in the loop
+__device__ __forceinline__ late_args late() {
+  late_args p = (late_args)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
+// Row tiles of sequence b on this kernel.
+__device__ __forceinline__ int row_tiles(const PagedAttnArgs& a, int b) {
+  int q0;
+  const int rows = a.Hq / a.Hkv * min(rows_of(a, b, q0), a.max_q);
+  return rows > a.rows_most ? (rows + kBlockM - 1) / kBlockM : 0;
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    x += lane >= o ? y : 0;
+  }
+  return x;
+}
+// Row tiles of all sequences, and the parts that their key ranges are split into.
+__device__ __forceinline__ int all_row_tiles(const PagedAttnArgs& a, int& parts) {
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+  for (int b = lane; b < a.B; b += 64) n += row_tiles(a, b);
+  n = __builtin_amdgcn_readlane(wave_scan(n), 63);
+  const int items = n * a.Hkv;
+  parts = a.tile_splits > 0 ? a.tile_splits : items > 0 ? min(max(a.tile_slots / items, 1), a.tile_parts) : 1;
+  return items;
+}
+// The sequence whose row tiles, each `times` times, hold item x; its first item and its row tiles.
+__device__ __forceinline__ int sequence_of_item(const PagedAttnArgs& a, int x, int times, int& first, int& tiles) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b0 = 0;; b0 += 64) {
+    const int n = b0 + lane < a.B ? row_tiles(a, b0 + lane) : 0;
+    const int upto = before + wave_scan(n) * times;
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    if (x < all || b0 + 64 >= a.B) {
+      const int i = min(__builtin_popcountll(__builtin_amdgcn_ballot_w64(upto <= x)), 63);
+      tiles = __builtin_amdgcn_readlane(n, i);
+      first = __builtin_amdgcn_readlane(upto, i) - tiles * times;
+      return b0 + i;
+    }
+    before = all;
+  }
+}
+
+constexpr int kTabHalf = 1024;             // page numbers of a half of the table in LDS
+
+template <int D>
+__global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAttnArgs a) {
+  constexpr int RB = 1;
+  typedef PipeTile<D, RB> Tile;
+  constexpr int BN = kKeyTile, BM = kBlockM, NW = kThreads / 64;
+  constexpr int RBY = D * 2;                 // bytes per LDS row
+  constexpr uint32_t TBY = BN * RBY;         // bytes of one K (or V) tile
+  constexpr int NLD = TBY / 1024 / NW;       // direct 1 KiB loads a wave and tile, of K and of V
+  constexpr int RPL = Tile::RPC;             // rows of one
+  constexpr int NDB = Tile::NDB, NKS = Tile::NKS;
+  constexpr int NB = kBuffers, AHEAD = NB - 1;
+  constexpr uint32_t kKBase = NB * TBY, kWrap = NB * TBY - 1;
+  constexpr int NL = 2 * NLD, LSTEP = (Tile::NSLOT - 2) / (NL + 1);
+  static_assert(NLD * NW * 1024 == TBY && BN == 64 && NLD * RPL == 8, "a wave loads 8 rows of a tile");
+  static_assert(BM == NW * 32 && RB == kRowBlocks && (NB & (NB - 1)) == 0 && LSTEP >= 1, "tile geometry");
+  typedef __attribute__((address_space(3))) u32x4* lds_u4;
+
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * NB * TBY];
+  __shared__ int32_t tab[2 * kTabHalf];
+  __shared__ int odd_s;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, hh = lane >> 5;
+  const int g = a.Hq / a.Hkv;
+
+  // ---- work item: the row tiles of one key range side by side (they share its K/V in an XCD's L2), longest first
+  int parts;
+  const int items = all_row_tiles(a, parts), n_work = items * parts;
+  // (starts that decrease may count rows twice: more partial results than there is room for)
+  if ((int)blockIdx.x >= n_work || (parts > 1 && n_work > a.tile_slots)) return;
+  const int L = xcd_remap(blockIdx.x, n_work);
+  int first_item, cnt;
+  const int b = __builtin_amdgcn_readfirstlane(sequence_of_item(a, L, a.Hkv * parts, first_item, cnt));
+  const int kp = (L - first_item) / cnt, rt = cnt - 1 - (L - first_item - kp * cnt);
+  const int kv = kp / parts, part = kp - kv * parts;
+  if (tid == 0) odd_s = 0;
+
+  // (in scalar registers, whatever the compiler makes of loads whose address it cannot prove to be the same in all lanes:
+  // no branch of the key loop may be on lanes)
+  Sequence s = sequence(a, b);
+  s.q0 = __builtin_amdgcn_readfirstlane(s.q0);
+  s.n = __builtin_amdgcn_readfirstlane(s.n);
+  s.H = __builtin_amdgcn_readfirstlane(s.H);
+  s.sink = __builtin_amdgcn_readfirstlane(s.sink);
+  s.first = __builtin_amdgcn_readfirstlane(s.first);
+  const int NR = g * s.n;
+  const KeyBlocks<BN> tiles(s);
+  auto lim_of_row = [&](int r) __attribute__((always_inline)) { return last_position(a, s, a.by_g(min(r, NR - 1))); };
+
+  // ---- this lane's packed row; rows past the end repeat the last one and are never stored
+  const int wrow0 = rt * BM + wave * 32;
+  const bool wave_active = wrow0 < NR;
+  const int my_row = min(wrow0 + l32, NR - 1);
+  const int tok = a.by_g(my_row), head = kv * g + my_row - tok * g;
+  const int lim = last_position(a, s, tok);                        // the row's last position
+  bf16x8 qf[RB][NKS];
+  WaveTile<D>::load_q(qf[0], a.q + ((int64_t)(s.q0 + tok) * a.Hq + head) * D + hh * 8);
+
+  // ---- tiles
+  const int first_lim = lim_of_row(wrow0), last_lim = lim_of_row(wrow0 + 31);
+  const int n_tiles = tiles.upto(lim_of_row((rt + 1) * BM - 1));
+  const int t_lo = (int)((int64_t)n_tiles * part / parts), t_hi = (int)((int64_t)n_tiles * (part + 1) / parts);
+  const int t_end = wave_active ? min(t_hi, tiles.upto(last_lim)) : t_lo;          // past the wave's last tile
+  const int kv_end = lim_of_row(NR - 1) + 1;                       // rows of the sequence that exist
+  const int cut_from = lim_of_row(rt * BM) + 1;                    // from here on some row of the work-group sees not all
+  const int sink = s.sink, first = s.first;
+  auto gap = [&](int p0) __attribute__((always_inline)) { return p0 + BN > sink && p0 < first; };
+
+  // ---- page numbers: entry (t - t_lo) * EPT + e of the part's tile t, in tab at that number mod 2 * kTabHalf
+  const int shift = a.page_shift;
+  const int ept_shift = shift < 6 ? 6 - shift : 0;                 // 64 / page_size pages a tile, or one
+  const int32_t* const row = a.table + (int64_t)b * a.width;
+  const int n_entries = (t_hi - t_lo) << ept_shift;
+  bool holes = false;
+  auto fill_tab = [&](int e0) __attribute__((always_inline)) {     // entries e0 .. e0 + kTabHalf - 1, without a branch
+#pragma unroll
+    for (int i = 0; i < kTabHalf / kThreads; ++i) {                // on lanes (past the last one: anything)
+      const int e = e0 + i * kThreads + tid, in = min(e, n_entries - 1);
+      const int p0 = tiles.position(t_lo + (in >> ept_shift)) + ((in & ((1 << ept_shift) - 1)) << (shift < 6 ? shift : 0));
+      const int at = p0 >> shift;
+      const int p = row[min(at, a.width - 1)];
+      tab[e & (2 * kTabHalf - 1)] = at < a.width && (uint32_t)p < (uint32_t)a.N ? p : -1;
+    }
+  };
+
+  // ---- tile loader
+  const int rbytes = a.Hkv * D * 2;
+  const int64_t pbytes = (int64_t)rbytes << shift;
+  const uint32_t my_part = (uint32_t)(wave * NLD * 1024);
+  uint32_t ld_k[NLD], ld_v;                                        // byte offsets from the wave's first row
+  {
+    int r, u;
+#pragma unroll
+    for (int n = 0; n < NLD; ++n) {
+      Tile::k_source(wave * NLD + n, lane, r, u);
+      ld_k[n] = (uint32_t)((n * RPL + r) * rbytes + u * 16);
+    }
+    Tile::v_source(lane, r, u);
+    ld_v = (uint32_t)(r * rbytes + u * 16);
+  }
+  u32x4 run_k, run_v;                        // resources of the wave's rows of the tile to be loaded
+  int run_p0 = 0;
+  bool run_gap = false;
+  auto start_tile = [&](int t) __attribute__((always_inline)) {
+    uint32_t bytes = 0;
+    int64_t at = 0;
+    if (t < t_hi) {
+      const int e0 = (t - t_lo) << ept_shift;
+      const int mine = tab[(e0 + (lane & ((1 << ept_shift) - 1))) & (2 * kTabHalf - 1)];
+      holes |= __builtin_amdgcn_ballot_w64(mine < 0) != 0;
+      const int page = __builtin_amdgcn_readlane(mine, shift < 6 ? (8 * wave) >> shift : 0);
+      run_p0 = __builtin_amdgcn_readfirstlane(tiles.position(t)) + 8 * wave;
+      const int rows = page < 0 ? 0 : min(max(kv_end - run_p0, 0), 8);
+      bytes = rows > 0 ? (uint32_t)((rows - 1) * rbytes + RBY) : 0;
+      at = max(page, 0) * pbytes + (run_p0 & ((1 << shift) - 1)) * rbytes + kv * RBY;
+      run_gap = run_p0 + 8 > sink && run_p0 < first;
+    }
+    const uint64_t pk = (uint64_t)a.k_pages + at, pv = (uint64_t)a.v_pages + at;
+    const uint32_t n = __builtin_amdgcn_readfirstlane(bytes);
+    run_k = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)pk), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(pk >> 32)) & 0xFFFFu, n, 0x00020000u};
+    run_v = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)pv), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(pv >> 32)) & 0xFFFFu, n, 0x00020000u};
+  };
+  // direct load i (0 .. NLD-1: K, NLD .. 2*NLD-1: V) to the buffers at byte offset `boff`.  m0, which holds a load's
+  // LDS address, is the compiler's own: every load sets it and gives it back.  Wait states that the compiler does not
+  // know assembly to need: one after a write of m0, five after a VALU write of a scalar operand.
+  auto load_direct = [&](auto idx, uint32_t boff) __attribute__((always_inline)) {
+    constexpr int i = decltype(idx)::value, n = i % NLD;
+    uint32_t off = i < NLD ? ld_k[n] : ld_v + n * RPL * rbytes;
+    if (__builtin_expect(run_gap, 0)) {      // rows that nobody sees: from outside the resource
+      int r, u;
+      if constexpr (i < NLD) Tile::k_source(wave * NLD + n, lane, r, u);
+      else Tile::v_source(lane, r, u);
+      const int p = run_p0 + n * RPL + r;
+      off = p >= sink && p < first ? kOutOfRange : off;
+    }
+    const uint32_t to = lds0 + my_part + boff + (i < NLD ? kKBase : 0u) + n * 1024;
+    const u32x4 rs = i < NLD ? run_k : run_v;
+    uint32_t m0;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 4\n\t"
+        "buffer_load_dwordx4 %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0"
+        : "=&s"(m0)
+        : "v"(off), "s"(rs), "s"(to)
+        : "memory");
+  };
+  auto load_whole = [&](uint32_t boff, int t) __attribute__((always_inline)) {
+    start_tile(t);
+    unrolled<NL>([&](auto i) __attribute__((always_inline)) { load_direct(i, boff); });
+  };
+
+  // ---- the wave's share of V of tile t, landed at `boff`: what is not finite becomes zero where the mask cuts
+  bool odd = false;
+  auto look = [&](int t, uint32_t boff) __attribute__((always_inline)) {
+    if (__builtin_expect(t < t_hi && tiles.position(t) + BN > cut_from, 0)) {
+      const uint32_t at = lds0 + boff + my_part + (uint32_t)(lane * 16);
+#pragma unroll
+      for (int n = 0; n < NLD; ++n) {
+        u32x4 y = *(lds_u4)(uintptr_t)(at + n * 1024);
+        u16x2 most{0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          largest_exponents(most, y[i]);
+          y[i] = finite_or_zero(y[i]);
+        }
+        odd |= not_finite(most);
+        *(lds_u4)(uintptr_t)(at + n * 1024) = y;
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  };
+  // tile t has landed (the loads of the AHEAD - 2 tiles after it may be in flight), for this wave and every other
+  auto landed = [&](int t, uint32_t boff) __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 2) * NL) : "memory");
+    look(t, boff);
+    barrier_keep_loads();
+  };
+  // what the mask takes from a half of tile t, whose keys start at position p0
+  auto mask = [&](int t, int p0, f32x16& x) __attribute__((always_inline)) {
+    const int e0 = (t - t_lo) << ept_shift, per = shift < 6 ? shift : 6;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int at = 8 * (v >> 2) + hh * 4 + (v & 3), p = p0 + at;
+      const bool none = p > lim || (p >= sink && p < first);
+      x[v] = none ? -INFINITY : x[v];
+    }
+    if (__builtin_expect(holes, 0)) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {          // eight keys lie in one page
+        const int in_tile = ((p0 & 32) | (8 * q)) >> per;
+        const bool none = tab[(e0 + in_tile) & (2 * kTabHalf - 1)] < 0;
+#pragma unroll
+        for (int v = 4 * q; v < 4 * q + 4; ++v) x[v] = none ? -INFINITY : x[v];
+      }
+    }
+  };
+
+  f32x16 o[RB][NDB];
+  float m_run[RB] = {-INFINITY}, l_run[RB] = {0.f}, neg_m[RB] = {INFINITY};
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) o[0][db] = f32x16{};
+  uint32_t k_rd[2], v_rd, v_nx;
+  Tile::start(k_rd, v_nx);
+  k_rd[0] += lds0 + kKBase;                  // the part's first tile: buffer 0
+  k_rd[1] += lds0 + kKBase;
+  v_nx += lds0;
+  v_rd = v_nx + (NB - 1) * TBY;
+  if (t_lo < t_hi) {
+    fill_tab(0);
+    fill_tab(kTabHalf);
+    // the pipeline's first P V multiplies zero probabilities with the last 16 rows of the last V buffer: any bits
+    // there must be finite
+    if (tid < RBY) *(lds_u4)(uintptr_t)(lds0 + (NB - 1) * TBY + 48 * RBY + tid * 16) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < AHEAD; ++i) load_whole(i * TBY, t_lo + i);
+    start_tile(t_lo + AHEAD);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * NL) : "memory");      // tile t_lo
+    look(t_lo, 0);
+    barrier_keep_loads();
+    // the half of the table that is not in use is filled for its next turn as the loads pass the middle of the other
+    auto more_tab = [&](int t) __attribute__((always_inline)) {
+      const int e = (t - t_lo) << ept_shift;
+      if (__builtin_expect((e & (kTabHalf - 1)) == kTabHalf / 2 && e > kTabHalf, 0)) fill_tab(e - kTabHalf / 2 + kTabHalf);
+    };
+    uint32_t boff = 0;                       // buffer offset of tile t
+    int t = t_lo;
+    if (t < t_end) {
+      bf16x8 vf[NDB] = {};
+      Tile wt{qf, k_rd, v_rd, v_nx, o, m_run, l_run, neg_m, vf, a.scale_log2};
+      f32x16 s0[RB], s1[RB];
+      bf16x8 p0[RB][2] = {}, p1[RB][2] = {};
+      // tiles that some lane's row does not see whole: mask them
+      auto cut = [&](int pos) __attribute__((always_inline)) { return pos + BN - 1 > first_lim || gap(pos) || holes; };
+      wt.first_logits(s0);
+      {
+        const int pos = tiles.position(t);
+        if (cut(pos)) mask(t, pos, s0[0]);
+      }
+      wt.first_max(s0);
+      for (; t < t_end; ++t) {
+        const int pos = tiles.position(t);
+        const bool masked = cut(pos);
+        if (__builtin_expect(masked, 0)) mask(t, pos, s0[0]);
+        uint32_t next = 0;                   // of tile t + 1
+        wt.template half<32, 48, 0>(s0, s1, p1, p0, [&](auto slot) __attribute__((always_inline)) {
+          constexpr int i = decltype(slot)::value;
+          if constexpr (i == Tile::NQK + Tile::NPV) {
+            next = (boff + TBY) & kWrap;
+            k_rd[0] += next - boff;          // K of tile t + 1
+            k_rd[1] += next - boff;
+            v_rd = v_nx;                     // V of tile t
+          }
+        });
+        landed(t + 1, next);
+        if (__builtin_expect(masked, 0)) mask(t, pos + 32, s1[0]);
+        const uint32_t fill = (boff + AHEAD * TBY) & kWrap;
+        wt.template half<0, 16, 32>(s1, s0, p0, p1, [&](auto slot) __attribute__((always_inline)) {
+          constexpr int j = decltype(slot)::value, i = j / LSTEP - 1;
+          if constexpr (j % LSTEP == 0 && i >= 0 && i < NL) load_direct(std::integral_constant<int, i>{}, fill);
+        });
+        v_nx += next - boff;                 // V of tile t + 1
+        boff = next;
+        more_tab(t + AHEAD);
+        start_tile(t + AHEAD + 1);
+      }
+      wt.template last_values<48>(p1);
+    }
+    for (; t < t_hi; ++t) {                  // tiles that this wave's rows do not see: it brings its share
+      const uint32_t next = (boff + TBY) & kWrap;
+      landed(t + 1, next);
+      unrolled<NL>([&](auto i) __attribute__((always_inline)) { load_direct(i, (boff + AHEAD * TBY) & kWrap); });
+      boff = next;
+      more_tab(t + AHEAD);
+      start_tile(t + AHEAD + 1);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the empty loads past the last tile
+  }
+
+  // ---- values of the cut tiles that are not finite
+  if (odd) odd_s = 1;
+  __syncthreads();
+  if (!wave_active) return;
+  const late_args l = late();
+  if (__builtin_expect(odd_s != 0, 0)) {
+    for (int t = t_lo; t < t_hi; ++t) {
+      const int pos = tiles.position(t);
+      if (pos + BN <= cut_from) continue;
+      for (int p = pos; p <= min(pos + BN - 1, last_lim); ++p) {
+        const int page = row[p >> shift];
+        if ((uint32_t)page >= (uint32_t)a.N || (p >= sink && p < first)) continue;
+        const uint16_t* v0 = l->v_pages + ((((int64_t)page << shift) + (p & ((1 << shift) - 1))) * a.Hkv + kv) * D + hh * 4;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const uint32_t bits = (uint32_t)v0[db * 32 + (v >> 2) * 8 + (v & 3)] << 16;
+            o[0][db][v] += (p <= lim && (bits & 0x7F800000u) == 0x7F800000u) ? __uint_as_float(bits) : 0.f;
+          }
+      }
+    }
+  }
+
+  const float l_tot = pair_sum(l_run[0]);
+  const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == l_tot ? 0.f : l_tot;        // 0 for an empty row, NaN stays
+  const float lse2 = l_tot > 0.f ? m_run[0] + __log2f(l_tot) : l_tot == l_tot ? -INFINITY : l_tot;
+  if (wrow0 + l32 >= NR) return;
+  const bool partial = parts > 1;
+  const int64_t prow = (int64_t)L * BM + wave * 32 + l32;
+  if (partial || l->out_f32) {
+    float* op = partial ? l->ws_o + prow * D : (float*)l->out + ((int64_t)(s.q0 + tok) * l->Hq + head) * D;
+    op += hh * 4;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const f32x16& x = o[0][db];
+        *(f32x4*)(op + db * 32 + q4 * 8) =
+            f32x4{x[q4 * 4] * inv, x[q4 * 4 + 1] * inv, x[q4 * 4 + 2] * inv, x[q4 * 4 + 3] * inv};
+      }
+  } else {
+    __bf16* op = (__bf16*)l->out + ((int64_t)(s.q0 + tok) * l->Hq + head) * D + hh * 4;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const f32x16& x = o[0][db];
+        *(bf16x4*)(op + db * 32 + q4 * 8) = bf16x4{(__bf16)(x[q4 * 4] * inv), (__bf16)(x[q4 * 4 + 1] * inv),
+                                                   (__bf16)(x[q4 * 4 + 2] * inv), (__bf16)(x[q4 * 4 + 3] * inv)};
+      }
+  }
+  if (hh != 0) return;
+  if (partial) l->ws_lse[prow] = lse2;
+  else if (l->lse) l->lse[(int64_t)head * l->total + s.q0 + tok] = lse2 * kLn2;
+}
+
+// The parts of a row tile joined, as in attn_rows_pages.hip: one thread takes four columns of a row, all parts' loads
+// together.
+constexpr int kMergeThreads = 256;
+template <int D, int NP>
+__device__ __forceinline__ f32x4 joined(const PagedAttnArgs& a, int64_t row0, int64_t step, int parts, int dq, float& lse2) {
+  float ls[NP];
+  f32x4 os[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {             // past the last part: the last one again, left out below
+    const int64_t at = row0 + min(i, parts - 1) * step;
+    ls[i] = i < parts ? a.ws_lse[at] : -INFINITY;
+    os[i] = *(const f32x4*)(a.ws_o + at * D + dq * 4);
+  }
+  float m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) m = fmaxf(m, ls[i]);
+  const float use = m == -INFINITY ? 0.f : m;
+  float sum = 0.f;
+  f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const float w = __builtin_amdgcn_exp2f(ls[i] - use);
+    sum += w;
+    acc += ls[i] == -INFINITY ? f32x4{0.f, 0.f, 0.f, 0.f} : w * os[i];
+  }
+  acc *= sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
+  lse2 = sum > 0.f ? use + __log2f(sum) : sum == sum ? -INFINITY : sum;
+  return acc;
+}
+
+template <int D>
+__global__ __launch_bounds__(kMergeThreads) void paged_tile_merge_kernel(PagedAttnArgs a) {
+  constexpr int NQ = D / 4, RPB = kMergeThreads / NQ, CH = kBlockM / RPB;
+  int parts;
+  const int items = all_row_tiles(a, parts);
+  const int it = blockIdx.x / CH;
+  if (parts == 1 || it >= items || items * parts > a.tile_slots) return;
+  int first_item, cnt;
+  const int b = sequence_of_item(a, it, a.Hkv, first_item, cnt);
+  const int kv = (it - first_item) / cnt, rt = it - first_item - kv * cnt;
+  const int r = (int)(blockIdx.x - it * CH) * RPB + threadIdx.x / NQ, dq = threadIdx.x % NQ;
+  const Sequence s = sequence(a, b);
+  const int g = a.Hq / a.Hkv, pr = rt * kBlockM + r;
+  if (pr >= g * s.n) return;
+  const int64_t row0 = ((int64_t)first_item * parts + (int64_t)kv * parts * cnt + cnt - 1 - rt) * kBlockM + r;
+  const int64_t step = (int64_t)cnt * kBlockM;
+  float lse2;
+  f32x4 acc;
+  if (parts <= 2) acc = joined<D, 2>(a, row0, step, parts, dq, lse2);
+  else if (parts <= 4) acc = joined<D, 4>(a, row0, step, parts, dq, lse2);
+  else if (parts <= 8) acc = joined<D, 8>(a, row0, step, parts, dq, lse2);
+  else acc = joined<D, 16>(a, row0, step, parts, dq, lse2);
+  const int t = a.by_g(pr), h = kv * g + pr - t * g;
+  const int64_t orow = (int64_t)(s.q0 + t) * a.Hq + h;
+  if (a.out_f32) *(f32x4*)((float*)a.out + orow * D + dq * 4) = acc;
+  else *(bf16x4*)((__bf16*)a.out + orow * D + dq * 4) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
+  if (dq == 0 && a.lse) a.lse[(int64_t)h * a.total + s.q0 + t] = lse2 * kLn2;
+}
+
+template <int D>
+hipError_t launch(const PagedAttnArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(paged_tile_kernel<D>, dim3((unsigned)a.tile_grid), dim3(kThreads), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.ws_o) return e;
+  constexpr int chunks = kBlockM / (kMergeThreads / (D / 4));
+  hipLaunchKernelGGL(paged_tile_merge_kernel<D>, dim3((unsigned)a.tile_items * chunks), dim3(kMergeThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_tile(const PagedAttnArgs& a, hipStream_t stream) {
+  if (a.tile_grid < 1 || a.tile_splits > kPagedTileParts) return hipErrorInvalidValue;
+  return a.D == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
+}
+
+}  // namespace vico

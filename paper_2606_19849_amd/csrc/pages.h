@@ -85,8 +85,9 @@ struct PagedAttnArgs {
   int rows_most;            // packed rows of a sequence up to which the rows kernel takes it
   int n_rt, row_blocks;     // rows kernel: row tiles of 16 * row_blocks rows of a sequence
   int parts, per_part;      // rows kernel: parts at most, 32-key blocks of a part at least
-  int tile_slots;           // 256-row kernel: work-groups that share the key ranges
-  int tile_splits;          // its parts: 0: those that fill the slots
+  // 256-row kernel: its launch, the row tiles of all heads that may be split, partial results that there is room for,
+  // and parts: the caller's (0: as many as fill the room), or at most
+  int tile_grid, tile_items, tile_slots, tile_splits, tile_parts;
   FastDiv by_g, by_rt, by_parts, by_kv;
 };
 hipError_t launch_paged_rows(const PagedAttnArgs& a, hipStream_t stream);

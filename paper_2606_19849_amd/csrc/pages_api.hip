@@ -64,13 +64,15 @@ void use_workspace(PagesArgs* a, void* workspace) {
 }
 
 // ---- attention: which sequences take which kernel, and how their keys are split.
-constexpr int kPagedRowsMost = 1 << 30;
+constexpr int kPagedRowsMost = 128;      // packed rows of a KV head up to which the rows kernel takes a sequence
 
 struct PagedPlan {
-  int rows_most, n_rt, row_blocks, parts, per_part;
   bool rows, tile;
+  int n_rt, row_blocks, parts, per_part;
+  int tile_grid, tile_items, tile_slots, tile_parts, tile_splits;
   int64_t rows_ws, ws_bytes;
 };
+int64_t partial_bytes(int64_t slots, int64_t rows, int64_t D) { return align256(slots * rows * D * 4) + align256(slots * rows * 4); }
 
 int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size, int32_t width, int32_t S, int64_t W,
                       int64_t hint, int32_t Hq, int32_t Hkv, int32_t D, int32_t splits, PagedPlan* pl) {
@@ -85,9 +87,8 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
   const int64_t cap = int64_t(width) * page_size, rows = int64_t(g) * n;
   int64_t keys = std::min(hint > 0 ? hint : cap, cap);
   if (W != VICO_FULL_HISTORY) keys = std::min(keys, S + W + n);
-  pl->rows_most = kPagedRowsMost;
   pl->rows = true;
-  const int64_t few = std::min<int64_t>(rows, pl->rows_most);
+  const int64_t few = std::min<int64_t>(rows, kPagedRowsMost);
   pl->row_blocks = few > 16 ? 2 : 1;
   pl->n_rt = (int)((few + 16 * pl->row_blocks - 1) / (16 * pl->row_blocks));
   const int64_t groups = int64_t(B) * Hkv * pl->n_rt, blocks = keys / kRowsBlock + 1;
@@ -96,8 +97,26 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
                          : (int)std::max<int64_t>(std::min(std::min<int64_t>(kPagedParts, target / groups), blocks / 8), 1);
   if (groups * pl->parts > kMaxKeys) return VICO_ERR_INVALID_ARG;
   pl->per_part = splits > 0 ? 1 : (int)((blocks + pl->parts - 1) / pl->parts);
-  if (pl->parts > 1) pl->rows_ws = align256(groups * pl->parts * 16 * pl->row_blocks * D * 4) + align256(groups * pl->parts * 16 * pl->row_blocks * 4);
+  if (pl->parts > 1) pl->rows_ws = partial_bytes(groups * pl->parts, 16 * pl->row_blocks, D);
   pl->ws_bytes = pl->rows_ws;
+  if (rows <= kPagedRowsMost) return VICO_OK;
+  // row tiles of 256: of a sequence its rows rounded up, and such a sequence has more than kPagedRowsMost
+  const int64_t all = int64_t(total) * g;
+  const int64_t items = Hkv * (all / kBlockM + std::min<int64_t>(B, all / (kPagedRowsMost + 1)));
+  pl->tile = true;
+  pl->tile_splits = std::min(splits, kPagedTileParts);
+  pl->tile_parts = (int)std::max<int64_t>(std::min<int64_t>(kPagedTileParts, keys / kKeyTile / kMinSplitTiles), 1);
+  if (splits > 0) {
+    pl->tile_slots = (int)std::min<int64_t>(items * pl->tile_splits, kMaxKeys);
+    pl->tile_grid = pl->tile_slots;
+    pl->tile_items = (int)std::min<int64_t>(items, kMaxKeys);
+  } else {
+    pl->tile_slots = kNumCUs;
+    pl->tile_grid = (int)std::max<int64_t>(items, kNumCUs);
+    pl->tile_items = (int)std::min<int64_t>(items, kNumCUs / 2);
+  }
+  if (items * std::max(pl->tile_splits, 1) * (kBlockM / 8) > kMaxKeys) return VICO_ERR_INVALID_ARG;
+  if (splits > 1 || (splits == 0 && pl->tile_parts > 1)) pl->ws_bytes += partial_bytes(pl->tile_slots, kBlockM, D);
   return VICO_OK;
 }
 
@@ -142,7 +161,7 @@ int vico_paged_attn_plan(int32_t num_seqs, int32_t total_q, int32_t max_q_len, i
   const int st = check_paged_shape(num_seqs, total_q, max_q_len, page_size, max_pages, sink_len, window, keys_hint,
                                    num_q_heads, num_kv_heads, head_dim, num_splits, &pl);
   if (st != VICO_OK) return st;
-  if (num_splits_out) *num_splits_out = std::max(pl.parts, 1);
+  if (num_splits_out) *num_splits_out = std::max(std::max(pl.parts, pl.tile_splits), pl.tile && num_splits == 0 ? pl.tile_parts : 1);
   if (workspace_bytes_out) *workspace_bytes_out = pl.ws_bytes;
   return VICO_OK;
 }
@@ -188,7 +207,7 @@ int vico_paged_attn(const void* q, const int32_t* q_start, const int32_t* seq_le
   a.out_f32 = out_dtype == VICO_DTYPE_F32;
   const double scale = softmax_scale > 0.f ? double(softmax_scale) : 1.0 / sqrt(double(head_dim));
   a.scale_log2 = (float)(scale * 1.4426950408889634);
-  a.rows_most = pl.rows_most; a.n_rt = pl.n_rt; a.row_blocks = pl.row_blocks;
+  a.rows_most = kPagedRowsMost; a.n_rt = pl.n_rt; a.row_blocks = pl.row_blocks;
   a.parts = pl.parts; a.per_part = pl.per_part;
   a.by_g = FastDiv::by(a.Hq / a.Hkv);
   a.by_kv = FastDiv::by(a.Hkv);
@@ -201,6 +220,16 @@ int vico_paged_attn(const void* q, const int32_t* q_start, const int32_t* seq_le
       a.ws_lse = (float*)((char*)workspace + align256(int64_t(a.B) * a.Hkv * a.n_rt * a.parts * 16 * a.row_blocks * a.D * 4));
     }
     e = launch_paged_rows(a, (hipStream_t)stream);
+  }
+  if (e == hipSuccess && pl.tile) {
+    a.tile_grid = pl.tile_grid; a.tile_items = pl.tile_items; a.tile_slots = pl.tile_slots;
+    a.tile_parts = pl.tile_parts; a.tile_splits = pl.tile_splits;
+    a.ws_o = nullptr;
+    if (pl.ws_bytes > pl.rows_ws) {
+      a.ws_o = (float*)((char*)workspace + pl.rows_ws);
+      a.ws_lse = (float*)((char*)a.ws_o + align256(int64_t(a.tile_slots) * kBlockM * a.D * 4));
+    }
+    e = launch_paged_tile(a, (hipStream_t)stream);
   }
   return status_of(e);
 }

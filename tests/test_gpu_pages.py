@@ -221,6 +221,7 @@ SEQS = {
     "short": [(5, 33), (2, 0), (0, 0), (17, 480), (3, 47)],
     "mixed": [(1, 90), (150, 77), (1, 1), (64, 0), (7, 300)],
     "chunk": [(333, 190)],
+    "chunks": [(129, 64), (200, 0), (1, 33), (65, 700), (256, 63)],
 }
 MASKS = [dict(), dict(sink=5, window=40), dict(sink=40, window=17), dict(window=0), dict(sink=64, window=64)]
 
@@ -271,17 +272,28 @@ def test_attention_past_the_table():
     # positions that the table has no entry for: their keys are not seen, their rows see the rest
     c = Cache(13, [(20, 40), (3, 100)], heads=ODD, page=16, width=3).device()
     check(c, c.attention(), c.oracle())
+    c = Cache(13, [(120, 40), (90, 3), (70, 500)], heads=ODD, page=16, width=7).device()
+    check(c, c.attention(), c.oracle())
+
+
+@pytest.mark.parametrize("window", [-1, 40000])
+@pytest.mark.parametrize("splits", [0, 1, 2])
+def test_long_histories_of_small_pages(splits, window):
+    # more pages a part than the 256-row kernel holds at once
+    for page in (16, 32):
+        c = Cache(25, [(70, 46000 * page // 16)], heads=(4, 2, 64), page=page, sink=100, window=window).device()
+        check(c, c.attention(splits=splits), c.oracle())
 
 
 @pytest.mark.parametrize("seqs,drop", [([(1, 100)], {(0, 0)}), ([(1, 40)], {(0, 0), (0, 1), (0, 2)}), ([(70, 90), (1, 50)], {(0, 2), (1, 1), (0, 9)}),
-                                       ([(3, 13)], {(0, 0)})], ids=str)
+                                       ([(3, 13)], {(0, 0)}), ([(200, 400), (90, 31)], {(0, 0), (0, 7), (0, 8), (0, 30), (1, 1), (1, 7)})], ids=str)
 def test_attention_without_some_pages(seqs, drop):
     c = Cache(14, seqs, heads=H128, page=16, drop=drop).device()
     check(c, c.attention(), c.oracle())
 
 
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
-@pytest.mark.parametrize("seqs", [[(1, 70), (2, 33)], [(9, 60)], [(150, 77)], [(300, 200), (1, 5)]], ids=str)
+@pytest.mark.parametrize("seqs", [[(1, 70), (2, 33)], [(9, 60)], [(150, 77)], [(300, 200), (1, 5)], [(90, 300), (260, 3)]], ids=str)
 def test_values_that_are_not_finite(seqs, value):
     for mask in (dict(), dict(sink=8, window=30)):
         c = Cache(15, seqs, heads=H128, page=16, **mask)
@@ -333,7 +345,7 @@ def test_arrays_that_make_no_sense_stay_in_bounds():
     """Lengths, starts and entries outside every range: rows that exist are written, nothing faults, no other row is."""
     c = Cache(18, [(3, 20), (4, 50)], heads=H128, page=16).device()
     big = 2 ** 31 - 1
-    for starts in ([-5, 3, 7], [0, 100, 200], [6, 3, 1], [0, big, -big - 1]):
+    for starts in ([-5, 3, 7], [0, 100, 200], [6, 3, 1], [0, big, -big - 1], [0, 9, 0]):
         for lens in ([-4, big], [big, -big - 1]):
             c.ds, c.dl = i32(starts), i32(lens)
             c.attention(max_q=9)
@@ -345,6 +357,11 @@ def test_arrays_that_make_no_sense_stay_in_bounds():
             vico.vico_pages_reserve(c.dt.clone(), refs, c.dl, c.ds, 16, moves, granted, ws)
             vico.vico_pages_fork(c.dt.clone(), refs, c.dl.clone(), i32([1, 0]), 16)
             torch.cuda.synchronize()
+    # starts that go up and down: more rows than the call has
+    c = Cache(19, [(100, 30)] + [(0, 30)] * 9, heads=H128, page=16).device()
+    c.ds = i32([0, 100, 0, 100, 0, 100, 0, 100, 0, 100, 0])
+    for splits in (0, 1, 4):
+        c.attention(splits=splits, max_q=100)
 
 
 def test_pool_past_the_32bit_offset_limit():

@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libvico.so")
 SOURCES = ["attn_fwd.hip", "attn_merge.hip", "attn_gather.hip", "attn_rows.hip", "retrieve.hip", "token_drop.hip", "kv_append.hip", "vico_api.hip", "noalloc.hip",
            "attn_rows_q4.hip", "attn_tile_q4.hip", "kv_q4.hip", "qk_norm_rope.hip", "cache_api.hip",
-           "pages_table.hip", "pages_move.hip", "attn_rows_pages.hip", "attn_tile_pages.hip", "pages_api.hip"]
+           "pages_table.hip", "pages_move.hip", "attn_pages.hip", "pages_api.hip"]
 BENCH_LIB = os.path.join(PKG, "libvico_bench.so")
 BENCH_SOURCES = ["mfma_peak.hip"]
 

@@ -1,0 +1,95 @@
+// The kernels of attention over the cache in pages (gfx950): which work-group does
+// what.  Sequences are of three classes by their packed rows (tokens times query heads
+// of a KV head): up to 16, decode steps and the shortest queries; up to
+// kPagedRowsMost; more.  Which sequence is of which class stands in device memory: a launch
+// has work-groups for every sequence in every class that max_q_len allows, and those
+// that find another class end.  What is left of a call in which a class has no
+// sequence is the time of that, about 1 us a 256 work-groups.
+//
+// Calls of one class, or of the first two, have kernels of four waves of which a CU
+// holds several, so that one's start is hidden behind another's keys.  With
+// the third, one launch does all: work-groups of the matrix cores first, which are
+// long, then those that stream keys.
+
+#include "attn_rows_pages.h"
+#include "attn_tile_pages.h"
+
+namespace vico {
+namespace {
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
+  __shared__ RowsLds<D, 1, 4> lds;
+  paged_rows<D, 1, 4>(a, a.few, blockIdx.x, lds);
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedAttnArgs a) {
+  __shared__ union { RowsLds<D, 1, 4> few; RowsLds<D, 2, 4> some; } lds;
+  const int blk = blockIdx.x;
+  if (blk < a.some.groups) paged_rows<D, 2, 4>(a, a.some, blk, lds.some);
+  else paged_rows<D, 1, 4>(a, a.few, blk - a.some.groups, lds.few);
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 1) void paged_mixed_kernel(PagedAttnArgs a) {
+  __shared__ union { TileLds<D> tile; RowsLds<D, 1, 8> rows; } lds;
+  const int blk = blockIdx.x;
+  if (blk < a.tile_grid) return paged_tile<D>(a, blk, lds.tile);
+  // 16-row tiles for both: the 256-row kernel's accumulation registers leave 128 others, and 32 rows do not fit those
+  const bool some = blk < a.tile_grid + a.some.groups;
+  paged_rows<D, 1, 8>(a, some ? a.some : a.few, blk - a.tile_grid - (some ? 0 : a.some.groups), lds.rows);
+}
+
+template <int D>
+__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArgs a) {
+  int blk = blockIdx.x;
+  if (blk < a.tile_merge) return paged_tile_merge<D>(a, blk);
+  blk -= a.tile_merge;
+  if (blk < a.some.merge) {
+    if (a.some.parts <= 8) paged_rows_merge<D, 1>(a, a.some, blk);
+    else paged_rows_merge<D, 8>(a, a.some, blk);
+    return;
+  }
+  blk -= a.some.merge;
+  if (a.few.parts <= 8) paged_rows_merge<D, 1>(a, a.few, blk);
+  else paged_rows_merge<D, 8>(a, a.few, blk);
+}
+
+// Work-groups of the merge for a class: none for a single part.
+template <int D>
+int merge_groups(const RowsClass& x, int B, int Hkv) {
+  constexpr int per = kMergeThreads / (D / 4);      // rows of a work-group with one thread for four columns
+  if (x.parts <= 1) return 0;
+  return B * Hkv * x.n_rt * x.tile_rows / per * (x.parts <= 8 ? 1 : 8);
+}
+
+template <int D>
+hipError_t launch(const PagedAttnArgs& args, hipStream_t stream) {
+  PagedAttnArgs a = args;
+  if (a.tile_grid > 0) {
+    hipLaunchKernelGGL(paged_mixed_kernel<D>, dim3((unsigned)(a.tile_grid + a.some.groups + a.few.groups)), dim3(kThreads), 0, stream, a);
+  } else if (a.some.groups > 0) {
+    hipLaunchKernelGGL(paged_rows_kernel<D>, dim3((unsigned)(a.some.groups + a.few.groups)), dim3(256), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL(paged_decode_kernel<D>, dim3((unsigned)a.few.groups), dim3(256), 0, stream, a);
+  }
+  const hipError_t e = hipGetLastError();
+  a.few.merge = merge_groups<D>(a.few, a.B, a.Hkv);
+  a.some.merge = merge_groups<D>(a.some, a.B, a.Hkv);
+  a.tile_merge = a.ws_o ? a.tile_items * (kBlockM / kTileMergeRows) : 0;
+  const int groups = a.few.merge + a.some.merge + a.tile_merge;
+  if (e != hipSuccess || groups == 0) return e;
+  hipLaunchKernelGGL(paged_merge_kernel<D>, dim3((unsigned)groups), dim3(kMergeThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream) {
+  if (a.few.groups < 1 || a.few.parts > kPagedParts || a.some.parts > kPagedParts || a.tile_splits > kPagedTileParts)
+    return hipErrorInvalidValue;
+  return a.D == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
+}
+
+}  // namespace vico

@@ -22,30 +22,31 @@
 //     are not finite: 0 times those is NaN, so they are zeros in the product and are
 //     added at the end for the rows that see them.
 
+#pragma once
+
 #include "attn_common.h"
 #include "pages.h"
 #include "values.h"
 
 namespace vico {
-namespace {
 
-constexpr int kPagedWaves = 4;
+template <int D, int NRB, int NW>
+struct RowsLds {
+  __attribute__((aligned(16))) float o[NW][16 * NRB][D + 8];
+  float m[NW][16 * NRB], l[NW][16 * NRB];
+  int odd;
+};
 
-template <int D, int NRB>
-__global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAttnArgs a) {
-  constexpr int NW = kPagedWaves;
+// Work-group `blk` of those that take the sequences of class x: row tiles of 16 * NRB rows.
+template <int D, int NRB, int NW>
+__device__ __forceinline__ void paged_rows(const PagedAttnArgs& a, const RowsClass& x, int blk, RowsLds<D, NRB, NW>& lds) {
   constexpr int NKS = D / 32;              // k-steps of Q K^T
   constexpr int VE = D / 16;               // dims per lane of a V row
   constexpr int RT = 16 * NRB;             // rows of the work-group
   constexpr int BK = kRowsBlock;           // keys per block
-  constexpr int OS = D + 8;                // row stride of the merge buffer (floats)
   static_assert(BK == 32, "two 16-key products per block");
   typedef uint32_t vrow_t __attribute__((ext_vector_type(VE / 2)));
   typedef const __attribute__((address_space(1))) char* gptr;
-
-  __shared__ __attribute__((aligned(16))) float o_s[NW][RT][OS];
-  __shared__ float m_s[NW][RT], l_s[NW][RT];
-  __shared__ int odd_s;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -53,23 +54,23 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAt
   const int g = a.Hq / a.Hkv;
 
   // ---- work item: row tiles of one key range side by side, then KV heads, parts, sequences
-  int L = xcd_remap(blockIdx.x, gridDim.x);
-  int next = a.by_rt(L);
-  const int rt = L - next * a.n_rt;
+  int L = xcd_remap(blk, x.groups);
+  int next = x.by_rt(L);
+  const int rt = L - next * x.n_rt;
   L = next;
   next = a.by_kv(L);
   const int kv = L - next * a.Hkv;
   L = next;
-  const int b = a.by_parts(L), part = L - b * a.parts;
+  const int b = x.by_parts(L), part = L - b * x.parts;
 
   const Sequence s = sequence(a, b);
   const int NR = g * s.n;
-  if (NR > a.rows_most || rt * RT >= NR) return;
+  if (NR > x.most || NR < x.least || rt * RT >= NR) return;
   const KeyBlocks<BK> blocks(s);
   int per;
-  const int parts = parts_of(a, blocks.upto(last_position(a, s, s.n - 1)), per);
+  const int parts = parts_of(x, blocks.upto(last_position(a, s, s.n - 1)), per);
   if (part >= parts) return;
-  if (tid == 0) odd_s = 0;
+  if (tid == 0) lds.odd = 0;
 
   // ---- Q rows as B fragments; rows past the end repeat the last one and are never stored
   bf16x8 qf[NRB][NKS];
@@ -121,38 +122,38 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAt
     int pv;                                        // page of keys 8j .. 8j + 7
     int pos;
   };
-  auto load_block = [&](int blk, int held, int i, Block& x) __attribute__((always_inline)) {
-    x.pos = blocks.position(blk);
+  auto load_block = [&](int blk, int held, int i, Block& y) __attribute__((always_inline)) {
+    y.pos = blocks.position(blk);
     const int pk = __shfl(held, 2 * i + (n >> 3), 64);
-    x.pv = __shfl(held, 2 * i + (j >> 1), 64);
-    const gptr kp = (gptr)a.k_pages + (max(pk, 0) * pbytes + (uint32_t)(((x.pos + ka) & in_page) * rbytes + kv * D * 2 + j * 16));
-    const gptr vp = (gptr)a.v_pages + (max(x.pv, 0) * pbytes + (uint32_t)(((x.pos + 8 * j) & in_page) * rbytes + kv * D * 2 + n * (VE * 2)));
+    y.pv = __shfl(held, 2 * i + (j >> 1), 64);
+    const gptr kp = (gptr)a.k_pages + (max(pk, 0) * pbytes + (uint32_t)(((y.pos + ka) & in_page) * rbytes + kv * D * 2 + j * 16));
+    const gptr vp = (gptr)a.v_pages + (max(y.pv, 0) * pbytes + (uint32_t)(((y.pos + 8 * j) & in_page) * rbytes + kv * D * 2 + n * (VE * 2)));
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int ks = 0; ks < NKS; ++ks)
-        x.k[h][ks] = *(const __attribute__((address_space(1))) u32x4*)(kp + h * 4 * rbytes + ks * 64);
+        y.k[h][ks] = *(const __attribute__((address_space(1))) u32x4*)(kp + h * 4 * rbytes + ks * 64);
 #pragma unroll
-    for (int r = 0; r < 8; ++r) x.v[r] = *(const __attribute__((address_space(1))) vrow_t*)(vp + r * rbytes);
+    for (int r = 0; r < 8; ++r) y.v[r] = *(const __attribute__((address_space(1))) vrow_t*)(vp + r * rbytes);
   };
 
-  auto compute_block = [&](Block& x) __attribute__((always_inline)) {
-    const int k0 = x.pos + 8 * j;                  // this lane's eight keys
-    const bool gap = x.pos + BK > s.sink && x.pos < s.first;
+  auto compute_block = [&](Block& y) __attribute__((always_inline)) {
+    const int k0 = y.pos + 8 * j;                  // this lane's eight keys
+    const bool gap = y.pos + BK > s.sink && y.pos < s.first;
     // what some lane's row does not see of the block
-    const bool cut = x.pos + BK - 1 > first_lim, holes = __builtin_amdgcn_ballot_w64(x.pv < 0) != 0;
+    const bool cut = y.pos + BK - 1 > first_lim, holes = __builtin_amdgcn_ballot_w64(y.pv < 0) != 0;
     if (__builtin_expect(cut || gap || holes, 0)) {
       u16x2 most{0, 0};
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
         const int p = k0 + r;
-        const bool none = x.pv < 0 || p > last_lim || (p >= s.sink && p < s.first);
-        x.v[r] = none ? vrow_t{} : x.v[r];
+        const bool none = y.pv < 0 || p > last_lim || (p >= s.sink && p < s.first);
+        y.v[r] = none ? vrow_t{} : y.v[r];
         if (cut) {
 #pragma unroll
           for (int d = 0; d < VE / 2; ++d) {
-            largest_exponents(most, x.v[r][d]);
-            x.v[r][d] = finite_or_zero(x.v[r][d]);
+            largest_exponents(most, y.v[r][d]);
+            y.v[r][d] = finite_or_zero(y.v[r][d]);
           }
         }
       }
@@ -167,13 +168,13 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAt
         sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks)
-          sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[h][ks]), qf[rb][ks], sc[h], 0, 0, 0);
+          sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y.k[h][ks]), qf[rb][ks], sc[h], 0, 0, 0);
       }
       if (__builtin_expect(cut || gap || holes, 0)) {
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
           const int p = k0 + v;
-          const bool none = x.pv < 0 || p > lim[rb] || (p >= s.sink && p < s.first);
+          const bool none = y.pv < 0 || p > lim[rb] || (p >= s.sink && p < s.first);
           sc[v / 4][v % 4] = none ? -INFINITY : sc[v / 4][v % 4];
         }
       }
@@ -209,7 +210,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAt
       u32x4 w;           // value e of this lane's 8 keys
 #pragma unroll
       for (int p = 0; p < 4; ++p)
-        w[p] = __builtin_amdgcn_perm(x.v[2 * p + 1][e / 2], x.v[2 * p][e / 2], (e & 1) ? 0x07060302u : 0x05040100u);
+        w[p] = __builtin_amdgcn_perm(y.v[2 * p + 1][e / 2], y.v[2 * p][e / 2], (e & 1) ? 0x07060302u : 0x05040100u);
       const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb) o[rb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb], o[rb][e], 0, 0, 0);
@@ -217,12 +218,12 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAt
   };
 
   // ---- the wave's blocks
-  for (int blk = b_lo + wave; blk < b_hi;) {
-    const int held = pages_from(blk);
-    for (int i = 0; i < 32 && blk < b_hi; ++i, blk += NW) {
-      Block x;
-      load_block(blk, held, i, x);
-      compute_block(x);
+  for (int at = b_lo + wave; at < b_hi;) {
+    const int held = pages_from(at);
+    for (int i = 0; i < 32 && at < b_hi; ++i, at += NW) {
+      Block y;
+      load_block(at, held, i, y);
+      compute_block(y);
     }
   }
 
@@ -233,10 +234,10 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAt
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (j == 0) {
-      m_s[wave][rb * 16 + n] = m_run[rb];
-      l_s[wave][rb * 16 + n] = l;
+      lds.m[wave][rb * 16 + n] = m_run[rb];
+      lds.l[wave][rb * 16 + n] = l;
     }
-    float* op = &o_s[wave][rb * 16 + n][VE * 4 * j];
+    float* op = &lds.o[wave][rb * 16 + n][VE * 4 * j];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAt
         *(f32x4*)(op + i * VE + e) = f32x4{o[rb][e][i], o[rb][e + 1][i], o[rb][e + 2][i], o[rb][e + 3][i]};
   }
   __syncthreads();
-  if (odd) odd_s = 1;
+  if (odd) lds.odd = 1;
   __syncthreads();
   constexpr int NQ = D / 4;
   const int rows = min(RT, NR - rt * RT);
@@ -252,20 +253,20 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAt
     const int r = it / NQ, dq = it % NQ;
     float m = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) m = fmaxf(m, m_s[w][r]);
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, lds.m[w][r]);
     const float m_use = m == -INFINITY ? 0.f : m;
     float l = 0.f;
     f32x4 acc{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float f = __builtin_amdgcn_exp2f(m_s[w][r] - m_use);      // 0 for a wave that saw no key of the row
-      l += f * l_s[w][r];
-      acc += f * *(const f32x4*)&o_s[w][r][dq * 4];
+      const float f = __builtin_amdgcn_exp2f(lds.m[w][r] - m_use);      // 0 for a wave that saw no key of the row
+      l += f * lds.l[w][r];
+      acc += f * *(const f32x4*)&lds.o[w][r][dq * 4];
     }
     acc *= l > 0.f ? 1.f / l : l == l ? 0.f : l;                      // an empty row is 0, a NaN stays one
     const float lse2 = l > 0.f ? m_use + __log2f(l) : l == l ? -INFINITY : l;
     const int pr = rt * RT + r, t = a.by_g(pr), h = kv * g + pr - t * g;
-    if (__builtin_expect(odd_s != 0, 0)) {       // values of the part's blocks on the diagonal, for the rows that see them
+    if (__builtin_expect(lds.odd != 0, 0)) {     // values of the part's blocks on the diagonal, for the rows that see them
       const int upto = last_position(a, s, t);
       for (int blk = max(b_lo, blocks.upto(first_lim) - 1); blk < b_hi; ++blk) {
         const int pos = blocks.position(blk);
@@ -283,9 +284,9 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAt
       }
     }
     if (parts > 1) {
-      const int64_t prow = ((((int64_t)b * a.parts + part) * a.Hkv + kv) * a.n_rt + rt) * RT + r;
-      *(f32x4*)(a.ws_o + prow * D + dq * 4) = acc;
-      if (dq == 0) a.ws_lse[prow] = lse2;
+      const int64_t prow = ((((int64_t)b * x.parts + part) * a.Hkv + kv) * x.n_rt + rt) * RT + r;
+      *(f32x4*)(x.ws_o + prow * D + dq * 4) = acc;
+      if (dq == 0) x.ws_lse[prow] = lse2;
       continue;
     }
     const int64_t orow = (int64_t)(s.q0 + t) * a.Hq + h;
@@ -302,23 +303,23 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_rows_kernel(PagedAt
 // infinity of a part reaches the row whatever the part's weight.
 constexpr int kMergeThreads = 256;
 template <int D, int PG>
-__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArgs a) {
+__device__ __forceinline__ void paged_rows_merge(const PagedAttnArgs& a, const RowsClass& x, int blk) {
   constexpr int NQ = D / 4, RPB = kMergeThreads / (NQ * PG), NP = kPagedParts / PG < 8 ? kPagedParts / PG : 8;
   __shared__ float m_s[PG][RPB][NQ], l_s[PG][RPB][NQ];
   __shared__ f32x4 acc_s[PG][RPB][NQ];
   const int tid = threadIdx.x, dq = tid % NQ, pg = tid / NQ % PG, rr = tid / (NQ * PG);
-  const int RT = 16 * a.row_blocks, chunks = RT / RPB;
-  const int L = blockIdx.x / chunks, r = (int)(blockIdx.x - L * chunks) * RPB + rr;      // RPB divides RT
-  int next = a.by_rt(L);
-  const int rt = L - next * a.n_rt;
+  const int RT = x.tile_rows, chunks = RT / RPB;
+  const int L = blk / chunks, r = (blk - L * chunks) * RPB + rr;      // RPB divides RT
+  int next = x.by_rt(L);
+  const int rt = L - next * x.n_rt;
   const int b = a.by_kv(next), kv = next - b * a.Hkv;
   const Sequence s = sequence(a, b);
   const int g = a.Hq / a.Hkv, NR = g * s.n;
-  if (NR > a.rows_most || rt * RT + r - rr >= NR) return;        // the whole work-group
+  if (NR > x.most || NR < x.least || rt * RT + r - rr >= NR) return;        // the whole work-group
   int per;
-  const int parts = parts_of(a, KeyBlocks<kRowsBlock>(s).upto(last_position(a, s, s.n - 1)), per);
+  const int parts = parts_of(x, KeyBlocks<kRowsBlock>(s).upto(last_position(a, s, s.n - 1)), per);
   if (parts == 1) return;                                        // written by the attention kernel
-  const int64_t row0 = (((int64_t)b * a.parts * a.Hkv + kv) * a.n_rt + rt) * RT + r, step = (int64_t)a.Hkv * a.n_rt * RT;
+  const int64_t row0 = (((int64_t)b * x.parts * a.Hkv + kv) * x.n_rt + rt) * RT + r, step = (int64_t)a.Hkv * x.n_rt * RT;
   float m = -INFINITY, l = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
   for (int p0 = pg; p0 < parts; p0 += PG * NP) {
@@ -327,8 +328,8 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArg
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int64_t at = row0 + min(p0 + i * PG, parts - 1) * step;
-      ls[i] = p0 + i * PG < parts ? a.ws_lse[at] : -INFINITY;
-      os[i] = *(const f32x4*)(a.ws_o + at * D + dq * 4);
+      ls[i] = p0 + i * PG < parts ? x.ws_lse[at] : -INFINITY;
+      os[i] = *(const f32x4*)(x.ws_o + at * D + dq * 4);
     }
     float mx = m;
 #pragma unroll
@@ -373,28 +374,6 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArg
   if (a.out_f32) *(f32x4*)((float*)a.out + orow * D + dq * 4) = acc;
   else *(bf16x4*)((__bf16*)a.out + orow * D + dq * 4) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
   if (dq == 0 && a.lse) a.lse[(int64_t)h * a.total + s.q0 + t] = lse2 * kLn2;
-}
-
-template <int D>
-hipError_t launch(const PagedAttnArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)(a.B * a.parts * a.Hkv * a.n_rt)), block(kPagedWaves * 64);
-  if (a.row_blocks == 1) hipLaunchKernelGGL((paged_rows_kernel<D, 1>), grid, block, 0, stream, a);
-  else if (a.row_blocks == 2) hipLaunchKernelGGL((paged_rows_kernel<D, 2>), grid, block, 0, stream, a);
-  else return hipErrorInvalidValue;
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.parts == 1) return e;
-  const unsigned rows = (unsigned)(a.B * a.Hkv * a.n_rt * 16 * a.row_blocks);
-  constexpr unsigned per = kMergeThreads / (D / 4);      // rows of a work-group with one thread for four columns
-  if (a.parts <= 8) hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(rows / per), dim3(kMergeThreads), 0, stream, a);
-  else hipLaunchKernelGGL((paged_merge_kernel<D, 8>), dim3(rows * 8 / per), dim3(kMergeThreads), 0, stream, a);
-  return hipGetLastError();
-}
-
-}  // namespace
-
-hipError_t launch_paged_rows(const PagedAttnArgs& a, hipStream_t stream) {
-  if (a.n_rt < 1 || a.parts < 1 || a.parts > kPagedParts) return hipErrorInvalidValue;
-  return a.D == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
 }
 
 }  // namespace vico

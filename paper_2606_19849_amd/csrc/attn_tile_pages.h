@@ -1,5 +1,5 @@
 // Attention over the cache in pages, many query rows a sequence (gfx950): what
-// attn_rows_pages.hip computes, for sequences whose rows share every key often
+// attn_rows_pages.h computes, for sequences whose rows share every key often
 // enough to be bound by the matrix cores -- visual chunks, long queries.
 //
 // A work-group of 8 waves owns 256 packed (token, query head) rows of one KV head of
@@ -14,8 +14,8 @@
 //   * The page numbers of the part's tiles are in LDS, checked, two halves in turn: one
 //     is filled while the other is read, in the middle of it, so that no wait or
 //     barrier of its own is needed.
-//   * Between sink and window nothing is walked; rows that no row of the sequence sees in
-//     the two tiles there are read from outside the resource, as zeros.
+//   * Between sink and window nothing is walked; what no row of the sequence sees in the
+//     two tiles there becomes zero in LDS.
 //   * Values that are not finite in tiles that the causal mask cuts are zeros in LDS (0
 //     times such a value would reach rows that do not see it) and are added afterwards for
 //     the rows that do.  Each wave looks at what it loaded, before the barrier that
@@ -24,12 +24,13 @@
 // row tiles of all sequences and finds its own; where they leave CUs idle, key ranges
 // are split and joined by the merge kernel.
 
+#pragma once
+
 #include "attn_pipe.h"
 #include "pages.h"
 #include "values.h"
 
 namespace vico {
-namespace {
 
 typedef const __attribute__((address_space(4))) PagedAttnArgs* late_args;
 // the kernel's arguments, read again where they are used: what only the start and the end need takes no registers
@@ -44,7 +45,7 @@ __device__ __forceinline__ late_args late() {
 __device__ __forceinline__ int row_tiles(const PagedAttnArgs& a, int b) {
   int q0;
   const int rows = a.Hq / a.Hkv * min(rows_of(a, b, q0), a.max_q);
-  return rows > a.rows_most ? (rows + kBlockM - 1) / kBlockM : 0;
+  return rows >= a.tile_least ? (rows + kBlockM - 1) / kBlockM : 0;
 }
 __device__ __forceinline__ int wave_scan(int x) {
   const int lane = threadIdx.x & 63;
@@ -55,14 +56,26 @@ __device__ __forceinline__ int wave_scan(int x) {
   }
   return x;
 }
-// Row tiles of all sequences, and the parts that their key ranges are split into.
+// Row tiles of all sequences and heads, and the parts that their key ranges are split into.
 __device__ __forceinline__ int all_row_tiles(const PagedAttnArgs& a, int& parts) {
   const int lane = threadIdx.x & 63;
-  int n = 0;
-  for (int b = lane; b < a.B; b += 64) n += row_tiles(a, b);
+  int n = 0, keys = 0;
+  for (int b = lane; b < a.B; b += 64) {
+    const int m = row_tiles(a, b);
+    n += m;
+    if (m > 0 && a.tile_parts > 1) {
+      const Sequence s = sequence(a, b);
+      keys = max(keys, KeyBlocks<kKeyTile>(s).upto(last_position(a, s, s.n - 1)));
+    }
+  }
   n = __builtin_amdgcn_readlane(wave_scan(n), 63);
   const int items = n * a.Hkv;
-  parts = a.tile_splits > 0 ? a.tile_splits : items > 0 ? min(max(a.tile_slots / items, 1), a.tile_parts) : 1;
+  parts = max(a.tile_splits, 1);
+  if (a.tile_parts <= 1 || items == 0) return items;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) keys = max(keys, __shfl_xor(keys, o, 64));
+  keys = __builtin_amdgcn_readfirstlane(keys);
+  parts = paged_tile_parts(items, keys, a.tile_parts, a.tile_slots);
   return items;
 }
 // The sequence whose row tiles, each `times` times, hold item x; its first item and its row tiles.
@@ -86,7 +99,14 @@ __device__ __forceinline__ int sequence_of_item(const PagedAttnArgs& a, int x, i
 constexpr int kTabHalf = 1024;             // page numbers of a half of the table in LDS
 
 template <int D>
-__global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAttnArgs a) {
+struct TileLds {
+  __attribute__((aligned(16))) uint8_t kv[2 * kBuffers * kKeyTile * D * 2];
+  int32_t tab[2 * kTabHalf];
+  int odd;
+};
+
+template <int D>
+__device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, TileLds<D>& sh) {
   constexpr int RB = 1;
   typedef PipeTile<D, RB> Tile;
   constexpr int BN = kKeyTile, BM = kBlockM, NW = kThreads / 64;
@@ -102,10 +122,8 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
   static_assert(BM == NW * 32 && RB == kRowBlocks && (NB & (NB - 1)) == 0 && LSTEP >= 1, "tile geometry");
   typedef __attribute__((address_space(3))) u32x4* lds_u4;
 
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * NB * TBY];
-  __shared__ int32_t tab[2 * kTabHalf];
-  __shared__ int odd_s;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
+  int32_t (&tab)[2 * kTabHalf] = sh.tab;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)sh.kv;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -116,13 +134,13 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
   int parts;
   const int items = all_row_tiles(a, parts), n_work = items * parts;
   // (starts that decrease may count rows twice: more partial results than there is room for)
-  if ((int)blockIdx.x >= n_work || (parts > 1 && n_work > a.tile_slots)) return;
-  const int L = xcd_remap(blockIdx.x, n_work);
+  if (blk >= n_work || (parts > 1 && n_work > a.tile_slots)) return;
+  const int L = xcd_remap(blk, n_work);
   int first_item, cnt;
   const int b = __builtin_amdgcn_readfirstlane(sequence_of_item(a, L, a.Hkv * parts, first_item, cnt));
   const int kp = (L - first_item) / cnt, rt = cnt - 1 - (L - first_item - kp * cnt);
   const int kv = kp / parts, part = kp - kv * parts;
-  if (tid == 0) odd_s = 0;
+  if (tid == 0) sh.odd = 0;
 
   // (in scalar registers, whatever the compiler makes of loads whose address it cannot prove to be the same in all lanes:
   // no branch of the key loop may be on lanes)
@@ -153,14 +171,22 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
   const int kv_end = lim_of_row(NR - 1) + 1;                       // rows of the sequence that exist
   const int cut_from = lim_of_row(rt * BM) + 1;                    // from here on some row of the work-group sees not all
   const int sink = s.sink, first = s.first;
-  auto gap = [&](int p0) __attribute__((always_inline)) { return p0 + BN > sink && p0 < first; };
+  // Tiles [t_plain, t_plain + n_plain) need no mask for this wave, and [t_plain, t_plain + n_whole) none for any row of
+  // the work-group: behind those that hold positions between sink and window, before the causal diagonal.  A page that
+  // is none makes all tiles from there on masked ones.
+  const int t_plain = sink < first ? tiles.of_sink + 1 : 0;
+  auto upto_whole = [&](int lim_) __attribute__((always_inline)) {      // tiles that lie wholly in positions <= lim_
+    const int n = (lim_ + 1) / BN;
+    return min(n, tiles.of_sink) + max(n - tiles.from, 0);
+  };
+  int n_plain = max(upto_whole(first_lim) - t_plain, 0);
+  const int n_whole = max(upto_whole(cut_from - 1) - t_plain, 0);
 
   // ---- page numbers: entry (t - t_lo) * EPT + e of the part's tile t, in tab at that number mod 2 * kTabHalf
   const int shift = a.page_shift;
   const int ept_shift = shift < 6 ? 6 - shift : 0;                 // 64 / page_size pages a tile, or one
   const int32_t* const row = a.table + (int64_t)b * a.width;
   const int n_entries = (t_hi - t_lo) << ept_shift;
-  bool holes = false;
   auto fill_tab = [&](int e0) __attribute__((always_inline)) {     // entries e0 .. e0 + kTabHalf - 1, without a branch
 #pragma unroll
     for (int i = 0; i < kTabHalf / kThreads; ++i) {                // on lanes (past the last one: anything)
@@ -168,13 +194,12 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
       const int p0 = tiles.position(t_lo + (in >> ept_shift)) + ((in & ((1 << ept_shift) - 1)) << (shift < 6 ? shift : 0));
       const int at = p0 >> shift;
       const int p = row[min(at, a.width - 1)];
-      tab[e & (2 * kTabHalf - 1)] = at < a.width && (uint32_t)p < (uint32_t)a.N ? p : -1;
+      tab[e & (2 * kTabHalf - 1)] = ((at < a.width) & ((uint32_t)p < (uint32_t)a.N)) ? p : -1;
     }
   };
 
   // ---- tile loader
   const int rbytes = a.Hkv * D * 2;
-  const int64_t pbytes = (int64_t)rbytes << shift;
   const uint32_t my_part = (uint32_t)(wave * NLD * 1024);
   uint32_t ld_k[NLD], ld_v;                                        // byte offsets from the wave's first row
   {
@@ -187,41 +212,39 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
     Tile::v_source(lane, r, u);
     ld_v = (uint32_t)(r * rbytes + u * 16);
   }
-  u32x4 run_k, run_v;                        // resources of the wave's rows of the tile to be loaded
-  int run_p0 = 0;
-  bool run_gap = false;
+  // Where the wave's rows of a tile lie: lane i of `run` has byte offset and bytes of the i-th of 64 tiles, computed for
+  // all of them at once; a tile takes its own by lane reads.
+  const uint64_t k_base = (uint64_t)a.k_pages + kv * RBY, v_base = (uint64_t)a.v_pages + kv * RBY;
+  const int my_page = shift < 6 ? (8 * wave) >> shift : 0, in_page = (1 << shift) - 1;
+  uint32_t run_lo = 0, run_hi = 0, run_bytes = 0;
+  auto find_tiles = [&](int t) __attribute__((always_inline)) {                     // of tiles t .. t + 63
+    const int tl = t + lane, e0 = (tl - t_lo) << ept_shift;
+    int bad = 0;
+    for (int e = 0; e < 1 << ept_shift; ++e) bad |= tab[(e0 + e) & (2 * kTabHalf - 1)] >> 31;
+    const bool some = tl < t_hi;             // past the part's last tile: nothing
+    n_plain = __builtin_amdgcn_ballot_w64(some & (bad != 0)) != 0 ? 0 : n_plain;
+    const int page = tab[(e0 + my_page) & (2 * kTabHalf - 1)], p0 = tiles.position(tl) + 8 * wave;
+    const int rows = (some & (page >= 0)) ? min(max(kv_end - p0, 0), 8) : 0;
+    const uint64_t at = (uint64_t)(uint32_t)((max(page, 0) << shift) + (p0 & in_page)) * (uint32_t)rbytes;
+    run_lo = (uint32_t)at;
+    run_hi = (uint32_t)(at >> 32);
+    run_bytes = (uint32_t)(rows * rbytes);
+  };
+  u32x4 run_k, run_v;                        // resources of the tile to be loaded
   auto start_tile = [&](int t) __attribute__((always_inline)) {
-    uint32_t bytes = 0;
-    int64_t at = 0;
-    if (t < t_hi) {
-      const int e0 = (t - t_lo) << ept_shift;
-      const int mine = tab[(e0 + (lane & ((1 << ept_shift) - 1))) & (2 * kTabHalf - 1)];
-      holes |= __builtin_amdgcn_ballot_w64(mine < 0) != 0;
-      const int page = __builtin_amdgcn_readlane(mine, shift < 6 ? (8 * wave) >> shift : 0);
-      run_p0 = __builtin_amdgcn_readfirstlane(tiles.position(t)) + 8 * wave;
-      const int rows = page < 0 ? 0 : min(max(kv_end - run_p0, 0), 8);
-      bytes = rows > 0 ? (uint32_t)((rows - 1) * rbytes + RBY) : 0;
-      at = max(page, 0) * pbytes + (run_p0 & ((1 << shift) - 1)) * rbytes + kv * RBY;
-      run_gap = run_p0 + 8 > sink && run_p0 < first;
-    }
-    const uint64_t pk = (uint64_t)a.k_pages + at, pv = (uint64_t)a.v_pages + at;
-    const uint32_t n = __builtin_amdgcn_readfirstlane(bytes);
-    run_k = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)pk), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(pk >> 32)) & 0xFFFFu, n, 0x00020000u};
-    run_v = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)pv), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(pv >> 32)) & 0xFFFFu, n, 0x00020000u};
+    const int i = (t - t_lo) & 63;
+    const uint64_t at = (uint32_t)__builtin_amdgcn_readlane(run_lo, i) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(run_hi, i) << 32;
+    const uint32_t bytes = __builtin_amdgcn_readlane(run_bytes, i);
+    const uint64_t pk = k_base + at, pv = v_base + at;                               // (below 2^48)
+    run_k = u32x4{(uint32_t)pk, (uint32_t)(pk >> 32), bytes, 0x00020000u};
+    run_v = u32x4{(uint32_t)pv, (uint32_t)(pv >> 32), bytes, 0x00020000u};
   };
   // direct load i (0 .. NLD-1: K, NLD .. 2*NLD-1: V) to the buffers at byte offset `boff`.  m0, which holds a load's
   // LDS address, is the compiler's own: every load sets it and gives it back.  Wait states that the compiler does not
   // know assembly to need: one after a write of m0, five after a VALU write of a scalar operand.
   auto load_direct = [&](auto idx, uint32_t boff) __attribute__((always_inline)) {
     constexpr int i = decltype(idx)::value, n = i % NLD;
-    uint32_t off = i < NLD ? ld_k[n] : ld_v + n * RPL * rbytes;
-    if (__builtin_expect(run_gap, 0)) {      // rows that nobody sees: from outside the resource
-      int r, u;
-      if constexpr (i < NLD) Tile::k_source(wave * NLD + n, lane, r, u);
-      else Tile::v_source(lane, r, u);
-      const int p = run_p0 + n * RPL + r;
-      off = p >= sink && p < first ? kOutOfRange : off;
-    }
+    const uint32_t off = i < NLD ? ld_k[n] : ld_v + n * RPL * rbytes;
     const uint32_t to = lds0 + my_part + boff + (i < NLD ? kKBase : 0u) + n * 1024;
     const u32x4 rs = i < NLD ? run_k : run_v;
     uint32_t m0;
@@ -237,19 +260,26 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
     unrolled<NL>([&](auto i) __attribute__((always_inline)) { load_direct(i, boff); });
   };
 
-  // ---- the wave's share of V of tile t, landed at `boff`: what is not finite becomes zero where the mask cuts
+  // ---- the wave's share of V of tile t, landed at `boff`: zeros for what no row sees, and for what is not finite
+  // where the mask cuts
   bool odd = false;
   auto look = [&](int t, uint32_t boff) __attribute__((always_inline)) {
-    if (__builtin_expect(t < t_hi && tiles.position(t) + BN > cut_from, 0)) {
+    if (__builtin_expect((uint32_t)(t - t_plain) >= (uint32_t)n_whole, 0)) {       // (past the last tile: zeros)
+      const int pos = tiles.position(t);
       const uint32_t at = lds0 + boff + my_part + (uint32_t)(lane * 16);
+      int r, u;
+      Tile::v_source(lane, r, u);
 #pragma unroll
       for (int n = 0; n < NLD; ++n) {
         u32x4 y = *(lds_u4)(uintptr_t)(at + n * 1024);
+        const int p = pos + 8 * wave + n * RPL + r;
+        const uint32_t keep = ((p >= sink) & (p < first)) ? 0u : ~0u;
         u16x2 most{0, 0};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          largest_exponents(most, y[i]);
-          y[i] = finite_or_zero(y[i]);
+          y[i] &= keep;
+          largest_exponents(most, pos + BN > cut_from ? y[i] : 0u);
+          y[i] = pos + BN > cut_from ? finite_or_zero(y[i]) : y[i];
         }
         odd |= not_finite(most);
         *(lds_u4)(uintptr_t)(at + n * 1024) = y;
@@ -272,7 +302,7 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
       const bool none = p > lim || (p >= sink && p < first);
       x[v] = none ? -INFINITY : x[v];
     }
-    if (__builtin_expect(holes, 0)) {
+    if (n_plain == 0) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {          // eight keys lie in one page
         const int in_tile = ((p0 & 32) | (8 * q)) >> per;
@@ -300,16 +330,19 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
     // there must be finite
     if (tid < RBY) *(lds_u4)(uintptr_t)(lds0 + (NB - 1) * TBY + 48 * RBY + tid * 16) = u32x4{0, 0, 0, 0};
     __syncthreads();
+    find_tiles(t_lo);
 #pragma unroll 1
     for (int i = 0; i < AHEAD; ++i) load_whole(i * TBY, t_lo + i);
-    start_tile(t_lo + AHEAD);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * NL) : "memory");      // tile t_lo
     look(t_lo, 0);
     barrier_keep_loads();
     // the half of the table that is not in use is filled for its next turn as the loads pass the middle of the other
+    // (t: the last tile that has been sent)
     auto more_tab = [&](int t) __attribute__((always_inline)) {
-      const int e = (t - t_lo) << ept_shift;
-      if (__builtin_expect((e & (kTabHalf - 1)) == kTabHalf / 2 && e > kTabHalf, 0)) fill_tab(e - kTabHalf / 2 + kTabHalf);
+      if (__builtin_expect(((t + 1 - t_lo) & 63) != 0, 1)) return;
+      const int e = (t + 1 - t_lo) << ept_shift;
+      if ((e & (kTabHalf - 1)) == kTabHalf / 2 && e > kTabHalf) fill_tab(e - kTabHalf / 2 + kTabHalf);
+      find_tiles(t + 1);
     };
     uint32_t boff = 0;                       // buffer offset of tile t
     int t = t_lo;
@@ -318,21 +351,16 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
       Tile wt{qf, k_rd, v_rd, v_nx, o, m_run, l_run, neg_m, vf, a.scale_log2};
       f32x16 s0[RB], s1[RB];
       bf16x8 p0[RB][2] = {}, p1[RB][2] = {};
-      // tiles that some lane's row does not see whole: mask them
-      auto cut = [&](int pos) __attribute__((always_inline)) { return pos + BN - 1 > first_lim || gap(pos) || holes; };
+      auto cut = [&]() __attribute__((always_inline)) { return (uint32_t)(t - t_plain) >= (uint32_t)n_plain; };
       wt.first_logits(s0);
-      {
-        const int pos = tiles.position(t);
-        if (cut(pos)) mask(t, pos, s0[0]);
-      }
+      if (cut()) mask(t, tiles.position(t), s0[0]);
       wt.first_max(s0);
       for (; t < t_end; ++t) {
-        const int pos = tiles.position(t);
-        const bool masked = cut(pos);
-        if (__builtin_expect(masked, 0)) mask(t, pos, s0[0]);
+        if (__builtin_expect(cut(), 0)) mask(t, tiles.position(t), s0[0]);
         uint32_t next = 0;                   // of tile t + 1
         wt.template half<32, 48, 0>(s0, s1, p1, p0, [&](auto slot) __attribute__((always_inline)) {
           constexpr int i = decltype(slot)::value;
+          if constexpr (i == Tile::NPV + 2) start_tile(t + AHEAD);
           if constexpr (i == Tile::NQK + Tile::NPV) {
             next = (boff + TBY) & kWrap;
             k_rd[0] += next - boff;          // K of tile t + 1
@@ -341,7 +369,7 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
           }
         });
         landed(t + 1, next);
-        if (__builtin_expect(masked, 0)) mask(t, pos + 32, s1[0]);
+        if (__builtin_expect(cut(), 0)) mask(t, tiles.position(t) + 32, s1[0]);
         const uint32_t fill = (boff + AHEAD * TBY) & kWrap;
         wt.template half<0, 16, 32>(s1, s0, p0, p1, [&](auto slot) __attribute__((always_inline)) {
           constexpr int j = decltype(slot)::value, i = j / LSTEP - 1;
@@ -350,27 +378,25 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
         v_nx += next - boff;                 // V of tile t + 1
         boff = next;
         more_tab(t + AHEAD);
-        start_tile(t + AHEAD + 1);
       }
       wt.template last_values<48>(p1);
     }
     for (; t < t_hi; ++t) {                  // tiles that this wave's rows do not see: it brings its share
       const uint32_t next = (boff + TBY) & kWrap;
       landed(t + 1, next);
-      unrolled<NL>([&](auto i) __attribute__((always_inline)) { load_direct(i, (boff + AHEAD * TBY) & kWrap); });
+      load_whole((boff + AHEAD * TBY) & kWrap, t + AHEAD);
       boff = next;
       more_tab(t + AHEAD);
-      start_tile(t + AHEAD + 1);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the empty loads past the last tile
   }
 
   // ---- values of the cut tiles that are not finite
-  if (odd) odd_s = 1;
+  if (odd) sh.odd = 1;
   __syncthreads();
   if (!wave_active) return;
   const late_args l = late();
-  if (__builtin_expect(odd_s != 0, 0)) {
+  if (__builtin_expect(sh.odd != 0, 0)) {
     for (int t = t_lo; t < t_hi; ++t) {
       const int pos = tiles.position(t);
       if (pos + BN <= cut_from) continue;
@@ -422,9 +448,8 @@ __global__ __launch_bounds__(kThreads, kWgPerCU) void paged_tile_kernel(PagedAtt
   else if (l->lse) l->lse[(int64_t)head * l->total + s.q0 + tok] = lse2 * kLn2;
 }
 
-// The parts of a row tile joined, as in attn_rows_pages.hip: one thread takes four columns of a row, all parts' loads
+// The parts of a row tile joined, as in attn_rows_pages.h: one thread takes four columns of a row, all parts' loads
 // together.
-constexpr int kMergeThreads = 256;
 template <int D, int NP>
 __device__ __forceinline__ f32x4 joined(const PagedAttnArgs& a, int64_t row0, int64_t step, int parts, int dq, float& lse2) {
   float ls[NP];
@@ -452,50 +477,37 @@ __device__ __forceinline__ f32x4 joined(const PagedAttnArgs& a, int64_t row0, in
   return acc;
 }
 
+constexpr int kTileMergeRows = 32;         // rows of a work-group
 template <int D>
-__global__ __launch_bounds__(kMergeThreads) void paged_tile_merge_kernel(PagedAttnArgs a) {
-  constexpr int NQ = D / 4, RPB = kMergeThreads / NQ, CH = kBlockM / RPB;
+__device__ __forceinline__ void paged_tile_merge(const PagedAttnArgs& a, int blk) {
+  constexpr int NQ = D / 4, RPB = kMergeThreads / NQ, CH = kBlockM / kTileMergeRows;
   int parts;
   const int items = all_row_tiles(a, parts);
-  const int it = blockIdx.x / CH;
+  const int it = blk / CH;
   if (parts == 1 || it >= items || items * parts > a.tile_slots) return;
   int first_item, cnt;
   const int b = sequence_of_item(a, it, a.Hkv, first_item, cnt);
   const int kv = (it - first_item) / cnt, rt = it - first_item - kv * cnt;
-  const int r = (int)(blockIdx.x - it * CH) * RPB + threadIdx.x / NQ, dq = threadIdx.x % NQ;
   const Sequence s = sequence(a, b);
-  const int g = a.Hq / a.Hkv, pr = rt * kBlockM + r;
-  if (pr >= g * s.n) return;
-  const int64_t row0 = ((int64_t)first_item * parts + (int64_t)kv * parts * cnt + cnt - 1 - rt) * kBlockM + r;
+  const int g = a.Hq / a.Hkv, dq = threadIdx.x % NQ;
+  const int64_t item0 = ((int64_t)first_item * parts + (int64_t)kv * parts * cnt + cnt - 1 - rt) * kBlockM;
   const int64_t step = (int64_t)cnt * kBlockM;
-  float lse2;
-  f32x4 acc;
-  if (parts <= 2) acc = joined<D, 2>(a, row0, step, parts, dq, lse2);
-  else if (parts <= 4) acc = joined<D, 4>(a, row0, step, parts, dq, lse2);
-  else if (parts <= 8) acc = joined<D, 8>(a, row0, step, parts, dq, lse2);
-  else acc = joined<D, 16>(a, row0, step, parts, dq, lse2);
-  const int t = a.by_g(pr), h = kv * g + pr - t * g;
-  const int64_t orow = (int64_t)(s.q0 + t) * a.Hq + h;
-  if (a.out_f32) *(f32x4*)((float*)a.out + orow * D + dq * 4) = acc;
-  else *(bf16x4*)((__bf16*)a.out + orow * D + dq * 4) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
-  if (dq == 0 && a.lse) a.lse[(int64_t)h * a.total + s.q0 + t] = lse2 * kLn2;
-}
-
-template <int D>
-hipError_t launch(const PagedAttnArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(paged_tile_kernel<D>, dim3((unsigned)a.tile_grid), dim3(kThreads), 0, stream, a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.ws_o) return e;
-  constexpr int chunks = kBlockM / (kMergeThreads / (D / 4));
-  hipLaunchKernelGGL(paged_tile_merge_kernel<D>, dim3((unsigned)a.tile_items * chunks), dim3(kMergeThreads), 0, stream, a);
-  return hipGetLastError();
-}
-
-}  // namespace
-
-hipError_t launch_paged_tile(const PagedAttnArgs& a, hipStream_t stream) {
-  if (a.tile_grid < 1 || a.tile_splits > kPagedTileParts) return hipErrorInvalidValue;
-  return a.D == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
+#pragma unroll
+  for (int i = 0; i < kTileMergeRows / RPB; ++i) {
+    const int r = (blk - it * CH) * kTileMergeRows + i * RPB + threadIdx.x / NQ, pr = rt * kBlockM + r;
+    if (pr >= g * s.n) return;
+    float lse2;
+    f32x4 acc;
+    if (parts <= 2) acc = joined<D, 2>(a, item0 + r, step, parts, dq, lse2);
+    else if (parts <= 4) acc = joined<D, 4>(a, item0 + r, step, parts, dq, lse2);
+    else if (parts <= 8) acc = joined<D, 8>(a, item0 + r, step, parts, dq, lse2);
+    else acc = joined<D, 16>(a, item0 + r, step, parts, dq, lse2);
+    const int t = a.by_g(pr), h = kv * g + pr - t * g;
+    const int64_t orow = (int64_t)(s.q0 + t) * a.Hq + h;
+    if (a.out_f32) *(f32x4*)((float*)a.out + orow * D + dq * 4) = acc;
+    else *(bf16x4*)((__bf16*)a.out + orow * D + dq * 4) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
+    if (dq == 0 && a.lse) a.lse[(int64_t)h * a.total + s.q0 + t] = lse2 * kLn2;
+  }
 }
 
 }  // namespace vico

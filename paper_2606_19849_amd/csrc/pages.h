@@ -63,8 +63,18 @@ struct PagedAppendArgs {
 hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream);
 
 // ---- attention
-constexpr int kPagedParts = 64;       // most key-range parts of a row tile (rows kernel)
+constexpr int kPagedParts = 64;       // most key-range parts of a row tile of the classes below
 constexpr int kPagedTileParts = 16;   // and of a 256-row tile
+// Sequences of `least` to `most` packed rows, on row tiles of tile_rows rows.
+struct RowsClass {
+  int least, most, tile_rows;
+  int n_rt;                 // row tiles of a sequence at most
+  int parts, per_part;      // parts of its key range at most, 32-key blocks of one at least
+  int groups, merge;        // work-groups: B * parts * Hkv * n_rt; of the merge
+  float* ws_o;              // partial results [B][parts][Hkv][n_rt][tile_rows][D], and their log2-sum-exps
+  float* ws_lse;
+  FastDiv by_rt, by_parts;
+};
 struct PagedAttnArgs {
   const uint16_t* q;
   const int32_t* q_start;
@@ -74,24 +84,38 @@ struct PagedAttnArgs {
   const int32_t* table;
   void* out;
   float* lse;               // may be null
-  float* ws_o;              // partial results of row tiles: [slot][rows][D] fp32, and their log2-sum-exps [slot][rows]
-  float* ws_lse;
   int B, total, max_q, N, width, page_shift;
   int S;
   int64_t W;                // < 0: the whole history
   int Hq, Hkv, D;
   int bidir, out_f32;
   float scale_log2;
-  int rows_most;            // packed rows of a sequence up to which the rows kernel takes it
-  int n_rt, row_blocks;     // rows kernel: row tiles of 16 * row_blocks rows of a sequence
-  int parts, per_part;      // rows kernel: parts at most, 32-key blocks of a part at least
-  // 256-row kernel: its launch, the row tiles of all heads that may be split, partial results that there is room for,
-  // and parts: the caller's (0: as many as fill the room), or at most
-  int tile_grid, tile_items, tile_slots, tile_splits, tile_parts;
-  FastDiv by_g, by_rt, by_parts, by_kv;
+  FastDiv by_g, by_kv;
+  RowsClass few, some;      // up to 16 rows, up to tile_least - 1 (groups 0: none)
+  // sequences of tile_least rows and more, on 256-row tiles: work-groups (0: none) and those of the merge, the row
+  // tiles of all heads that may be split, room for partial results, the parts that the caller asked for (0: the
+  // kernel's choice, of tile_parts at most)
+  int tile_least, tile_grid, tile_merge, tile_items, tile_slots, tile_splits, tile_parts;
+  float* ws_o;              // partial results of 256-row tiles [slot][256][D], and their log2-sum-exps (null: no parts)
+  float* ws_lse;
 };
-hipError_t launch_paged_rows(const PagedAttnArgs& a, hipStream_t stream);
-hipError_t launch_paged_tile(const PagedAttnArgs& a, hipStream_t stream);
+// Parts of the key ranges of `items` row tiles over `tiles` 64-key tiles: the number with the least time, counted in such
+// tiles (1.35 us with heads of size 128): rounds of work-groups over the CUs, each a start, an end and its keys, then
+// the merge and the partial results' way to memory and back.  (3B heads, 64 row tiles of 139 tiles, us measured with
+// the chunk kernel: 2 parts 126, 3 91.7, 4 84.7, 6 105, 8 96.7.)
+__host__ __device__ inline int paged_tile_parts(int items, int tiles, int most, int slots) {
+  int best = 1 << 30, parts = 1;
+  for (int p = 1; p <= most && (p == 1 || items * p <= slots); ++p) {
+    const int rounds = (items * p + kNumCUs - 1) / kNumCUs;
+    const int cost = 32 * rounds * (6 + (tiles + p - 1) / p) + (p > 1 ? 64 + items * p * 5 / 4 : 0);
+    if (cost < best) {
+      best = cost;
+      parts = p;
+    }
+  }
+  return parts;
+}
+hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream);
 
 // What a sequence's rows are and see.  Numbers from device memory are brought
 // into range here: whatever the arrays hold, rows lie in [0, total) and positions in
@@ -128,9 +152,9 @@ struct KeyBlocks {
   __device__ __forceinline__ int upto(int last) const { return max(last / BN + 1 - from, 0) + of_sink; }
   __device__ __forceinline__ int position(int i) const { return (i < of_sink ? i : i - of_sink + from) * BN; }
 };
-// Parts of a sequence's key range on the rows kernel, and 32-key blocks of one.
-__device__ __forceinline__ int parts_of(const PagedAttnArgs& a, int blocks, int& per) {
-  per = max(a.per_part, a.by_parts(blocks + a.parts - 1));
+// Parts of a sequence's key range, and 32-key blocks of one.
+__device__ __forceinline__ int parts_of(const RowsClass& x, int blocks, int& per) {
+  per = max(x.per_part, x.by_parts(blocks + x.parts - 1));
   return max((blocks + per - 1) / per, 1);
 }
 

@@ -63,16 +63,35 @@ void use_workspace(PagesArgs* a, void* workspace) {
   a->need = (int32_t*)p;
 }
 
-// ---- attention: which sequences take which kernel, and how their keys are split.
-constexpr int kPagedRowsMost = 128;      // packed rows of a KV head up to which the rows kernel takes a sequence
+// ---- attention: the classes of sequences that a call may have, and how their keys are split.
+constexpr int kFewRows = 16;
+constexpr int kSomeRows = 128;                                             // more: 256-row tiles
+constexpr int64_t kPagedWorkspace = int64_t(64) << 20;                     // most bytes of a split picked by the library
 
 struct PagedPlan {
-  bool rows, tile;
-  int n_rt, row_blocks, parts, per_part;
+  RowsClass few, some;
   int tile_grid, tile_items, tile_slots, tile_parts, tile_splits;
-  int64_t rows_ws, ws_bytes;
+  int64_t few_ws, some_ws, ws_bytes;
 };
 int64_t partial_bytes(int64_t slots, int64_t rows, int64_t D) { return align256(slots * rows * D * 4) + align256(slots * rows * 4); }
+
+// A class of sequences with up to `rows` rows over `keys` keys, in work-groups of which `target` are wanted.
+bool plan_rows(RowsClass* x, int64_t least, int64_t rows, int tile_rows, int64_t B, int64_t Hkv, int64_t keys, int64_t target,
+               int splits) {
+  x->least = (int)least;
+  x->most = (int)rows;
+  x->tile_rows = tile_rows;
+  x->n_rt = (int)((rows + tile_rows - 1) / tile_rows);
+  const int64_t groups = B * Hkv * x->n_rt, blocks = keys / kRowsBlock + 1;
+  x->parts = splits > 0 ? std::min(splits, kPagedParts)
+                        : (int)std::max<int64_t>(std::min(std::min<int64_t>(kPagedParts, target / groups), blocks / 8), 1);
+  x->per_part = splits > 0 ? 1 : (int)((blocks + x->parts - 1) / x->parts);
+  if (groups * x->parts > kMaxKeys) return false;
+  x->groups = (int)(groups * x->parts);
+  x->by_rt = FastDiv::by(x->n_rt);
+  x->by_parts = FastDiv::by(x->parts);
+  return true;
+}
 
 int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size, int32_t width, int32_t S, int64_t W,
                       int64_t hint, int32_t Hq, int32_t Hkv, int32_t D, int32_t splits, PagedPlan* pl) {
@@ -87,36 +106,42 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
   const int64_t cap = int64_t(width) * page_size, rows = int64_t(g) * n;
   int64_t keys = std::min(hint > 0 ? hint : cap, cap);
   if (W != VICO_FULL_HISTORY) keys = std::min(keys, S + W + n);
-  pl->rows = true;
-  const int64_t few = std::min<int64_t>(rows, kPagedRowsMost);
-  pl->row_blocks = few > 16 ? 2 : 1;
-  pl->n_rt = (int)((few + 16 * pl->row_blocks - 1) / (16 * pl->row_blocks));
-  const int64_t groups = int64_t(B) * Hkv * pl->n_rt, blocks = keys / kRowsBlock + 1;
-  const int64_t target = (B == 1 ? 2 : 4) * kNumCUs;
-  pl->parts = splits > 0 ? std::min(splits, kPagedParts)
-                         : (int)std::max<int64_t>(std::min(std::min<int64_t>(kPagedParts, target / groups), blocks / 8), 1);
-  if (groups * pl->parts > kMaxKeys) return VICO_ERR_INVALID_ARG;
-  pl->per_part = splits > 0 ? 1 : (int)((blocks + pl->parts - 1) / pl->parts);
-  if (pl->parts > 1) pl->rows_ws = partial_bytes(groups * pl->parts, 16 * pl->row_blocks, D);
-  pl->ws_bytes = pl->rows_ws;
-  if (rows <= kPagedRowsMost) return VICO_OK;
-  // row tiles of 256: of a sequence its rows rounded up, and such a sequence has more than kPagedRowsMost
-  const int64_t all = int64_t(total) * g;
-  const int64_t items = Hkv * (all / kBlockM + std::min<int64_t>(B, all / (kPagedRowsMost + 1)));
-  pl->tile = true;
-  pl->tile_splits = std::min(splits, kPagedTileParts);
-  pl->tile_parts = (int)std::max<int64_t>(std::min<int64_t>(kPagedTileParts, keys / kKeyTile / kMinSplitTiles), 1);
-  if (splits > 0) {
-    pl->tile_slots = (int)std::min<int64_t>(items * pl->tile_splits, kMaxKeys);
-    pl->tile_grid = pl->tile_slots;
-    pl->tile_items = (int)std::min<int64_t>(items, kMaxKeys);
-  } else {
-    pl->tile_slots = kNumCUs;
-    pl->tile_grid = (int)std::max<int64_t>(items, kNumCUs);
-    pl->tile_items = (int)std::min<int64_t>(items, kNumCUs / 2);
+  // work-groups: two rounds of two a CU where sequences differ; in a launch with 256-row tiles as many as leave those
+  // room for their partial results, and no more than needed where one long sequence is all that is expected
+  const bool tile = rows > kSomeRows;
+  const int64_t groups = int64_t(B) * Hkv;
+  const int64_t target = tile && B == 1 ? 1 : tile ? std::min<int64_t>(std::max<int64_t>(8 * groups, kNumCUs), 4 * kNumCUs) : (B == 1 ? 2 : 4) * kNumCUs;
+  if (!plan_rows(&pl->few, 1, std::min<int64_t>(rows, kFewRows), 16, B, Hkv, keys, target, splits)) return VICO_ERR_INVALID_ARG;
+  if (pl->few.parts > 1) pl->few_ws = partial_bytes(pl->few.groups, 16, D);
+  if (rows > kFewRows) {
+    if (!plan_rows(&pl->some, kFewRows + 1, std::min<int64_t>(rows, kSomeRows), tile ? 16 : 32, B, Hkv, keys, tile ? std::min<int64_t>(target, kNumCUs / 4) : target, splits))
+      return VICO_ERR_INVALID_ARG;
+    if (pl->some.parts > 1) pl->some_ws = partial_bytes(pl->some.groups, pl->some.tile_rows, D);
   }
+  pl->ws_bytes = pl->few_ws + pl->some_ws;
+  if (!tile) return VICO_OK;
+  // row tiles of 256: of a sequence its rows rounded up, and such a sequence has more than kSomeRows
+  const int64_t all = int64_t(total) * g;
+  const int64_t items = Hkv * (all / kBlockM + std::min<int64_t>(B, all / (kSomeRows + 1)));
+  pl->tile_splits = std::min(splits, kPagedTileParts);
   if (items * std::max(pl->tile_splits, 1) * (kBlockM / 8) > kMaxKeys) return VICO_ERR_INVALID_ARG;
-  if (splits > 1 || (splits == 0 && pl->tile_parts > 1)) pl->ws_bytes += partial_bytes(pl->tile_slots, kBlockM, D);
+  pl->tile_items = (int)items;
+  if (splits > 0) {
+    pl->tile_slots = pl->tile_grid = (int)items * pl->tile_splits;
+  } else {
+    pl->tile_parts = (int)std::max<int64_t>(std::min<int64_t>(kPagedTileParts, keys / kKeyTile / kMinSplitTiles), 1);
+    pl->tile_slots = (int)std::min((kPagedWorkspace - pl->ws_bytes - 512) / (kBlockM * (D + 1) * 4), items * pl->tile_parts);
+    pl->tile_grid = (int)std::max<int64_t>(items, pl->tile_slots);
+    pl->tile_items = (int)std::min<int64_t>(items, pl->tile_slots / 2);
+    if (pl->tile_items == 0) pl->tile_parts = 1;
+    if (B == 1) {                            // known here: the call's rows are the one sequence's
+      pl->tile_splits = paged_tile_parts((int)items, (int)(keys / kKeyTile), pl->tile_parts, pl->tile_slots);
+      pl->tile_parts = 0;
+      pl->tile_slots = pl->tile_grid = (int)items * pl->tile_splits;
+      pl->tile_items = (int)items;
+    }
+  }
+  if (std::max(pl->tile_splits, pl->tile_parts) > 1) pl->ws_bytes += partial_bytes(pl->tile_slots, kBlockM, D);
   return VICO_OK;
 }
 
@@ -161,7 +186,7 @@ int vico_paged_attn_plan(int32_t num_seqs, int32_t total_q, int32_t max_q_len, i
   const int st = check_paged_shape(num_seqs, total_q, max_q_len, page_size, max_pages, sink_len, window, keys_hint,
                                    num_q_heads, num_kv_heads, head_dim, num_splits, &pl);
   if (st != VICO_OK) return st;
-  if (num_splits_out) *num_splits_out = std::max(std::max(pl.parts, pl.tile_splits), pl.tile && num_splits == 0 ? pl.tile_parts : 1);
+  if (num_splits_out) *num_splits_out = std::max(std::max(std::max(pl.few.parts, pl.some.parts), std::max(pl.tile_splits, pl.tile_parts)), 1);
   if (workspace_bytes_out) *workspace_bytes_out = pl.ws_bytes;
   return VICO_OK;
 }
@@ -207,30 +232,24 @@ int vico_paged_attn(const void* q, const int32_t* q_start, const int32_t* seq_le
   a.out_f32 = out_dtype == VICO_DTYPE_F32;
   const double scale = softmax_scale > 0.f ? double(softmax_scale) : 1.0 / sqrt(double(head_dim));
   a.scale_log2 = (float)(scale * 1.4426950408889634);
-  a.rows_most = kPagedRowsMost; a.n_rt = pl.n_rt; a.row_blocks = pl.row_blocks;
-  a.parts = pl.parts; a.per_part = pl.per_part;
   a.by_g = FastDiv::by(a.Hq / a.Hkv);
   a.by_kv = FastDiv::by(a.Hkv);
-  hipError_t e = hipSuccess;
-  if (pl.rows) {
-    a.by_rt = FastDiv::by(a.n_rt);
-    a.by_parts = FastDiv::by(a.parts);
-    if (a.parts > 1) {
-      a.ws_o = (float*)workspace;
-      a.ws_lse = (float*)((char*)workspace + align256(int64_t(a.B) * a.Hkv * a.n_rt * a.parts * 16 * a.row_blocks * a.D * 4));
-    }
-    e = launch_paged_rows(a, (hipStream_t)stream);
-  }
-  if (e == hipSuccess && pl.tile) {
-    a.tile_grid = pl.tile_grid; a.tile_items = pl.tile_items; a.tile_slots = pl.tile_slots;
-    a.tile_parts = pl.tile_parts; a.tile_splits = pl.tile_splits;
-    a.ws_o = nullptr;
-    if (pl.ws_bytes > pl.rows_ws) {
-      a.ws_o = (float*)((char*)workspace + pl.rows_ws);
-      a.ws_lse = (float*)((char*)a.ws_o + align256(int64_t(a.tile_slots) * kBlockM * a.D * 4));
-    }
-    e = launch_paged_tile(a, (hipStream_t)stream);
-  }
+  a.few = pl.few;
+  a.some = pl.some;
+  a.tile_least = kSomeRows + 1;
+  a.tile_grid = pl.tile_grid; a.tile_items = pl.tile_items; a.tile_slots = pl.tile_slots;
+  a.tile_parts = pl.tile_parts; a.tile_splits = pl.tile_splits;
+  char* ws = (char*)workspace;
+  auto room = [&](int64_t slots, int64_t rows_of_slot, int64_t bytes, float** o, float** lse) {
+    if (bytes == 0) return;
+    *o = (float*)ws;
+    *lse = (float*)(ws + align256(slots * rows_of_slot * a.D * 4));
+    ws += bytes;
+  };
+  room(pl.few.groups, 16, pl.few_ws, &a.few.ws_o, &a.few.ws_lse);
+  room(pl.some.groups, pl.some.tile_rows, pl.some_ws, &a.some.ws_o, &a.some.ws_lse);
+  room(pl.tile_slots, kBlockM, pl.ws_bytes - pl.few_ws - pl.some_ws, &a.ws_o, &a.ws_lse);
+  const hipError_t e = launch_paged_attention(a, (hipStream_t)stream);
   return status_of(e);
 }
 

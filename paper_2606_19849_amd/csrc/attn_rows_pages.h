@@ -53,15 +53,18 @@ __device__ __forceinline__ void paged_rows(const PagedAttnArgs& a, const RowsCla
   const int n = lane & 15, j = lane >> 4;
   const int g = a.Hq / a.Hkv;
 
-  // ---- work item: row tiles of one key range side by side, then KV heads, parts, sequences
-  int L = xcd_remap(blk, x.groups);
-  int next = x.by_rt(L);
-  const int rt = L - next * x.n_rt;
-  L = next;
-  next = a.by_kv(L);
-  const int kv = L - next * a.Hkv;
-  L = next;
-  const int b = x.by_parts(L), part = L - b * x.parts;
+  // ---- work item.  The row tiles and KV heads of one key range lie on one XCD (work-groups go round the XCDs): they
+  // share its L2, and the heads of a token its pages of memory.  Parts and sequences go round them: sequences differ in
+  // length, and whole ones on an XCD leave it with more or less than its share
+  int local = blk / kNumXcd;
+  int next = x.by_rt(local);
+  const int rt = local - next * x.n_rt;
+  local = next;
+  next = a.by_kv(local);
+  const int kv = local - next * a.Hkv;
+  next = next * kNumXcd + blk % kNumXcd;
+  if (next >= a.B * x.parts) return;
+  const int b = x.by_parts(next), turned = next - b * x.parts + b, part = turned - x.by_parts(turned) * x.parts;
 
   const Sequence s = sequence(a, b);
   const int NR = g * s.n;

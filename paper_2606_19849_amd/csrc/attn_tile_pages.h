@@ -8,14 +8,12 @@
 // with K and V loaded straight to LDS three tiles ahead and one barrier a tile.
 //   * Tiles are aligned to positions, and a wave's share of a tile is 8 consecutive
 //     rows: they lie in one page whatever its size (16 tokens at least).  So a page
-//     costs a wave one number and two buffer resources a tile, all scalar.  A resource
-//     ends behind the last row that exists: rows past the sequence, and rows of a page
-//     that is none, read as zeros.
+//     costs a wave one scalar offset a tile.
 //   * The page numbers of the part's tiles are in LDS, checked, two halves in turn: one
 //     is filled while the other is read, in the middle of it, so that no wait or
 //     barrier of its own is needed.
 //   * Between sink and window nothing is walked; what no row of the sequence sees in the
-//     two tiles there becomes zero in LDS.
+//     two tiles there, behind the sequence's end or for want of a page becomes zero in LDS.
 //   * Values that are not finite in tiles that the causal mask cuts are zeros in LDS (0
 //     times such a value would reach rows that do not see it) and are added afterwards for
 //     the rows that do.  Each wave looks at what it loaded, before the barrier that
@@ -138,12 +136,11 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
   const int L = xcd_remap(blk, n_work);
   int first_item, cnt;
   const int b = __builtin_amdgcn_readfirstlane(sequence_of_item(a, L, a.Hkv * parts, first_item, cnt));
-  const int kp = (L - first_item) / cnt, rt = cnt - 1 - (L - first_item - kp * cnt);
-  const int kv = kp / parts, part = kp - kv * parts;
+  // (in scalar registers, whatever the compiler makes of divisions and of loads whose address it cannot prove to be the
+  // same in all lanes: no branch of the key loop may be on lanes)
+  const int kp = __builtin_amdgcn_readfirstlane((L - first_item) / cnt), rt = cnt - 1 - (L - first_item - kp * cnt);
+  const int kv = __builtin_amdgcn_readfirstlane(kp / parts), part = kp - kv * parts;
   if (tid == 0) sh.odd = 0;
-
-  // (in scalar registers, whatever the compiler makes of loads whose address it cannot prove to be the same in all lanes:
-  // no branch of the key loop may be on lanes)
   Sequence s = sequence(a, b);
   s.q0 = __builtin_amdgcn_readfirstlane(s.q0);
   s.n = __builtin_amdgcn_readfirstlane(s.n);
@@ -164,12 +161,13 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
   WaveTile<D>::load_q(qf[0], a.q + ((int64_t)(s.q0 + tok) * a.Hq + head) * D + hh * 8);
 
   // ---- tiles
-  const int first_lim = lim_of_row(wrow0), last_lim = lim_of_row(wrow0 + 31);
-  const int n_tiles = tiles.upto(lim_of_row((rt + 1) * BM - 1));
-  const int t_lo = (int)((int64_t)n_tiles * part / parts), t_hi = (int)((int64_t)n_tiles * (part + 1) / parts);
+  const int first_lim = __builtin_amdgcn_readfirstlane(lim_of_row(wrow0)), last_lim = __builtin_amdgcn_readfirstlane(lim_of_row(wrow0 + 31));
+  const int n_tiles = __builtin_amdgcn_readfirstlane(tiles.upto(lim_of_row((rt + 1) * BM - 1)));
+  const int t_lo = __builtin_amdgcn_readfirstlane((int)((int64_t)n_tiles * part / parts));
+  const int t_hi = __builtin_amdgcn_readfirstlane((int)((int64_t)n_tiles * (part + 1) / parts));
   const int t_end = wave_active ? min(t_hi, tiles.upto(last_lim)) : t_lo;          // past the wave's last tile
-  const int kv_end = lim_of_row(NR - 1) + 1;                       // rows of the sequence that exist
-  const int cut_from = lim_of_row(rt * BM) + 1;                    // from here on some row of the work-group sees not all
+  const int kv_end = __builtin_amdgcn_readfirstlane(lim_of_row(NR - 1) + 1);                       // rows of the sequence that exist
+  const int cut_from = __builtin_amdgcn_readfirstlane(lim_of_row(rt * BM) + 1);                    // from here on some row of the work-group sees not all
   const int sink = s.sink, first = s.first;
   // Tiles [t_plain, t_plain + n_plain) need no mask for this wave, and [t_plain, t_plain + n_whole) none for any row of
   // the work-group: behind those that hold positions between sink and window, before the causal diagonal.  A page that
@@ -212,32 +210,49 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
     Tile::v_source(lane, r, u);
     ld_v = (uint32_t)(r * rbytes + u * 16);
   }
-  // Where the wave's rows of a tile lie: lane i of `run` has byte offset and bytes of the i-th of 64 tiles, computed for
-  // all of them at once; a tile takes its own by lane reads.
-  const uint64_t k_base = (uint64_t)a.k_pages + kv * RBY, v_base = (uint64_t)a.v_pages + kv * RBY;
+  // Where the wave's rows of a tile lie in the pools, the same in both: lane i of `run` has it for the i-th of 64 tiles,
+  // computed for all of them at once; a tile takes its own by lane reads.  It is the loads' scalar offset, below 2^31,
+  // from a resource that holds for 2 GiB of the pool; for rows without a page, page 0 is read, and look() makes them
+  // zeros.  (A resource of its own for each tile took 4 % longer: each scalar instruction between MFMAs counts.)
   const int my_page = shift < 6 ? (8 * wave) >> shift : 0, in_page = (1 << shift) - 1;
-  uint32_t run_lo = 0, run_hi = 0, run_bytes = 0;
+  uint32_t run_lo = 0, run_hi = 0;
+  // the resources, `window` 2 GiB pieces into the pools (addresses are below 2^48)
+  auto resource = [&](const uint16_t* pool, uint32_t window) __attribute__((always_inline)) {
+    const late_args l = late();
+    const uint64_t before = ((uint64_t)window << 31) + (uint32_t)(kv * RBY), p = (uint64_t)pool + before;
+    const uint64_t left = ((uint64_t)(uint32_t)l->N << l->page_shift) * (uint32_t)(l->Hkv * RBY) - before;
+    const uint32_t bytes = left > 0xFFFFFFFFull ? 0xFFFFFFFFu : (uint32_t)left;
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(p >> 32)),
+                 (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+  };
+  u32x4 run_k = resource(late()->k_pages, 0), run_v = resource(late()->v_pages, 0);
+  uint32_t run_at = 0, run_window = 0;       // of the tile to be loaded
+  bool far = false;                          // the 64 tiles lie in several windows: moved at each of them
+  auto start_tile = [&](int t) __attribute__((always_inline)) { run_at = __builtin_amdgcn_readlane(run_lo, (t - t_lo) & 63); };
+  auto move_window = [&](uint32_t window) __attribute__((always_inline)) {
+    if (window == run_window) return;
+    run_window = window;
+    run_k = resource(late()->k_pages, window);
+    run_v = resource(late()->v_pages, window);
+  };
   auto find_tiles = [&](int t) __attribute__((always_inline)) {                     // of tiles t .. t + 63
     const int tl = t + lane, e0 = (tl - t_lo) << ept_shift;
-    int bad = 0;
-    for (int e = 0; e < 1 << ept_shift; ++e) bad |= tab[(e0 + e) & (2 * kTabHalf - 1)] >> 31;
+    const int pos = tiles.position(tl), size = min(1 << shift, BN);
+    bool bad = false;                        // no page where some row sees a position
+    for (int e = 0; e < 1 << ept_shift; ++e) {
+      const int at = pos + e * size;
+      bad |= (tab[(e0 + e) & (2 * kTabHalf - 1)] < 0) & (at < kv_end) & !((at >= sink) & (at + size <= first));
+    }
     const bool some = tl < t_hi;             // past the part's last tile: nothing
-    n_plain = __builtin_amdgcn_ballot_w64(some & (bad != 0)) != 0 ? 0 : n_plain;
-    const int page = tab[(e0 + my_page) & (2 * kTabHalf - 1)], p0 = tiles.position(tl) + 8 * wave;
-    const int rows = (some & (page >= 0)) ? min(max(kv_end - p0, 0), 8) : 0;
-    const uint64_t at = (uint64_t)(uint32_t)((max(page, 0) << shift) + (p0 & in_page)) * (uint32_t)rbytes;
-    run_lo = (uint32_t)at;
-    run_hi = (uint32_t)(at >> 32);
-    run_bytes = (uint32_t)(rows * rbytes);
-  };
-  u32x4 run_k, run_v;                        // resources of the tile to be loaded
-  auto start_tile = [&](int t) __attribute__((always_inline)) {
-    const int i = (t - t_lo) & 63;
-    const uint64_t at = (uint32_t)__builtin_amdgcn_readlane(run_lo, i) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(run_hi, i) << 32;
-    const uint32_t bytes = __builtin_amdgcn_readlane(run_bytes, i);
-    const uint64_t pk = k_base + at, pv = v_base + at;                               // (below 2^48)
-    run_k = u32x4{(uint32_t)pk, (uint32_t)(pk >> 32), bytes, 0x00020000u};
-    run_v = u32x4{(uint32_t)pv, (uint32_t)(pv >> 32), bytes, 0x00020000u};
+    n_plain = __builtin_amdgcn_ballot_w64(some & bad) != 0 ? 0 : n_plain;
+    const int page = tab[(e0 + my_page) & (2 * kTabHalf - 1)], p0 = pos + 8 * wave;
+    const int there = (some & (page >= 0)) ? page : 0;
+    const uint64_t at = (uint64_t)(uint32_t)((there << shift) + (p0 & in_page)) * (uint32_t)rbytes;
+    run_lo = (uint32_t)at & 0x7FFFFFFFu;
+    run_hi = (uint32_t)(at >> 31);
+    const uint32_t window = __builtin_amdgcn_readlane(run_hi, 0);
+    far = __builtin_amdgcn_ballot_w64(some & (run_hi != window)) != 0;
+    if (!far) move_window(window);
   };
   // direct load i (0 .. NLD-1: K, NLD .. 2*NLD-1: V) to the buffers at byte offset `boff`.  m0, which holds a load's
   // LDS address, is the compiler's own: every load sets it and gives it back.  Wait states that the compiler does not
@@ -247,25 +262,28 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
     const uint32_t off = i < NLD ? ld_k[n] : ld_v + n * RPL * rbytes;
     const uint32_t to = lds0 + my_part + boff + (i < NLD ? kKBase : 0u) + n * 1024;
     const u32x4 rs = i < NLD ? run_k : run_v;
+    const uint32_t so = run_at;
     uint32_t m0;
     asm volatile(
         "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 4\n\t"
-        "buffer_load_dwordx4 %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0"
+        "buffer_load_dwordx4 %1, %2, %4 offen lds\n\ts_mov_b32 m0, %0"
         : "=&s"(m0)
-        : "v"(off), "s"(rs), "s"(to)
+        : "v"(off), "s"(rs), "s"(to), "s"(so)
         : "memory");
   };
   auto load_whole = [&](uint32_t boff, int t) __attribute__((always_inline)) {
     start_tile(t);
+    move_window(__builtin_amdgcn_readlane(run_hi, (t - t_lo) & 63));
     unrolled<NL>([&](auto i) __attribute__((always_inline)) { load_direct(i, boff); });
   };
 
-  // ---- the wave's share of V of tile t, landed at `boff`: zeros for what no row sees, and for what is not finite
-  // where the mask cuts
-  bool odd = false;
+  // ---- the wave's share of V of tile t, landed at `boff`: zeros for what no row sees (the sequence's last tile is cut by
+  // the mask, so its end is among them), and for what is not finite where the mask cuts
+  uint32_t odd = 0;
   auto look = [&](int t, uint32_t boff) __attribute__((always_inline)) {
-    if (__builtin_expect((uint32_t)(t - t_plain) >= (uint32_t)n_whole, 0)) {       // (past the last tile: zeros)
+    if (__builtin_expect((uint32_t)(t - t_plain) >= (uint32_t)n_whole || n_plain == 0, 0)) {
       const int pos = tiles.position(t);
+      const bool none = tab[(((t - t_lo) << ept_shift) + my_page) & (2 * kTabHalf - 1)] < 0;
       const uint32_t at = lds0 + boff + my_part + (uint32_t)(lane * 16);
       int r, u;
       Tile::v_source(lane, r, u);
@@ -273,7 +291,7 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
       for (int n = 0; n < NLD; ++n) {
         u32x4 y = *(lds_u4)(uintptr_t)(at + n * 1024);
         const int p = pos + 8 * wave + n * RPL + r;
-        const uint32_t keep = ((p >= sink) & (p < first)) ? 0u : ~0u;
+        const uint32_t keep = (none | ((p >= sink) & (p < first)) | (p >= kv_end)) ? 0u : ~0u;
         u16x2 most{0, 0};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -281,17 +299,11 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
           largest_exponents(most, pos + BN > cut_from ? y[i] : 0u);
           y[i] = pos + BN > cut_from ? finite_or_zero(y[i]) : y[i];
         }
-        odd |= not_finite(most);
+        odd |= not_finite(most) ? 1u : 0u;
         *(lds_u4)(uintptr_t)(at + n * 1024) = y;
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-  };
-  // tile t has landed (the loads of the AHEAD - 2 tiles after it may be in flight), for this wave and every other
-  auto landed = [&](int t, uint32_t boff) __attribute__((always_inline)) {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 2) * NL) : "memory");
-    look(t, boff);
-    barrier_keep_loads();
   };
   // what the mask takes from a half of tile t, whose keys start at position p0
   auto mask = [&](int t, int p0, f32x16& x) __attribute__((always_inline)) {
@@ -351,12 +363,19 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
       Tile wt{qf, k_rd, v_rd, v_nx, o, m_run, l_run, neg_m, vf, a.scale_log2};
       f32x16 s0[RB], s1[RB];
       bf16x8 p0[RB][2] = {}, p1[RB][2] = {};
-      auto cut = [&]() __attribute__((always_inline)) { return (uint32_t)(t - t_plain) >= (uint32_t)n_plain; };
+      // How many tiles from t on need no mask, have none to look at behind them, no page numbers to be found and no
+      // window to move: their steps ask for nothing but this, once between the halves and once at the end (no MFMA's shadow lies on either).
+      auto quiet_from = [&](int t) __attribute__((always_inline)) {
+        const int plain = (uint32_t)(t - t_plain) < (uint32_t)n_plain ? t_plain + n_plain - t : 0;
+        const int whole = (uint32_t)(t + 1 - t_plain) < (uint32_t)n_whole ? t_plain + n_whole - t - 1 : 0;
+        return far ? 0 : __builtin_amdgcn_readfirstlane(min(min(plain, whole), -(t + AHEAD + 1 - t_lo) & 63));
+      };
+      auto cut = [&](int t) __attribute__((always_inline)) { return (uint32_t)(t - t_plain) >= (uint32_t)n_plain; };
       wt.first_logits(s0);
-      if (cut()) mask(t, tiles.position(t), s0[0]);
+      if (cut(t)) mask(t, tiles.position(t), s0[0]);
       wt.first_max(s0);
+      int quiet = quiet_from(t);
       for (; t < t_end; ++t) {
-        if (__builtin_expect(cut(), 0)) mask(t, tiles.position(t), s0[0]);
         uint32_t next = 0;                   // of tile t + 1
         wt.template half<32, 48, 0>(s0, s1, p1, p0, [&](auto slot) __attribute__((always_inline)) {
           constexpr int i = decltype(slot)::value;
@@ -368,8 +387,14 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
             v_rd = v_nx;                     // V of tile t
           }
         });
-        landed(t + 1, next);
-        if (__builtin_expect(cut(), 0)) mask(t, tiles.position(t) + 32, s1[0]);
+        // tile t + 1 has landed (the loads of the AHEAD - 2 tiles after it may be in flight), for this wave ...
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 2) * NL) : "memory");
+        if (__builtin_expect(quiet <= 0, 0)) {
+          move_window(__builtin_amdgcn_readlane(run_hi, (t + AHEAD - t_lo) & 63));
+          look(t + 1, next);
+          if (cut(t)) mask(t, tiles.position(t) + 32, s1[0]);
+        }
+        barrier_keep_loads();                // ... and every other
         const uint32_t fill = (boff + AHEAD * TBY) & kWrap;
         wt.template half<0, 16, 32>(s1, s0, p0, p1, [&](auto slot) __attribute__((always_inline)) {
           constexpr int j = decltype(slot)::value, i = j / LSTEP - 1;
@@ -377,13 +402,19 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
         });
         v_nx += next - boff;                 // V of tile t + 1
         boff = next;
-        more_tab(t + AHEAD);
+        if (__builtin_expect(--quiet <= 0, 0)) {
+          more_tab(t + AHEAD);
+          quiet = quiet_from(t + 1);
+          if (cut(t + 1)) mask(t + 1, tiles.position(t + 1), s0[0]);
+        }
       }
       wt.template last_values<48>(p1);
     }
     for (; t < t_hi; ++t) {                  // tiles that this wave's rows do not see: it brings its share
       const uint32_t next = (boff + TBY) & kWrap;
-      landed(t + 1, next);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 2) * NL) : "memory");
+      look(t + 1, next);
+      barrier_keep_loads();
       load_whole((boff + AHEAD * TBY) & kWrap, t + AHEAD);
       boff = next;
       more_tab(t + AHEAD);
@@ -392,7 +423,7 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
   }
 
   // ---- values of the cut tiles that are not finite
-  if (odd) sh.odd = 1;
+  if (odd != 0) sh.odd = 1;
   __syncthreads();
   if (!wave_active) return;
   const late_args l = late();

@@ -70,7 +70,8 @@ struct RowsClass {
   int least, most, tile_rows;
   int n_rt;                 // row tiles of a sequence at most
   int parts, per_part;      // parts of its key range at most, 32-key blocks of one at least
-  int groups, merge;        // work-groups: B * parts * Hkv * n_rt; of the merge
+  int groups, merge;        // work-groups: Hkv * n_rt for each of B * parts key ranges, in eights; of the merge
+  int slots;                // partial results: B * parts * Hkv * n_rt
   float* ws_o;              // partial results [B][parts][Hkv][n_rt][tile_rows][D], and their log2-sum-exps
   float* ws_lse;
   FastDiv by_rt, by_parts;

@@ -86,8 +86,9 @@ bool plan_rows(RowsClass* x, int64_t least, int64_t rows, int tile_rows, int64_t
   x->parts = splits > 0 ? std::min(splits, kPagedParts)
                         : (int)std::max<int64_t>(std::min(std::min<int64_t>(kPagedParts, target / groups), blocks / 8), 1);
   x->per_part = splits > 0 ? 1 : (int)((blocks + x->parts - 1) / x->parts);
-  if (groups * x->parts > kMaxKeys) return false;
-  x->groups = (int)(groups * x->parts);
+  if (groups * x->parts > kMaxKeys / 8) return false;
+  x->slots = (int)(groups * x->parts);
+  x->groups = (int)((B * x->parts + 7) / 8 * 8 * Hkv * x->n_rt);
   x->by_rt = FastDiv::by(x->n_rt);
   x->by_parts = FastDiv::by(x->parts);
   return true;
@@ -106,17 +107,19 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
   const int64_t cap = int64_t(width) * page_size, rows = int64_t(g) * n;
   int64_t keys = std::min(hint > 0 ? hint : cap, cap);
   if (W != VICO_FULL_HISTORY) keys = std::min(keys, S + W + n);
-  // work-groups: two rounds of two a CU where sequences differ; in a launch with 256-row tiles as many as leave those
+  // work-groups: some rounds of them where sequences differ (answer tokens of 32 sequences of 1000 to 16000 keys, us
+  // with 4, 8, 12, 16 a CU: 123.0, 124.1, 120.7, 120.2); in a launch with 256-row tiles as many as leave those
   // room for their partial results, and no more than needed where one long sequence is all that is expected
   const bool tile = rows > kSomeRows;
   const int64_t groups = int64_t(B) * Hkv;
-  const int64_t target = tile && B == 1 ? 1 : tile ? std::min<int64_t>(std::max<int64_t>(8 * groups, kNumCUs), 4 * kNumCUs) : (B == 1 ? 2 : 4) * kNumCUs;
+  const int64_t target = tile && B == 1 ? 1 : tile ? std::min<int64_t>(std::max<int64_t>(8 * groups, kNumCUs), 4 * kNumCUs)
+                                                 : (B == 1 ? 2 : rows > kFewRows ? 4 : 12) * kNumCUs;
   if (!plan_rows(&pl->few, 1, std::min<int64_t>(rows, kFewRows), 16, B, Hkv, keys, target, splits)) return VICO_ERR_INVALID_ARG;
-  if (pl->few.parts > 1) pl->few_ws = partial_bytes(pl->few.groups, 16, D);
+  if (pl->few.parts > 1) pl->few_ws = partial_bytes(pl->few.slots, 16, D);
   if (rows > kFewRows) {
     if (!plan_rows(&pl->some, kFewRows + 1, std::min<int64_t>(rows, kSomeRows), tile ? 16 : 32, B, Hkv, keys, tile ? std::min<int64_t>(target, kNumCUs / 4) : target, splits))
       return VICO_ERR_INVALID_ARG;
-    if (pl->some.parts > 1) pl->some_ws = partial_bytes(pl->some.groups, pl->some.tile_rows, D);
+    if (pl->some.parts > 1) pl->some_ws = partial_bytes(pl->some.slots, pl->some.tile_rows, D);
   }
   pl->ws_bytes = pl->few_ws + pl->some_ws;
   if (!tile) return VICO_OK;
@@ -246,8 +249,8 @@ int vico_paged_attn(const void* q, const int32_t* q_start, const int32_t* seq_le
     *lse = (float*)(ws + align256(slots * rows_of_slot * a.D * 4));
     ws += bytes;
   };
-  room(pl.few.groups, 16, pl.few_ws, &a.few.ws_o, &a.few.ws_lse);
-  room(pl.some.groups, pl.some.tile_rows, pl.some_ws, &a.some.ws_o, &a.some.ws_lse);
+  room(pl.few.slots, 16, pl.few_ws, &a.few.ws_o, &a.few.ws_lse);
+  room(pl.some.slots, pl.some.tile_rows, pl.some_ws, &a.some.ws_o, &a.some.ws_lse);
   room(pl.tile_slots, kBlockM, pl.ws_bytes - pl.few_ws - pl.some_ws, &a.ws_o, &a.ws_lse);
   const hipError_t e = launch_paged_attention(a, (hipStream_t)stream);
   return status_of(e);

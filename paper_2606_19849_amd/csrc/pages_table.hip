@@ -25,62 +25,69 @@ constexpr int kTableThreads = 256;
 
 __device__ __forceinline__ bool is_page(int e, int n) { return (uint32_t)e < (uint32_t)n; }
 
-// ---- fork.  A work-group owns columns of the table for all rows: it reads what the
-// changed rows become into LDS before any of them is written, so rows may be taken
-// from each other in any way.
-constexpr int kForkThreads = 512;
-constexpr int kForkEntries = 32768;        // of a work-group: 128 KB of LDS
+// ---- fork.  A work-group owns columns of the table for all rows: its threads hold what the changed rows' entries
+// become, and were, in registers before any of them is written, so rows may be taken from each other in any way.
+// Few entries: one work-group takes all columns, slice after slice, and the lengths; of a large table each takes slices
+// of its own, and the lengths, which all of them read, are another launch's.  (16 of 32 rows of 190 entries: 6.4 us
+// with the new entries in LDS and their old values read after the barrier.)
+constexpr int kForkThreads = 1024, kForkPer = 8, kForkEntries = kForkThreads * kForkPer;
 
-__device__ __forceinline__ int parent_of(const PagesArgs& a, int b) {
-  const int p = a.parent[b];
-  return p == b || p < -1 || p >= a.B ? b : p;
-}
-__device__ __forceinline__ void fork_lengths(const PagesArgs& a, int32_t* lds) {
+__global__ __launch_bounds__(kForkThreads) void pages_fork_kernel(PagesArgs a) {
+  __shared__ int32_t row_s[kMaxSeqs], from_s[kMaxSeqs], len_s[kMaxSeqs], keep_s[kMaxSeqs], rows_s;
+  if (threadIdx.x == 0) rows_s = 0;
+  __syncthreads();
   for (int b = threadIdx.x; b < a.B; b += kForkThreads) {
-    const int p = parent_of(a, b);
-    lds[b] = p < 0 ? 0 : a.seq_len[p];
+    const int p = a.parent[b];
+    if (p == b || p < -1 || p >= a.B) continue;
+    const int len = p < 0 ? 0 : a.seq_len[p], i = atomicAdd(&rows_s, 1);       // (any order)
+    row_s[i] = b;
+    from_s[i] = p;
+    len_s[i] = len;
+    keep_s[i] = len > 0 ? min(((len - 1) >> a.page_shift) + 1, a.width) : 0;
   }
   __syncthreads();
-  for (int b = threadIdx.x; b < a.B; b += kForkThreads)
-    if (parent_of(a, b) != b) a.seq_len[b] = lds[b];
-}
-
-// cols: columns of a slice (a power of two).  One work-group takes all slices and the lengths; several take one each,
-// and the lengths, which all of them read, are another launch's.
-__global__ __launch_bounds__(kForkThreads) void pages_fork_kernel(PagesArgs a, int cols, int slices) {
-  __shared__ int32_t becomes[kForkEntries];
-  const int shift = 31 - __builtin_clz(cols);
-  for (int s = blockIdx.x; s < slices; s += gridDim.x) {
-    const int c0 = s * cols;
-    for (int i = threadIdx.x; i < a.B * cols; i += kForkThreads) {
-      const int b = i >> shift, c = c0 + (i & (cols - 1)), p = parent_of(a, b);
-      if (p == b || c >= a.width) continue;
-      int e = -1;
-      if (p >= 0) {
-        const int len = a.seq_len[p];
-        if (len > 0 && c <= (len - 1) >> a.page_shift) e = a.table[(int64_t)p * a.width + c];
-      }
-      becomes[i] = is_page(e, a.N) ? e : -1;
+  const int rows = rows_s;
+  if (rows == 0) return;
+  const int cols = min(kForkEntries / rows, a.width);
+  for (int c0 = blockIdx.x * cols; c0 < a.width; c0 += gridDim.x * cols) {
+    int old[kForkPer], e[kForkPer];
+    int32_t* at[kForkPer];
+#pragma unroll
+    for (int u = 0; u < kForkPer; ++u) {
+      const int i = u * kForkThreads + threadIdx.x, r = i / cols, c = c0 + i - r * cols;
+      at[u] = nullptr;
+      e[u] = old[u] = -1;
+      if (r >= rows || c >= a.width) continue;
+      at[u] = a.table + (int64_t)row_s[r] * a.width + c;
+      old[u] = *at[u];
+      if (c < keep_s[r]) e[u] = a.table[(int64_t)from_s[r] * a.width + c];
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.B * cols; i += kForkThreads) {
-      const int b = i >> shift, c = c0 + (i & (cols - 1));
-      if (parent_of(a, b) == b || c >= a.width) continue;
-      int32_t* const at = a.table + (int64_t)b * a.width + c;
-      const int old = *at, e = becomes[i];
-      if (old == e) continue;
-      *at = e;
-      if (is_page(old, a.N)) atomicSub(a.refs + old, 1);
-      if (e >= 0) atomicAdd(a.refs + e, 1);
+    __syncthreads();                      // every row of these columns is read
+#pragma unroll
+    for (int u = 0; u < kForkPer; ++u) {
+      if (!at[u]) continue;
+      const int to = is_page(e[u], a.N) ? e[u] : -1;
+      if (old[u] == to) continue;
+      *at[u] = to;
+      if (is_page(old[u], a.N)) atomicSub(a.refs + old[u], 1);
+      if (to >= 0) atomicAdd(a.refs + to, 1);
     }
-    __syncthreads();
   }
-  if (gridDim.x == 1) fork_lengths(a, becomes);
+  if (gridDim.x > 1) return;
+  for (int i = threadIdx.x; i < rows; i += kForkThreads) a.seq_len[row_s[i]] = len_s[i];
 }
 
 __global__ __launch_bounds__(kForkThreads) void pages_fork_lengths_kernel(PagesArgs a) {
-  __shared__ int32_t becomes[kMaxSeqs];
-  fork_lengths(a, becomes);
+  __shared__ int32_t len_s[kMaxSeqs];
+  for (int b = threadIdx.x; b < a.B; b += kForkThreads) {
+    const int p = a.parent[b];
+    len_s[b] = p < 0 ? 0 : a.seq_len[p < a.B ? p : 0];
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.B; b += kForkThreads) {
+    const int p = a.parent[b];
+    if (p != b && p >= -1 && p < a.B) a.seq_len[b] = len_s[b];
+  }
 }
 
 // ---- free
@@ -121,6 +128,7 @@ __device__ __forceinline__ void flag_pages(const PagesArgs& a, int block, int32_
 }
 
 // Sums over the work-group: inclusive sum of x over the threads up to this one; `total` of all.
+template <int NT = kTableThreads>
 __device__ __forceinline__ int group_scan(int x, int& total, int32_t* wave_sum) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
@@ -134,11 +142,25 @@ __device__ __forceinline__ int group_scan(int x, int& total, int32_t* wave_sum) 
   int before = 0;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kTableThreads / 64; ++w) {
+  for (int w = 0; w < NT / 64; ++w) {
     before += w < wave ? wave_sum[w] : 0;
     total += wave_sum[w];
   }
   return x + before;
+}
+
+// Position of the r-th bit that is set in x (r counts from 0, and there is one).
+__device__ __forceinline__ int nth_bit(uint64_t x, int r) {
+  int at = 0;
+#pragma unroll
+  for (int half = 32; half > 0; half >>= 1) {
+    const int n = __builtin_popcountll(x & ((uint64_t(1) << half) - 1));
+    const bool upper = n <= r;
+    r -= upper ? n : 0;
+    x = upper ? x >> half : x;
+    at += upper ? half : 0;
+  }
+  return at;
 }
 
 // The flags counted up to each block, in LDS; ranks and r-th flags from it.
@@ -186,16 +208,7 @@ struct Ranks {
       ++w;
       x = FLAG ? a.flags[w] : ~a.flags[w];
     }
-    int at = 0;                           // the r-th bit of x
-#pragma unroll
-    for (int half = 32; half > 0; half >>= 1) {
-      const int n = __builtin_popcountll(x & ((uint64_t(1) << half) - 1));
-      const bool upper = n <= r;
-      r -= upper ? n : 0;
-      x = upper ? x >> half : x;
-      at += upper ? half : 0;
-    }
-    return w * 64 + at;
+    return w * 64 + nth_bit(x, r);
   }
 };
 
@@ -312,15 +325,192 @@ __global__ __launch_bounds__(kTableThreads) void pages_compact_kernel(PagesArgs 
   }
 }
 
+// ---- small pools: one work-group, one launch, flags and counts in LDS.  (2300 pages, 32 rows, 16 of them with new
+// tokens: 9 us in two launches.)
+constexpr int kSmallThreads = 1024;
+constexpr int kSmallPages = 65536;         // reserve: a count for each word of flags is one a thread
+constexpr int kSmallEntries = 65536;       // of the table
+
+struct SmallRanks {                        // as Ranks, from words of flags in LDS
+  uint64_t flags[kSmallPages / 64];
+  int32_t upto[kSmallPages / 64];          // flags in the words before
+  int32_t wave_sum[kSmallThreads / 64];
+  // every thread: after the flags have been written; returns their number
+  __device__ __forceinline__ int count(int words) {
+    __syncthreads();
+    const int n = (int)threadIdx.x < words ? __builtin_popcountll(flags[threadIdx.x]) : 0;
+    int total;
+    const int incl = group_scan<kSmallThreads>(n, total, wave_sum);
+    if ((int)threadIdx.x < words) upto[threadIdx.x] = incl - n;
+    __syncthreads();
+    return total;
+  }
+  __device__ __forceinline__ bool set(int p) const { return (flags[p >> 6] >> (p & 63)) & 1; }
+  __device__ __forceinline__ int below(int p) const {
+    return upto[p >> 6] + __builtin_popcountll(flags[p >> 6] & ((uint64_t(1) << (p & 63)) - 1));
+  }
+  template <bool FLAG>
+  __device__ __forceinline__ int nth(int r, int words) const {
+    auto before = [&](int w) { return FLAG ? upto[w] : w * 64 - upto[w]; };
+    int lo = 0, hi = words;                // the last word with before(w) <= r
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (before(mid) <= r) lo = mid;
+      else hi = mid;
+    }
+    return lo * 64 + nth_bit(FLAG ? flags[lo] : ~flags[lo], r - before(lo));
+  }
+};
+
+// The new tokens' entries of all rows are numbered one after the other, which is the order that free pages are given
+// out in; a thread takes every 1024th.
+__global__ __launch_bounds__(kSmallThreads) void pages_reserve_small_kernel(PagesArgs a) {
+  __shared__ SmallRanks free;
+  __shared__ uint64_t once[kSmallPages / 64];
+  __shared__ int32_t end_s[kMaxSeqs], need_s[kMaxSeqs], upto_s[kMaxSeqs];      // of each row: entries and wants up to its end
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int words = (a.N + 63) / 64;
+  for (int i0 = 0; i0 < a.N; i0 += 4 * kSmallThreads) {
+    int c[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int p = i0 + u * kSmallThreads + tid;
+      c[u] = p < a.N ? a.refs[p] : 2;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint64_t none = __builtin_amdgcn_ballot_w64(c[u] <= 0), one = __builtin_amdgcn_ballot_w64(c[u] == 1);
+      const int w = (i0 + u * kSmallThreads) / 64 + wave;
+      if (lane == 0 && w < words) {
+        free.flags[w] = none;
+        once[w] = one;
+      }
+    }
+  }
+  int entries = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kSmallThreads) {
+    const int b = b0 + tid;
+    int H, j0 = 0, j1 = 0;
+    bool ok = true;
+    if (b < a.B) {
+      ok = new_entries(a, b, H, j0, j1);
+      need_s[b] = 0;
+    }
+    int sum;
+    const int incl = group_scan<kSmallThreads>(j1 - j0, sum, free.wave_sum);
+    if (b < a.B) {
+      end_s[b] = entries + incl;
+      if (j1 == j0) {                     // nothing new, or no room in the table
+        a.granted[b] = ok;
+        a.moves[2 * b] = -1;
+        a.moves[2 * b + 1] = -1;
+      }
+    }
+    entries += sum;
+  }
+  const int n_free = free.count(words);
+  // the wants of each row, and up to its end
+  int H = 0, j0 = 0, j = 0, e = -1, row = 0, rank = 0;
+  bool wants = false;
+  auto look_at = [&](int i) {
+    int lo = -1, hi = a.B - 1;            // the first row whose end is past i
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (end_s[mid] > i) hi = mid;
+      else lo = mid;
+    }
+    row = hi;
+    int j1;
+    new_entries(a, row, H, j0, j1);
+    j = j0 + i - (row > 0 ? end_s[row - 1] : 0);
+    e = a.table[(int64_t)row * a.width + j];
+    wants = !(is_page(e, a.N) && ((once[e >> 6] >> (e & 63)) & 1));
+  };
+  int wanted = 0;
+  for (int i0 = 0; i0 < entries; i0 += kSmallThreads) {
+    const int i = i0 + tid;
+    wants = false;
+    if (i < entries) look_at(i);
+    int sum;
+    rank = wanted + group_scan<kSmallThreads>(wants, sum, free.wave_sum);
+    if (i < entries) {
+      if (wants) atomicAdd(&need_s[row], 1);
+      if (i == end_s[row] - 1) upto_s[row] = rank;
+    }
+    wanted += sum;
+  }
+  __syncthreads();
+  int given = 0;
+  for (int i0 = 0; i0 < entries; i0 += kSmallThreads) {
+    const int i = i0 + tid;
+    if (entries > kSmallThreads) {        // (a single round has its entries still)
+      wants = false;
+      if (i < entries) look_at(i);
+      int sum;
+      rank = given + group_scan<kSmallThreads>(wants, sum, free.wave_sum);
+      given += sum;
+    }
+    if (i >= entries) continue;
+    const bool ok = need_s[row] == 0 || upto_s[row] <= n_free;
+    const int p = wants && ok ? free.nth<true>(rank - 1, words) : -1;
+    const bool held = p >= 0 && is_page(e, a.N) && !free.set(e);
+    if (j == j0) {
+      const bool moves = held && (H & ((1 << a.page_shift) - 1)) != 0;
+      a.granted[row] = ok;
+      a.moves[2 * row] = moves ? e : -1;
+      a.moves[2 * row + 1] = moves ? p : -1;
+    }
+    if (p < 0) continue;
+    a.table[(int64_t)row * a.width + j] = p;
+    a.refs[p] = 1;
+    if (held) atomicSub(a.refs + e, 1);
+  }
+}
+
+constexpr int kSmallCompact = 16 * kSmallThreads;      // pages, and entries: those of a thread stay in its registers
+__global__ __launch_bounds__(kSmallThreads) void pages_compact_small_kernel(PagesArgs a) {
+  __shared__ SmallRanks used;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int words = (a.N + 63) / 64, entries = a.B * a.width;
+  int c[kSmallCompact / kSmallThreads], e[kSmallCompact / kSmallThreads];
+#pragma unroll
+  for (int u = 0; u < kSmallCompact / kSmallThreads; ++u) {
+    const int i = u * kSmallThreads + tid;
+    c[u] = i < a.N ? a.refs[i] : 0;
+    e[u] = i < entries ? a.table[i] : -1;
+  }
+#pragma unroll
+  for (int u = 0; u < kSmallCompact / kSmallThreads; ++u) {
+    const uint64_t set = __builtin_amdgcn_ballot_w64(c[u] > 0);
+    const int w = u * (kSmallThreads / 64) + wave;
+    if (lane == 0 && w < words) used.flags[w] = set;
+  }
+  const int U = used.count(words), low = U < a.N ? used.below(U) : U, moved = U - low;
+  if (tid == 0) *a.count = moved;
+#pragma unroll
+  for (int u = 0; u < kSmallCompact / kSmallThreads; ++u) {
+    const int i = u * kSmallThreads + tid;
+    if (i < a.N && i >= U && c[u] > 0) {
+      const int m = used.below(i) - low, to = used.nth<false>(m, words);
+      a.moves[2 * m] = i;
+      a.moves[2 * m + 1] = to;
+      a.refs[to] = c[u];
+      a.refs[i] = 0;
+    }
+    if (e[u] >= U && e[u] < a.N && used.set(e[u])) a.table[i] = used.nth<false>(used.below(e[u]) - low, words);
+  }
+  for (int i = moved + tid; i < a.max_moves; i += kSmallThreads) {
+    a.moves[2 * i] = -1;
+    a.moves[2 * i + 1] = -1;
+  }
+}
+
 }  // namespace
 
 hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream) {
-  int cols = 64;
-  while (cols * a.B > kForkEntries) cols /= 2;          // B <= 4096: eight at least
-  const int slices = (a.width + cols - 1) / cols;
-  // few entries: one work-group, one launch
-  const int groups = (int64_t)a.B * a.width <= 16384 ? 1 : slices;
-  hipLaunchKernelGGL(pages_fork_kernel, dim3(groups), dim3(kForkThreads), 0, stream, a, cols, slices);
+  const int cols = std::max(kForkEntries / a.B, 1), slices = (a.width + cols - 1) / cols;
+  const int groups = (int64_t)a.B * a.width <= kSmallEntries ? 1 : std::min(slices, 1024);
+  hipLaunchKernelGGL(pages_fork_kernel, dim3(groups), dim3(kForkThreads), 0, stream, a);
   if (groups > 1) hipLaunchKernelGGL(pages_fork_lengths_kernel, dim3(1), dim3(kForkThreads), 0, stream, a);
   return hipGetLastError();
 }
@@ -332,6 +522,10 @@ hipError_t launch_pages_free(const PagesArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream) {
+  if (a.N <= kSmallPages && (int64_t)a.B * a.width <= kSmallEntries) {
+    hipLaunchKernelGGL(pages_reserve_small_kernel, dim3(1), dim3(kSmallThreads), 0, stream, a);
+    return hipGetLastError();
+  }
   constexpr int rows = kTableThreads / 64;
   hipLaunchKernelGGL(pages_count_kernel, dim3(a.n_blocks + (a.B + rows - 1) / rows), dim3(kTableThreads), 0, stream, a);
   hipLaunchKernelGGL(pages_reserve_kernel, dim3(a.B), dim3(kTableThreads), 0, stream, a);
@@ -339,6 +533,10 @@ hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t stream) {
+  if (a.N <= kSmallCompact && (int64_t)a.B * a.width <= kSmallCompact) {
+    hipLaunchKernelGGL(pages_compact_small_kernel, dim3(1), dim3(kSmallThreads), 0, stream, a);
+    return hipGetLastError();
+  }
   const int64_t work = std::max<int64_t>((int64_t)a.B * a.width, a.max_moves);
   const int groups = (int)std::min<int64_t>((work + kTableThreads - 1) / kTableThreads, 1024);
   hipLaunchKernelGGL(pages_in_use_kernel, dim3(a.n_blocks), dim3(kTableThreads), 0, stream, a);

@@ -57,7 +57,7 @@ def guarded(x, extra=8):
 
 
 TABLES = [(1, 16, 8, 4), (3, 16, 40, 9), (7, 64, 300, 70), (33, 16, 1500, 64), (65, 32, 5000, 130), (130, 16, 3000, 33),
-          (600, 16, 6000, 12)]
+          (600, 16, 6000, 12), (130, 16, 70000, 600), (3000, 16, 20000, 30)]
 
 
 @pytest.mark.parametrize("rows,page,N,width", TABLES)

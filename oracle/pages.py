@@ -100,30 +100,32 @@ def paged_attention(q, q_start, seq_len, k_pages, v_pages, table, sink=0, window
                     max_q=None, bound=None):
     """(out [rows, Hq, d], lse [Hq, rows], covered [rows]) in float64; out is 0 and lse -inf for a row without keys.
 
-    bound: called for every row and head group with (row, heads, q of the heads, K, V of the visible keys, p)."""
+    bound: called for every sequence and KV head with (rows, heads, K and V of the keys that some row sees, p)."""
     N, page, Hkv, d = k_pages.shape
     rows, Hq, _ = q.shape
     g, s = Hq // Hkv, (1.0 / math.sqrt(d) if scale is None else scale)
     out, lse, covered = np.zeros((rows, Hq, d)), np.full((Hq, rows), -np.inf), np.zeros(rows, bool)
     for b, row in enumerate(table):
         n = q_start[b + 1] - q_start[b]
-        for i in range(n if max_q is None else min(n, max_q)):
-            t = q_start[b] + i
-            covered[t] = True
-            pos = visible(row, seq_len[b], n, i, page, N, sink, window, bidirectional)
-            if not pos:
-                continue
-            pos = np.array(pos)
-            ids = np.array(row)[pos // page]
-            K, V = k_pages[ids, pos % page], v_pages[ids, pos % page]        # [keys, Hkv, d]
-            for h in range(Hkv):
-                hs = slice(h * g, (h + 1) * g)
-                z = s * (q[t, hs] @ K[:, h].T)
-                m = z.max(1, keepdims=True)
-                p = np.exp(z - m)
+        m = n if max_q is None else min(n, max_q)
+        rs = slice(q_start[b], q_start[b] + m)
+        covered[rs] = True
+        pos = np.array(visible(row, seq_len[b], n, n - 1, page, N, sink, window, bidirectional), dtype=np.int64) if m else []
+        if len(pos) == 0:
+            continue
+        ids = np.array(row)[pos // page]
+        K, V = k_pages[ids, pos % page], v_pages[ids, pos % page]            # [keys, Hkv, d]
+        seen = pos[None] <= seq_len[b] + (np.full(m, n - 1) if bidirectional else np.arange(m))[:, None]
+        some = seen.any(1)
+        for h in range(Hkv):
+            for hq in range(h * g, (h + 1) * g):
+                z = np.where(seen, s * (q[rs, hq] @ K[:, h].T), -np.inf)
+                top = np.where(some, z.max(1), 0.0)[:, None]
+                p = np.exp(z - top)
                 total = p.sum(1, keepdims=True)
-                out[t, hs] = (p / total) @ V[:, h]
-                lse[hs, t] = (m + np.log(total))[:, 0]
+                p /= np.where(total > 0, total, 1.0)
+                out[rs, hq] = p @ V[:, h]
+                lse[hq, rs] = np.where(some, top[:, 0] + np.log(np.where(total > 0, total, 1.0))[:, 0], -np.inf)
                 if bound is not None:
-                    bound(t, hs, q[t, hs], K[:, h], V[:, h], p / total)
+                    bound(rs, hq, K[:, h], V[:, h], p)
     return out, lse, covered

@@ -59,9 +59,8 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArg
 // Work-groups of the merge for a class: none for a single part.
 template <int D>
 int merge_groups(const RowsClass& x, int B, int Hkv) {
-  constexpr int per = kMergeThreads / (D / 4);      // rows of a work-group with one thread for four columns
-  if (x.parts <= 1) return 0;
-  return B * Hkv * x.n_rt * x.tile_rows / per * (x.parts <= 8 ? 1 : 8);
+  const int per = kMergeThreads / (D / 4) / (x.parts <= 8 ? 1 : 8);      // rows of a work-group
+  return x.parts <= 1 ? 0 : B * Hkv * x.n_rt * ((x.merge_rows + per - 1) / per);
 }
 
 template <int D>

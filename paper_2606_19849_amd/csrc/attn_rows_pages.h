@@ -311,8 +311,8 @@ __device__ __forceinline__ void paged_rows_merge(const PagedAttnArgs& a, const R
   __shared__ float m_s[PG][RPB][NQ], l_s[PG][RPB][NQ];
   __shared__ f32x4 acc_s[PG][RPB][NQ];
   const int tid = threadIdx.x, dq = tid % NQ, pg = tid / NQ % PG, rr = tid / (NQ * PG);
-  const int RT = x.tile_rows, chunks = RT / RPB;
-  const int L = blk / chunks, r = (blk - L * chunks) * RPB + rr;      // RPB divides RT
+  const int RT = x.tile_rows, chunks = (x.merge_rows + RPB - 1) / RPB;       // (RPB divides RT)
+  const int L = blk / chunks, r = (blk - L * chunks) * RPB + rr;
   int next = x.by_rt(L);
   const int rt = L - next * x.n_rt;
   const int b = a.by_kv(next), kv = next - b * a.Hkv;

@@ -72,8 +72,15 @@ __device__ __forceinline__ int all_row_tiles(const PagedAttnArgs& a, int& parts)
   if (a.tile_parts <= 1 || items == 0) return items;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) keys = max(keys, __shfl_xor(keys, o, 64));
-  keys = __builtin_amdgcn_readfirstlane(keys);
-  parts = paged_tile_parts(items, keys, a.tile_parts, a.tile_slots);
+  // lane p - 1 takes p parts; of equal times the fewest
+  static_assert(kPagedTileParts <= 64, "one lane for each number of parts");
+  const int p = lane + 1;
+  const bool fits = p <= a.tile_parts && (p == 1 || items <= a.tile_slots / p);
+  int best = fits ? (int)min(paged_tile_cost(items, keys, p), (int64_t)(1 << 24) - 1) : 1 << 24;
+  best = best * 64 + lane;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) best = min(best, __shfl_xor(best, o, 64));
+  parts = (__builtin_amdgcn_readfirstlane(best) & 63) + 1;
   return items;
 }
 // The sequence whose row tiles, each `times` times, hold item x; its first item and its row tiles.

@@ -68,6 +68,7 @@ constexpr int kPagedTileParts = 16;   // and of a 256-row tile
 // Sequences of `least` to `most` packed rows, on row tiles of tile_rows rows.
 struct RowsClass {
   int least, most, tile_rows;
+  int merge_rows;           // of a row tile, rows that a sequence may have there
   int n_rt;                 // row tiles of a sequence at most
   int parts, per_part;      // parts of its key range at most, 32-key blocks of one at least
   int groups, merge;        // work-groups: Hkv * n_rt for each of B * parts key ranges, in eights; of the merge
@@ -104,16 +105,14 @@ struct PagedAttnArgs {
 // tiles (1.35 us with heads of size 128): rounds of work-groups over the CUs, each a start, an end and its keys, then
 // the merge and the partial results' way to memory and back.  (3B heads, 64 row tiles of 139 tiles, us measured with
 // the chunk kernel: 2 parts 126, 3 91.7, 4 84.7, 6 105, 8 96.7.)
-__host__ __device__ inline int paged_tile_parts(int items, int tiles, int most, int slots) {
-  int best = 1 << 30, parts = 1;
-  for (int p = 1; p <= most && (p == 1 || items * p <= slots); ++p) {
-    const int rounds = (items * p + kNumCUs - 1) / kNumCUs;
-    const int cost = 32 * rounds * (6 + (tiles + p - 1) / p) + (p > 1 ? 64 + items * p * 5 / 4 : 0);
-    if (cost < best) {
-      best = cost;
-      parts = p;
-    }
-  }
+__host__ __device__ inline int64_t paged_tile_cost(int items, int tiles, int p) {
+  const int64_t rounds = ((int64_t)items * p + kNumCUs - 1) / kNumCUs;
+  return 32 * rounds * (6 + (tiles + p - 1) / p) + (p > 1 ? 64 + (int64_t)items * p * 5 / 4 : 0);
+}
+inline int paged_tile_parts(int items, int tiles, int most, int slots) {
+  int parts = 1;
+  for (int p = 2; p <= most && items * p <= slots; ++p)
+    if (paged_tile_cost(items, tiles, p) < paged_tile_cost(items, tiles, parts)) parts = p;
   return parts;
 }
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream);

@@ -65,12 +65,13 @@ void use_workspace(PagesArgs* a, void* workspace) {
 
 // ---- attention: the classes of sequences that a call may have, and how their keys are split.
 constexpr int kFewRows = 16;
-constexpr int kSomeRows = 128;                                             // more: 256-row tiles
+constexpr int kSomeRows = 64;                                              // more: 256-row tiles, in a launch that has them
+constexpr int kRowsOnly = 1024;                                            // a launch may do without them up to here
 constexpr int64_t kPagedWorkspace = int64_t(64) << 20;                     // most bytes of a split picked by the library
 
 struct PagedPlan {
   RowsClass few, some;
-  int tile_grid, tile_items, tile_slots, tile_parts, tile_splits;
+  int some_most, tile_grid, tile_items, tile_slots, tile_parts, tile_splits;
   int64_t few_ws, some_ws, ws_bytes;
 };
 int64_t partial_bytes(int64_t slots, int64_t rows, int64_t D) { return align256(slots * rows * D * 4) + align256(slots * rows * 4); }
@@ -82,6 +83,7 @@ bool plan_rows(RowsClass* x, int64_t least, int64_t rows, int tile_rows, int64_t
   x->most = (int)rows;
   x->tile_rows = tile_rows;
   x->n_rt = (int)((rows + tile_rows - 1) / tile_rows);
+  x->merge_rows = (int)std::min<int64_t>(rows, tile_rows);
   const int64_t groups = B * Hkv * x->n_rt, blocks = keys / kRowsBlock + 1;
   x->parts = splits > 0 ? std::min(splits, kPagedParts)
                         : (int)std::max<int64_t>(std::min(std::min<int64_t>(kPagedParts, target / groups), blocks / 8), 1);
@@ -92,6 +94,25 @@ bool plan_rows(RowsClass* x, int64_t least, int64_t rows, int tile_rows, int64_t
   x->by_rt = FastDiv::by(x->n_rt);
   x->by_parts = FastDiv::by(x->parts);
   return true;
+}
+
+// Whether the call does without 256-row tiles: its time on row tiles of 32 against theirs, from the rows that its sequences
+// have on average.  Each row tile of 32 streams its keys for itself, 1.6 ns for a 32-key block with all CUs at work (1.1
+// with heads of size 64); 256 rows read them once, but a launch with such tiles starts slowly and has few of them.
+// Measured, us, 32-row tiles / 256-row tiles, 7B heads: one sequence of 126 rows over 8000 keys 20.5 / 30.9, 252 rows
+// 25.9 / 36.6, 511 rows 34.0 / 42.2, over 40000 keys 108.5 / 83.6; eight of 35 rows over 8000 keys 42.3 / 39.9, of 70
+// rows 55.7 / 41.1, of 252 rows over 1000 keys 32.2 / 37.7, over 8000 keys 93.9 / 60.2; 3B heads, eight of 144 rows over
+// 8000 keys 50.1 / 41.5; small heads, one of 292 rows over 8000 keys 14.7 / 25.5, eight 47.9 / 37.9.
+bool rows_alone(int64_t B, int64_t rows, int64_t all, int64_t Hkv, int64_t keys, int D) {
+  if (rows > kRowsOnly) return false;
+  const double tiles32 = double(Hkv) * (double(all) / 32 + double(B));
+  const double t_rows = (D == 128 ? 12.0 : 8.0) + (D == 128 ? 1.6e-3 : 1.1e-3) * tiles32 * double(keys) / kRowsBlock;
+  const int64_t each = std::max<int64_t>((all / B + kBlockM - 1) / kBlockM, 1), items = Hkv * B * each;
+  if (items > (1 << 20)) return false;
+  const int tiles = (int)(keys / kKeyTile) + 1;
+  const int p = paged_tile_parts((int)items, tiles, std::max(std::min(tiles / kMinSplitTiles, kPagedTileParts), 1), 450);
+  const double t_tile = 4.0 + (D == 128 ? 1.35 : 0.9) / 32 * double(paged_tile_cost((int)items, tiles, p));
+  return t_rows <= t_tile;
 }
 
 int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size, int32_t width, int32_t S, int64_t W,
@@ -106,25 +127,27 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
   if (n == 0 || B == 0) return VICO_OK;
   const int64_t cap = int64_t(width) * page_size, rows = int64_t(g) * n;
   int64_t keys = std::min(hint > 0 ? hint : cap, cap);
-  if (W != VICO_FULL_HISTORY) keys = std::min(keys, S + W + n);
+  if (W != VICO_FULL_HISTORY && W < keys) keys = std::min(keys, S + W + n);
   // work-groups: some rounds of them where sequences differ (answer tokens of 32 sequences of 1000 to 16000 keys, us
   // with 4, 8, 12, 16 a CU: 123.0, 124.1, 120.7, 120.2); in a launch with 256-row tiles as many as leave those
   // room for their partial results, and no more than needed where one long sequence is all that is expected
-  const bool tile = rows > kSomeRows;
+  const int64_t all = int64_t(total) * g;
+  const bool tile = rows > kSomeRows && !rows_alone(B, rows, all, Hkv, keys, D);
+  const int64_t some_most = tile ? kSomeRows : rows;
   const int64_t groups = int64_t(B) * Hkv;
   const int64_t target = tile && B == 1 ? 1 : tile ? std::min<int64_t>(std::max<int64_t>(8 * groups, kNumCUs), 4 * kNumCUs)
                                                  : (B == 1 ? 2 : rows > kFewRows ? 4 : 12) * kNumCUs;
   if (!plan_rows(&pl->few, 1, std::min<int64_t>(rows, kFewRows), 16, B, Hkv, keys, target, splits)) return VICO_ERR_INVALID_ARG;
   if (pl->few.parts > 1) pl->few_ws = partial_bytes(pl->few.slots, 16, D);
   if (rows > kFewRows) {
-    if (!plan_rows(&pl->some, kFewRows + 1, std::min<int64_t>(rows, kSomeRows), tile ? 16 : 32, B, Hkv, keys, tile ? std::min<int64_t>(target, kNumCUs / 4) : target, splits))
+    if (!plan_rows(&pl->some, kFewRows + 1, some_most, tile ? 16 : 32, B, Hkv, keys, tile ? std::min<int64_t>(target, kNumCUs / 4) : target, splits))
       return VICO_ERR_INVALID_ARG;
     if (pl->some.parts > 1) pl->some_ws = partial_bytes(pl->some.slots, pl->some.tile_rows, D);
   }
+  pl->some_most = (int)some_most;
   pl->ws_bytes = pl->few_ws + pl->some_ws;
   if (!tile) return VICO_OK;
   // row tiles of 256: of a sequence its rows rounded up, and such a sequence has more than kSomeRows
-  const int64_t all = int64_t(total) * g;
   const int64_t items = Hkv * (all / kBlockM + std::min<int64_t>(B, all / (kSomeRows + 1)));
   pl->tile_splits = std::min(splits, kPagedTileParts);
   if (items * std::max(pl->tile_splits, 1) * (kBlockM / 8) > kMaxKeys) return VICO_ERR_INVALID_ARG;
@@ -239,7 +262,7 @@ int vico_paged_attn(const void* q, const int32_t* q_start, const int32_t* seq_le
   a.by_kv = FastDiv::by(a.Hkv);
   a.few = pl.few;
   a.some = pl.some;
-  a.tile_least = kSomeRows + 1;
+  a.tile_least = pl.some_most + 1;
   a.tile_grid = pl.tile_grid; a.tile_items = pl.tile_items; a.tile_slots = pl.tile_slots;
   a.tile_parts = pl.tile_parts; a.tile_splits = pl.tile_splits;
   char* ws = (char*)workspace;

@@ -95,9 +95,9 @@ class Cache:
         kmax, most = np.zeros((rows, self.Hq)), [1]
         s = self.D ** -0.5 if scale is None else scale
 
-        def bound(t, hs, qt, K, V, p):
-            A[t, hs] = p @ np.abs(V)
-            kmax[t, hs] = np.sqrt((K ** 2).sum(-1)).max()
+        def bound(rs, hq, K, V, p):
+            A[rs, hq] = p @ np.abs(V)
+            kmax[rs, hq] = np.sqrt((K ** 2).sum(-1)).max()
             most[0] = max(most[0], K.shape[0])
 
         out, lse, covered = pages.paged_attention(q, self.q_start, self.H, k, v, self.table, self.sink, self.window,

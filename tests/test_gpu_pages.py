@@ -15,6 +15,7 @@ from tests._pages import DEV, Cache, check, f64, i32
 pytestmark = pytest.mark.gpu
 
 H128, H7B, H3B, ODD = (4, 2, 128), (28, 4, 128), (16, 2, 128), (6, 2, 64)
+WIDE, SMALL = (18, 2, 128), (17, 1, 64)       # from 57 and 61 tokens on, a sequence has rows for 256-row tiles
 
 
 # ---------------------------------------------------------------- the table
@@ -219,7 +220,7 @@ SEQS = {
     "decode": [(1, 200)],
     "decodes": [(1, 0), (1, 15), (1, 16), (1, 31), (1, 700), (0, 9), (1, 64), (1, 63)],
     "short": [(5, 33), (2, 0), (0, 0), (17, 480), (3, 47)],
-    "mixed": [(1, 90), (150, 77), (1, 1), (64, 0), (7, 300)],
+    "mixed": [(1, 90), (150, 77), (1, 1), (64, 0), (3, 20), (7, 300)],
     "chunk": [(333, 190)],
     "chunks": [(129, 64), (200, 0), (1, 33), (65, 700), (256, 63)],
 }
@@ -230,7 +231,7 @@ MASKS = [dict(), dict(sink=5, window=40), dict(sink=40, window=17), dict(window=
 @pytest.mark.parametrize("mask", MASKS, ids=str)
 @pytest.mark.parametrize("name", SEQS)
 def test_attention(name, mask, page):
-    heads = {16: ODD, 64: (4, 4, 128), 256: H128}[page]
+    heads = {16: SMALL, 64: WIDE, 256: H128}[page]
     c = Cache(len(name) + page, SEQS[name], heads=heads, page=page, **mask).device()
     check(c, c.attention(), c.oracle())
     check(c, c.attention(dtype=torch.bfloat16, splits=5, lse=False), c.oracle())
@@ -238,42 +239,47 @@ def test_attention(name, mask, page):
 
 @pytest.mark.parametrize("heads", [H7B, H3B, (1, 1, 64), (8, 1, 64), (9, 3, 128), (40, 2, 64)], ids=str)
 def test_attention_heads(heads):
-    for seqs in ([(1, 300), (1, 35)], [(9, 60), (70, 20)]):
+    for seqs in ([(1, 300), (1, 35)], [(9, 60), (70, 20)], [(9, 60), (1100 * heads[1] // heads[0] + 1, 20)]):
         c = Cache(sum(heads), seqs, heads=heads, page=32, sink=16, window=100).device()
         check(c, c.attention(), c.oracle())
 
 
 @pytest.mark.parametrize("splits", [1, 2, 7, 33, 64, 1000])
 def test_attention_parts(splits):
-    for seqs in ([(1, 2500), (1, 7), (1, 900)], [(9, 1500), (40, 100)]):
-        c = Cache(splits, seqs, heads=H128, page=16).device()
+    for seqs, heads in (([(1, 2500), (1, 7), (1, 900)], H128), ([(9, 1500), (40, 100)], H128), ([(60, 900), (2, 100), (4, 300)], WIDE)):
+        c = Cache(splits, seqs, heads=heads, page=16).device()
         check(c, c.attention(splits=splits), c.oracle())
 
 
 @pytest.mark.parametrize("hint", [1, 100, 1 << 20])
 def test_attention_hints(hint):
-    c = Cache(7, [(1, 1300), (30, 600), (1, 2)], heads=H128, page=64).device()
-    check(c, c.attention(hint=hint), c.oracle())
+    for heads in (H128, (40, 1, 128)):
+        c = Cache(7, [(1, 1300), (30, 600), (1, 2)], heads=heads, page=64).device()
+        check(c, c.attention(hint=hint), c.oracle())
 
 
 @pytest.mark.parametrize("mask", MASKS[:3], ids=str)
 def test_attention_bidirectional(mask):
-    c = Cache(11, SEQS["mixed"], heads=H128, page=32, **mask).device()
-    check(c, c.attention(flags=vico.VICO_ATTN_BIDIRECTIONAL), c.oracle(bidirectional=True))
+    for heads in (H128, WIDE):
+        c = Cache(11, SEQS["mixed"], heads=heads, page=32, **mask).device()
+        check(c, c.attention(flags=vico.VICO_ATTN_BIDIRECTIONAL), c.oracle(bidirectional=True))
 
 
 def test_attention_scale_and_fewer_rows():
     c = Cache(12, SEQS["short"], heads=ODD, page=16).device()
     check(c, c.attention(scale=0.31), c.oracle(scale=float(np.float32(0.31))))
     check(c, c.attention(max_q=3), c.oracle(max_q=3))
+    c = Cache(12, SEQS["mixed"], heads=WIDE, page=16).device()
+    check(c, c.attention(scale=0.31, max_q=120), c.oracle(scale=float(np.float32(0.31)), max_q=120))
 
 
 def test_attention_past_the_table():
     # positions that the table has no entry for: their keys are not seen, their rows see the rest
     c = Cache(13, [(20, 40), (3, 100)], heads=ODD, page=16, width=3).device()
     check(c, c.attention(), c.oracle())
-    c = Cache(13, [(120, 40), (90, 3), (70, 500)], heads=ODD, page=16, width=7).device()
-    check(c, c.attention(), c.oracle())
+    for heads in (ODD, SMALL):
+        c = Cache(13, [(120, 40), (90, 3), (70, 500)], heads=heads, page=16, width=7).device()
+        check(c, c.attention(), c.oracle())
 
 
 @pytest.mark.parametrize("window", [-1, 40000])
@@ -281,22 +287,23 @@ def test_attention_past_the_table():
 def test_long_histories_of_small_pages(splits, window):
     # more pages a part than the 256-row kernel holds at once
     for page in (16, 32):
-        c = Cache(25, [(70, 46000 * page // 16)], heads=(4, 2, 64), page=page, sink=100, window=window).device()
+        c = Cache(25, [(69, 46000 * page // 16)], heads=(15, 1, 64), page=page, sink=100, window=window).device()
         check(c, c.attention(splits=splits), c.oracle())
 
 
 @pytest.mark.parametrize("seqs,drop", [([(1, 100)], {(0, 0)}), ([(1, 40)], {(0, 0), (0, 1), (0, 2)}), ([(70, 90), (1, 50)], {(0, 2), (1, 1), (0, 9)}),
                                        ([(3, 13)], {(0, 0)}), ([(200, 400), (90, 31)], {(0, 0), (0, 7), (0, 8), (0, 30), (1, 1), (1, 7)})], ids=str)
 def test_attention_without_some_pages(seqs, drop):
-    c = Cache(14, seqs, heads=H128, page=16, drop=drop).device()
-    check(c, c.attention(), c.oracle())
+    for heads in (H128, WIDE):
+        c = Cache(14, seqs, heads=heads, page=16, drop=drop).device()
+        check(c, c.attention(), c.oracle())
 
 
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("seqs", [[(1, 70), (2, 33)], [(9, 60)], [(150, 77)], [(300, 200), (1, 5)], [(90, 300), (260, 3)]], ids=str)
 def test_values_that_are_not_finite(seqs, value):
-    for mask in (dict(), dict(sink=8, window=30)):
-        c = Cache(15, seqs, heads=H128, page=16, **mask)
+    for mask, g in ((dict(), 2), (dict(sink=8, window=30), 2), (dict(), 9), (dict(sink=8, window=30), 9)):
+        c = Cache(15, seqs, heads=(2 * g, 2, 128), page=16, **mask)
         zero = []
         for b, (n, H) in enumerate(seqs):
             lo = H - 30 if mask else 0
@@ -312,33 +319,33 @@ def test_values_that_are_not_finite(seqs, value):
                 for i in range(c.n[b]):
                     t = c.q_start[b] + i
                     if p <= c.H[b] + i:
-                        got = out[t, 2 * h:2 * h + 2, d]
-                        assert not torch.isfinite(got).any(), (b, p, i)
-                        out[t, 2 * h:2 * h + 2, d] = torch.tensor(ref[0][t, 2 * h:2 * h + 2, d], dtype=torch.float32, device=DEV)
+                        hs = slice(g * h, g * h + g)
+                        assert not torch.isfinite(out[t, hs, d]).any(), (b, p, i)
+                        out[t, hs, d] = torch.tensor(ref[0][t, hs, d], dtype=torch.float32, device=DEV)
             check(c, (out, lse), ref)
 
 
 def test_nan_keys_stay_in_the_rows_that_see_them():
-    c = Cache(16, [(40, 50), (1, 30)], heads=H128, page=16)
-    page, at = c.place(0, 70)
-    c.k[page, at, 0, 3] = float("nan")
-    c.device()
-    for splits in (0, 4):
-        out, lse = c.attention(splits=splits)
-        clean = Cache(16, [(40, 50), (1, 30)], heads=H128, page=16).device()
-        clean.parts = c.parts
-        ref = clean.oracle()
-        assert torch.isnan(out[20:40, :2]).all() and torch.isnan(lse[:2, 20:40]).all()
-        out[20:40, :2] = torch.tensor(ref[0][20:40, :2], dtype=torch.float32, device=DEV)
-        lse[:2, 20:40] = torch.tensor(ref[1][:2, 20:40], dtype=torch.float32, device=DEV)
-        check(c, (out, lse), ref)
+    for g in (2, 30):
+        c = Cache(16, [(40, 50), (1, 30)], heads=(2 * g, 2, 128), page=16)
+        page, at = c.place(0, 70)
+        c.k[page, at, 0, 3] = float("nan")
+        c.device()
+        for splits in (0, 4):
+            out, lse = c.attention(splits=splits)
+            clean = Cache(16, [(40, 50), (1, 30)], heads=(2 * g, 2, 128), page=16).device()
+            clean.parts = c.parts
+            ref = clean.oracle()
+            assert torch.isnan(out[20:40, :g]).all() and torch.isnan(lse[:g, 20:40]).all()
+            out[20:40, :g] = torch.tensor(ref[0][20:40, :g], dtype=torch.float32, device=DEV)
+            lse[:g, 20:40] = torch.tensor(ref[1][:g, 20:40], dtype=torch.float32, device=DEV)
+            check(c, (out, lse), ref)
 
 
 def test_large_logits():
-    c = Cache(17, [(1, 400), (37, 100)], heads=H128, page=16, sigma=40.0).device()
-    out, lse = c.attention()
-    ref = c.oracle()
-    check(c, (out, lse), ref)
+    for heads in (H128, (30, 1, 128)):
+        c = Cache(17, [(1, 400), (37, 100)], heads=heads, page=16, sigma=40.0).device()
+        check(c, c.attention(), c.oracle())
 
 
 def test_arrays_that_make_no_sense_stay_in_bounds():
@@ -358,7 +365,7 @@ def test_arrays_that_make_no_sense_stay_in_bounds():
             vico.vico_pages_fork(c.dt.clone(), refs, c.dl.clone(), i32([1, 0]), 16)
             torch.cuda.synchronize()
     # starts that go up and down: more rows than the call has
-    c = Cache(19, [(100, 30)] + [(0, 30)] * 9, heads=H128, page=16).device()
+    c = Cache(19, [(100, 30)] + [(0, 30)] * 9, heads=WIDE, page=16).device()
     c.ds = i32([0, 100, 0, 100, 0, 100, 0, 100, 0, 100, 0])
     for splits in (0, 1, 4):
         c.attention(splits=splits, max_q=100)
@@ -371,7 +378,7 @@ def test_pool_past_the_32bit_offset_limit():
     ids = [4199, 3, 2101, 4100]
     g = torch.Generator()
     g.manual_seed(5)
-    n, H, rows = 33, 3 * page + 100, 33
+    n, H = 150, 3 * page + 100
     c = Cache(19, [(1, 1)], heads=H7B, page=page)
     c.n, c.H, c.q_start, c.width, c.page = [n], [H], [0, n], 4, page
     c.q = (torch.randn(n, 28, D, generator=g) * 2).to(torch.bfloat16)
@@ -387,7 +394,6 @@ def test_pool_past_the_32bit_offset_limit():
     vico.vico_paged_append(new_k, new_v, s, l, k, v, t)
     c.k[3, 100:100 + n], c.v[3, 100:100 + n] = new_k.cpu(), new_v.cpu()
     c.dk, c.dv, c.dq, c.dt, c.ds, c.dl = k, v, c.q.to(DEV), t, s, l
-    rows = [0, 17, 32]
     out, lse = c.attention()
     ref = c.oracle(max_q=None)
     check(c, (out, lse), ref)
@@ -499,7 +505,7 @@ def capture(f):
 
 
 def test_a_step_replays_as_a_graph():
-    c = Cache(21, [(1, 90), (150, 77), (1, 1)], heads=H128, page=16, sink=8, window=60).device()
+    c = Cache(21, [(1, 90), (150, 77), (1, 1)], heads=WIDE, page=16, sink=8, window=60).device()
     eager = c.attention()
     out, lse = torch.zeros_like(eager[0]), torch.zeros_like(eager[1])
     ws = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
@@ -544,7 +550,7 @@ def test_a_step_replays_as_a_graph():
 
 def test_on_another_stream_and_twice_at_once():
     a = Cache(22, [(1, 900), (40, 100)], heads=H128, page=16).device()
-    b = Cache(23, [(1, 700), (1, 40), (9, 300)], heads=H128, page=64).device()
+    b = Cache(23, [(1, 700), (1, 40), (90, 300)], heads=WIDE, page=64).device()
     ra, rb = a.oracle(), b.oracle()
     s, t = torch.cuda.Stream(), torch.cuda.Stream()
     check(a, a.attention(stream=s), ra)
@@ -564,7 +570,7 @@ def test_on_another_stream_and_twice_at_once():
 
 
 def test_results_repeat():
-    c = Cache(24, [(1, 3000), (70, 500), (1, 80)], heads=H7B, page=16).device()
+    c = Cache(24, [(1, 3000), (170, 500), (20, 600), (1, 80)], heads=H7B, page=16).device()
     first = c.attention(dtype=torch.bfloat16)
     for _ in range(3):
         again = c.attention(dtype=torch.bfloat16)

@@ -40,7 +40,8 @@
  *                     calls' q, k, v and out, and take positions seq_len[b] ...
  * The caller moves seq_len on after the last layer.  All of these live in device
  * memory, so the device checks them: a position without a page is neither
- * written nor attended to, rows outside [0, total) do not exist.
+ * written nor attended to, rows outside [0, total) do not exist.  A table or pool
+ * without an entry is VICO_ERR_CAPACITY where a call has something to do with it.
  */
 #ifndef VICO_PAGES_H
 #define VICO_PAGES_H
@@ -94,8 +95,9 @@ int vico_paged_append(const void* k, const void* v, int32_t total_tokens, const 
  *                  (<= 64)
  *   workspace      at least the bytes that vico_paged_attn_plan reports for the
  *                  same arguments (at most 64 MiB with num_splits = 0)
- * total_q <= 2^20; out is below 2^31 bytes as fp32.  A pool or a table without an
- * entry is VICO_ERR_CAPACITY where there are rows.
+ * total_q <= 2^20; out is below 2^31 bytes as fp32; calls that would take 2^22
+ * work-groups or more (num_seqs * num_kv_heads past some hundred thousand) are
+ * VICO_ERR_INVALID_ARG.
  *
  * Arithmetic: as for vico_chunk_prefill_attn.  A NaN or an infinity in the value
  * of a key reaches the rows that see the key, as one or the other and whatever

@@ -151,6 +151,7 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
   Sequence s = sequence(a, b);
   s.q0 = __builtin_amdgcn_readfirstlane(s.q0);
   s.n = __builtin_amdgcn_readfirstlane(s.n);
+  s.all = __builtin_amdgcn_readfirstlane(s.all);
   s.H = __builtin_amdgcn_readfirstlane(s.H);
   s.sink = __builtin_amdgcn_readfirstlane(s.sink);
   s.first = __builtin_amdgcn_readfirstlane(s.first);

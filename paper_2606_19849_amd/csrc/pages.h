@@ -121,7 +121,7 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream);
 // into range here: whatever the arrays hold, rows lie in [0, total) and positions in
 // [0, width * page_size).
 struct Sequence {
-  int q0, n;                // its first row, its rows
+  int q0, n, all;           // its first row, its rows that are computed, its rows
   int H;                    // tokens before them
   int sink, first;          // visible before the new tokens: [0, sink) and [first, H), sink <= first
 };
@@ -132,7 +132,8 @@ __device__ __forceinline__ int rows_of(const A& a, int b, int& q0) {
 }
 __device__ __forceinline__ Sequence sequence(const PagedAttnArgs& a, int b) {
   Sequence s;
-  s.n = min(rows_of(a, b, s.q0), a.max_q);
+  s.all = rows_of(a, b, s.q0);
+  s.n = min(s.all, a.max_q);
   s.H = min(max(a.seq_len[b], 0), a.width << a.page_shift);
   s.first = a.W < 0 || a.W >= s.H ? 0 : s.H - (int)a.W;
   s.sink = min(a.S, s.first);
@@ -140,7 +141,7 @@ __device__ __forceinline__ Sequence sequence(const PagedAttnArgs& a, int b) {
 }
 // A row's last position: token t of the sequence's chunk.
 __device__ __forceinline__ int last_position(const PagedAttnArgs& a, const Sequence& s, int t) {
-  return min(s.H + (a.bidir ? s.n - 1 : t), (a.width << a.page_shift) - 1);
+  return min(s.H + (a.bidir ? s.all - 1 : t), (a.width << a.page_shift) - 1);
 }
 // Blocks of BN positions (a power of two): those of the sink, then those from the window on; the first block after the
 // sink's, and how many there are up to position `last`.

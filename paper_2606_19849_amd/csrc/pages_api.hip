@@ -65,6 +65,7 @@ void use_workspace(PagesArgs* a, void* workspace) {
 
 // ---- attention: the classes of sequences that a call may have, and how their keys are split.
 constexpr int kFewRows = 16;
+constexpr int64_t kMaxGroups = int64_t(1) << 23;                           // work-groups of a launch: fewer
 constexpr int kSomeRows = 64;                                              // more: 256-row tiles, in a launch that has them
 constexpr int kRowsOnly = 1024;                                            // a launch may do without them up to here
 constexpr int64_t kPagedWorkspace = int64_t(64) << 20;                     // most bytes of a split picked by the library
@@ -88,9 +89,11 @@ bool plan_rows(RowsClass* x, int64_t least, int64_t rows, int tile_rows, int64_t
   x->parts = splits > 0 ? std::min(splits, kPagedParts)
                         : (int)std::max<int64_t>(std::min(std::min<int64_t>(kPagedParts, target / groups), blocks / 8), 1);
   x->per_part = splits > 0 ? 1 : (int)((blocks + x->parts - 1) / x->parts);
-  if (groups * x->parts > kMaxKeys / 8) return false;
+  // (a launch has fewer than 2^32 threads: 512 a work-group, and 256 in the merge, with a row or more)
+  const int64_t launched = (B * x->parts + 7) / 8 * 8 * Hkv * x->n_rt;
+  if (launched >= kMaxGroups / 2 || (x->parts > 1 && groups * tile_rows >= kMaxGroups / 2)) return false;
   x->slots = (int)(groups * x->parts);
-  x->groups = (int)((B * x->parts + 7) / 8 * 8 * Hkv * x->n_rt);
+  x->groups = (int)launched;
   x->by_rt = FastDiv::by(x->n_rt);
   x->by_parts = FastDiv::by(x->parts);
   return true;
@@ -150,7 +153,7 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
   // row tiles of 256: of a sequence its rows rounded up, and such a sequence has more than kSomeRows
   const int64_t items = Hkv * (all / kBlockM + std::min<int64_t>(B, all / (kSomeRows + 1)));
   pl->tile_splits = std::min(splits, kPagedTileParts);
-  if (items * std::max(pl->tile_splits, 1) * (kBlockM / 8) > kMaxKeys) return VICO_ERR_INVALID_ARG;
+  if (items * std::max(pl->tile_splits, 8) >= kMaxGroups / 2) return VICO_ERR_INVALID_ARG;
   pl->tile_items = (int)items;
   if (splits > 0) {
     pl->tile_slots = pl->tile_grid = (int)items * pl->tile_splits;

@@ -184,10 +184,20 @@ struct Ranks {
   __device__ __forceinline__ int below(int p) const {
     const int block = p / kPageBlock;
     if (block >= a.n_blocks) return total;
+    uint64_t x[kPageBlock / 64];
+    words(block, x);
     int n = upto[block];
-    for (int w = block * (kPageBlock / 64); w < (p >> 6); ++w) n += __builtin_popcountll(a.flags[w]);
-    const int bit = p & 63;
-    return bit == 0 ? n : n + __builtin_popcountll(a.flags[p >> 6] & ((uint64_t(1) << bit) - 1));
+#pragma unroll
+    for (int w = 0; w < kPageBlock / 64; ++w) {
+      const int bits = min(max(p - block * kPageBlock - 64 * w, 0), 64);         // of this word, those below p
+      n += __builtin_popcountll(bits == 64 ? x[w] : x[w] & ((uint64_t(1) << bits) - 1));
+    }
+    return n;
+  }
+  // the words of a block, all loads together
+  __device__ __forceinline__ void words(int block, uint64_t (&x)[kPageBlock / 64]) const {
+#pragma unroll
+    for (int w = 0; w < kPageBlock / 64; ++w) x[w] = a.flags[block * (kPageBlock / 64) + w];
   }
   // page of the r-th flag that is set (FLAG) or not (r counts from 0, and there is one)
   template <bool FLAG>
@@ -200,13 +210,20 @@ struct Ranks {
       else hi = mid;
     }
     r -= before(lo);
-    int w = lo * (kPageBlock / 64);
-    const int last = w + kPageBlock / 64 - 1;
-    uint64_t x = FLAG ? a.flags[w] : ~a.flags[w];
-    while (w < last && __builtin_popcountll(x) <= r) {
-      r -= __builtin_popcountll(x);
-      ++w;
-      x = FLAG ? a.flags[w] : ~a.flags[w];
+    uint64_t y[kPageBlock / 64];
+    words(lo, y);
+    uint64_t x = 0;
+    int w = 0;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < kPageBlock / 64; ++i) {
+      const uint64_t z = FLAG ? y[i] : ~y[i];
+      const int n = __builtin_popcountll(z);
+      const bool here = !found & (r < n);
+      x = here ? z : x;
+      w = here ? lo * (kPageBlock / 64) + i : w;
+      found |= here;
+      r -= found ? 0 : n;
     }
     return w * 64 + nth_bit(x, r);
   }

@@ -263,6 +263,8 @@ def test_attention_bidirectional(mask):
     for heads in (H128, WIDE):
         c = Cache(11, SEQS["mixed"], heads=heads, page=32, **mask).device()
         check(c, c.attention(flags=vico.VICO_ATTN_BIDIRECTIONAL), c.oracle(bidirectional=True))
+        # fewer rows than a sequence has still see all of its chunk
+        check(c, c.attention(flags=vico.VICO_ATTN_BIDIRECTIONAL, max_q=70), c.oracle(bidirectional=True, max_q=70))
 
 
 def test_attention_scale_and_fewer_rows():

@@ -75,7 +75,8 @@ def _attn(**kw):
     (dict(q=A + 8), -4), (dict(vp=A + 4 * G + 8), -4), (dict(out=A + 6 * G + 2), -4), (dict(lse=A + 7 * G + 2), -4),
     (dict(ws=A + 8 * G + 4), -4), (dict(pt=A + 5 * G + 1), -4), (dict(ws=None, splits=4), -5), (dict(wb=1000, splits=4), -5),
     (dict(out=A), -1), (dict(out=A + 3 * G), -1), (dict(lse=A + 6 * G), -1), (dict(ws=A + 4 * G, splits=4), -1),
-    (dict(lse=A + 5 * G), -1)])
+    (dict(lse=A + 5 * G), -1),
+    (dict(B=4096, Hq=1024, Hkv=1024, D=64, total=4096, most=2), -1)])          # more work-groups than a launch has
 def test_attention_rejects_bad_arguments(kw, status):
     assert _attn(**kw) == status
 

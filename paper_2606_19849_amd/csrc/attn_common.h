@@ -42,6 +42,17 @@ __device__ __forceinline__ float pair_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Inclusive sum over the lanes up to this one: inside the rows of 16, then across them.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);       // row_shr 1, 2, 4, 8: 0 from outside of the row
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);      // lane 15 of a row to the next one: rows 1, 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);      // lane 31 to rows 2, 3
+  return x;
+}
+
 // The log2-sum-exp that a key-range part leaves for the merge: NaN where the
 // part's sum is (a NaN or infinite logit), or the merge would take the part for
 // one that saw no key and drop it.

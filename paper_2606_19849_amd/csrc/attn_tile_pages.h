@@ -45,15 +45,6 @@ __device__ __forceinline__ int row_tiles(const PagedAttnArgs& a, int b) {
   const int rows = a.Hq / a.Hkv * min(rows_of(a, b, q0), a.max_q);
   return rows >= a.tile_least ? (rows + kBlockM - 1) / kBlockM : 0;
 }
-__device__ __forceinline__ int wave_scan(int x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o, 64);
-    x += lane >= o ? y : 0;
-  }
-  return x;
-}
 // Row tiles of all sequences and heads, and the parts that their key ranges are split into.
 __device__ __forceinline__ int all_row_tiles(const PagedAttnArgs& a, int& parts) {
   const int lane = threadIdx.x & 63;
@@ -139,7 +130,12 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
   int parts;
   const int items = all_row_tiles(a, parts), n_work = items * parts;
   // (starts that decrease may count rows twice: more partial results than there is room for)
-  if (blk >= n_work || (parts > 1 && n_work > a.tile_slots)) return;
+  const bool fits = parts == 1 || (n_work <= a.tile_slots && items <= a.tile_items);
+  if (blk == 0 && tid == 0 && a.ws_items) {
+    a.ws_items->items = fits && parts > 1 ? items : 0;
+    a.ws_items->parts = parts;
+  }
+  if (blk >= n_work || !fits) return;
   const int L = xcd_remap(blk, n_work);
   int first_item, cnt;
   const int b = __builtin_amdgcn_readfirstlane(sequence_of_item(a, L, a.Hkv * parts, first_item, cnt));
@@ -156,6 +152,8 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
   s.sink = __builtin_amdgcn_readfirstlane(s.sink);
   s.first = __builtin_amdgcn_readfirstlane(s.first);
   const int NR = g * s.n;
+  if (parts > 1 && part == 0 && tid == 0)
+    a.ws_items->item[(unsigned)first_item / (unsigned)parts + kv * cnt + cnt - 1 - rt] = TileItem{s.q0, NR, kv, rt, L, cnt};
   const KeyBlocks<BN> tiles(s);
   auto lim_of_row = [&](int r) __attribute__((always_inline)) { return last_position(a, s, a.by_g(min(r, NR - 1))); };
 
@@ -520,32 +518,27 @@ constexpr int kTileMergeRows = 32;         // rows of a work-group
 template <int D>
 __device__ __forceinline__ void paged_tile_merge(const PagedAttnArgs& a, int blk) {
   constexpr int NQ = D / 4, RPB = kMergeThreads / NQ, CH = kBlockM / kTileMergeRows;
-  int parts;
-  const int items = all_row_tiles(a, parts);
   const int it = blk / CH;
-  if (parts == 1 || it >= items || items * parts > a.tile_slots) return;
-  int first_item, cnt;
-  const int b = sequence_of_item(a, it, a.Hkv, first_item, cnt);
-  const int kv = (it - first_item) / cnt, rt = it - first_item - kv * cnt;
-  const Sequence s = sequence(a, b);
+  const TileItem x = a.ws_items->item[it];       // (whatever stands there past the last one)
+  const int parts = a.ws_items->parts;
+  if (it >= a.ws_items->items) return;
   const int g = a.Hq / a.Hkv, dq = threadIdx.x % NQ;
-  const int64_t item0 = ((int64_t)first_item * parts + (int64_t)kv * parts * cnt + cnt - 1 - rt) * kBlockM;
-  const int64_t step = (int64_t)cnt * kBlockM;
+  const int64_t item0 = (int64_t)x.slot * kBlockM, step = (int64_t)x.step * kBlockM;
 #pragma unroll
   for (int i = 0; i < kTileMergeRows / RPB; ++i) {
-    const int r = (blk - it * CH) * kTileMergeRows + i * RPB + threadIdx.x / NQ, pr = rt * kBlockM + r;
-    if (pr >= g * s.n) return;
+    const int r = (blk - it * CH) * kTileMergeRows + i * RPB + threadIdx.x / NQ, pr = x.rt * kBlockM + r;
+    if (pr >= x.rows) return;
     float lse2;
     f32x4 acc;
     if (parts <= 2) acc = joined<D, 2>(a, item0 + r, step, parts, dq, lse2);
     else if (parts <= 4) acc = joined<D, 4>(a, item0 + r, step, parts, dq, lse2);
     else if (parts <= 8) acc = joined<D, 8>(a, item0 + r, step, parts, dq, lse2);
     else acc = joined<D, 16>(a, item0 + r, step, parts, dq, lse2);
-    const int t = a.by_g(pr), h = kv * g + pr - t * g;
-    const int64_t orow = (int64_t)(s.q0 + t) * a.Hq + h;
+    const int t = a.by_g(pr), h = x.kv * g + pr - t * g;
+    const int64_t orow = (int64_t)(x.q0 + t) * a.Hq + h;
     if (a.out_f32) *(f32x4*)((float*)a.out + orow * D + dq * 4) = acc;
     else *(bf16x4*)((__bf16*)a.out + orow * D + dq * 4) = bf16x4{(__bf16)acc[0], (__bf16)acc[1], (__bf16)acc[2], (__bf16)acc[3]};
-    if (dq == 0 && a.lse) a.lse[(int64_t)h * a.total + s.q0 + t] = lse2 * kLn2;
+    if (dq == 0 && a.lse) a.lse[(int64_t)h * a.total + x.q0 + t] = lse2 * kLn2;
   }
 }
 

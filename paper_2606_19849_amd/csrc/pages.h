@@ -100,6 +100,16 @@ struct PagedAttnArgs {
   int tile_least, tile_grid, tile_merge, tile_items, tile_slots, tile_splits, tile_parts;
   float* ws_o;              // partial results of 256-row tiles [slot][256][D], and their log2-sum-exps (null: no parts)
   float* ws_lse;
+  struct TileItems* ws_items;
+};
+// What the 256-row kernel leaves for the merge: the row tiles that it has split, found by no search of their sequences.
+struct TileItem {
+  int q0, rows, kv, rt;     // the sequence's first row and packed rows, the head, the row tile
+  int slot, step;           // of the first part's result, and on to the next part's
+};
+struct TileItems {
+  int items, parts;         // (items: 0 where nothing is split)
+  TileItem item[1];         // tile_items of them
 };
 // Parts of the key ranges of `items` row tiles over `tiles` 64-key tiles: the number with the least time, counted in such
 // tiles (1.35 us with heads of size 128): rounds of work-groups over the CUs, each a start, an end and its keys, then

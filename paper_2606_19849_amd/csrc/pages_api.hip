@@ -70,6 +70,8 @@ constexpr int kSomeRows = 64;                                              // mo
 constexpr int kRowsOnly = 1024;                                            // a launch may do without them up to here
 constexpr int64_t kPagedWorkspace = int64_t(64) << 20;                     // most bytes of a split picked by the library
 
+int64_t items_bytes(int64_t items) { return align256(sizeof(TileItems) + items * sizeof(TileItem)); }
+
 struct PagedPlan {
   RowsClass few, some;
   int some_most, tile_grid, tile_items, tile_slots, tile_parts, tile_splits;
@@ -159,7 +161,7 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
     pl->tile_slots = pl->tile_grid = (int)items * pl->tile_splits;
   } else {
     pl->tile_parts = (int)std::max<int64_t>(std::min<int64_t>(kPagedTileParts, keys / kKeyTile / kMinSplitTiles), 1);
-    pl->tile_slots = (int)std::min((kPagedWorkspace - pl->ws_bytes - 512) / (kBlockM * (D + 1) * 4), items * pl->tile_parts);
+    pl->tile_slots = (int)std::min((kPagedWorkspace - pl->ws_bytes - items_bytes(1024) - 512) / (kBlockM * (D + 1) * 4), items * pl->tile_parts);
     pl->tile_grid = (int)std::max<int64_t>(items, pl->tile_slots);
     pl->tile_items = (int)std::min<int64_t>(items, pl->tile_slots / 2);
     if (pl->tile_items == 0) pl->tile_parts = 1;
@@ -170,7 +172,8 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
       pl->tile_items = (int)items;
     }
   }
-  if (std::max(pl->tile_splits, pl->tile_parts) > 1) pl->ws_bytes += partial_bytes(pl->tile_slots, kBlockM, D);
+  if (std::max(pl->tile_splits, pl->tile_parts) > 1)
+    pl->ws_bytes += items_bytes(pl->tile_items) + partial_bytes(pl->tile_slots, kBlockM, D);
   return VICO_OK;
 }
 
@@ -277,7 +280,11 @@ int vico_paged_attn(const void* q, const int32_t* q_start, const int32_t* seq_le
   };
   room(pl.few.slots, 16, pl.few_ws, &a.few.ws_o, &a.few.ws_lse);
   room(pl.some.slots, pl.some.tile_rows, pl.some_ws, &a.some.ws_o, &a.some.ws_lse);
-  room(pl.tile_slots, kBlockM, pl.ws_bytes - pl.few_ws - pl.some_ws, &a.ws_o, &a.ws_lse);
+  if (pl.ws_bytes > pl.few_ws + pl.some_ws) {
+    a.ws_items = (TileItems*)ws;
+    ws += items_bytes(pl.tile_items);
+    room(pl.tile_slots, kBlockM, partial_bytes(pl.tile_slots, kBlockM, a.D), &a.ws_o, &a.ws_lse);
+  }
   const hipError_t e = launch_paged_attention(a, (hipStream_t)stream);
   return status_of(e);
 }

@@ -16,6 +16,7 @@
 
 #include <algorithm>
 
+#include "attn_common.h"
 #include "pages.h"
 
 namespace vico {
@@ -131,11 +132,7 @@ __device__ __forceinline__ void flag_pages(const PagesArgs& a, int block, int32_
 template <int NT = kTableThreads>
 __device__ __forceinline__ int group_scan(int x, int& total, int32_t* wave_sum) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o, 64);
-    x += lane >= o ? y : 0;
-  }
+  x = wave_scan(x);
   __syncthreads();                        // wave_sum is free
   if (lane == 63) wave_sum[wave] = x;
   __syncthreads();

@@ -64,16 +64,6 @@ struct Segments {
     slot = hi > lo ? (int)lo : 0;
     return hi > lo ? (int)(hi - lo) : 0;
   }
-  // inclusive sum over the lanes up to this one: inside the rows of 16, then across them
-  static __device__ __forceinline__ int scan(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);       // row_shr 1, 2, 4, 8: 0 from outside of the row
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);      // lane 15 of a row to the next one: rows 1, 3
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);      // lane 31 to rows 2, 3
-    return x;
-  }
   // The state is the kernel's locals, the table in LDS, the lanes' window of it and the window's first segment:
   Lds& l;
   int &incl, &shift, &win;
@@ -85,7 +75,7 @@ struct Segments {
     int slot = 0;
     if (n <= 64) {
       const int len = lane < n ? clipped(start, length, lane, cap, slot) : 0;
-      incl = scan(len);
+      incl = wave_scan(len);
       shift = slot - (incl - len);
       return __builtin_amdgcn_readlane(incl, 63);
     }
@@ -97,7 +87,7 @@ struct Segments {
       l.shift[s] = slot;
       run += len[e];
     }
-    const int upto = scan(run);
+    const int upto = wave_scan(run);
     if (lane == 63) l.wave[tid >> 6] = upto;
     __syncthreads();
     int base = upto - run;

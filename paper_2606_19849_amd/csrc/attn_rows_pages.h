@@ -54,8 +54,10 @@ __device__ __forceinline__ void paged_rows(const PagedAttnArgs& a, const RowsCla
   const int g = a.Hq / a.Hkv;
 
   // ---- work item.  The row tiles and KV heads of one key range lie on one XCD (work-groups go round the XCDs): they
-  // share its L2, and the heads of a token its pages of memory.  Parts and sequences go round them: sequences differ in
-  // length, and whole ones on an XCD leave it with more or less than its share
+  // share its L2, and the heads of a token its pages of memory.  Parts and sequences go round them, each sequence's
+  // parts from another XCD on: short sequences have the first parts only.  (32 sequences of 1000 to 16000 keys in 8
+  // parts, us a call: so 122; every sequence's first part on the first XCD 150; the heads of a token on different XCDs
+  // 136; a stretch of sequences on each XCD 123.)
   int local = blk / kNumXcd;
   int next = x.by_rt(local);
   const int rt = local - next * x.n_rt;

@@ -304,8 +304,8 @@ __device__ __forceinline__ void paged_rows(const PagedAttnArgs& a, const RowsCla
 // The parts of a row tile joined: PG groups of threads take every PG-th part, D / 4
 // threads four columns each; all loads of a thread are on their way together.
 //     lse = log2 sum_s 2^lse_s,   O = sum_s 2^(lse_s - lse) O_s
-// A part without a key of the row (lse_s = -inf) counts for nothing; a NaN or an
-// infinity of a part reaches the row whatever the part's weight.
+// A part without a key of the row (lse_s = -inf) is all zeros; a NaN or an
+// infinity of a part reaches the row whatever the part's weight, 0 as well.
 constexpr int kMergeThreads = 256;
 template <int D, int PG>
 __device__ __forceinline__ void paged_rows_merge(const PagedAttnArgs& a, const RowsClass& x, int blk) {
@@ -346,7 +346,7 @@ __device__ __forceinline__ void paged_rows_merge(const PagedAttnArgs& a, const R
     for (int i = 0; i < NP; ++i) {
       const float w = __builtin_amdgcn_exp2f(ls[i] - use);
       l += w;
-      acc += ls[i] == -INFINITY ? f32x4{0.f, 0.f, 0.f, 0.f} : w * os[i];
+      acc += w * os[i];
     }
     m = mx;
   }

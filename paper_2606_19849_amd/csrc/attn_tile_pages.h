@@ -499,7 +499,7 @@ __device__ __forceinline__ f32x4 joined(const PagedAttnArgs& a, int64_t row0, in
   float ls[NP];
   f32x4 os[NP];
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {             // past the last part: the last one again, left out below
+  for (int i = 0; i < NP; ++i) {             // past the last part: the last one again, with a weight of 0
     const int64_t at = row0 + min(i, parts - 1) * step;
     ls[i] = i < parts ? a.ws_lse[at] : -INFINITY;
     os[i] = *(const f32x4*)(a.ws_o + at * D + dq * 4);
@@ -514,7 +514,7 @@ __device__ __forceinline__ f32x4 joined(const PagedAttnArgs& a, int64_t row0, in
   for (int i = 0; i < NP; ++i) {
     const float w = __builtin_amdgcn_exp2f(ls[i] - use);
     sum += w;
-    acc += ls[i] == -INFINITY ? f32x4{0.f, 0.f, 0.f, 0.f} : w * os[i];
+    acc += w * os[i];
   }
   acc *= sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
   lse2 = sum > 0.f ? use + __log2f(sum) : sum == sum ? -INFINITY : sum;

@@ -344,6 +344,26 @@ def test_nan_keys_stay_in_the_rows_that_see_them():
             check(c, (out, lse), ref)
 
 
+@pytest.mark.parametrize("n", [1, 20, 200])
+def test_values_of_keys_whose_logits_are_minus_infinity(n):
+    """A weight of 0 in every part that has the key, and in the whole row: a value that is not finite reaches the row."""
+    c = Cache(25, [(n, 500)], heads=(8, 1, 128), page=16)
+    c.q[:, :, 3] = 1.0
+    for p in range(192):
+        page, at = c.place(0, p)
+        c.k[page, at, 0, 3] = -float("inf")
+    page, at = c.place(0, 40)
+    outs = []
+    for value in (0.0, float("inf")):
+        c.v[page, at, 0, 9] = value
+        c.device()
+        outs.append([c.attention(splits=splits) for splits in (0, 1, 4, 9)])
+    other = [d for d in range(128) if d != 9]
+    for (x, xl), (y, yl) in zip(*outs):
+        assert torch.isfinite(x[:n]).all() and not torch.isfinite(y[:n, :, 9]).any()
+        assert torch.equal(x[:, :, other], y[:, :, other]) and torch.equal(xl, yl)
+
+
 def test_large_logits():
     for heads in (H128, (30, 1, 128)):
         c = Cache(17, [(1, 400), (37, 100)], heads=heads, page=16, sigma=40.0).device()

@@ -9,9 +9,11 @@
 // Calls of one class, or of the first two, have kernels of four waves of which a CU
 // holds several, so that one's start is hidden behind another's keys.  With
 // the third, one launch does all: work-groups of the matrix cores first, which are
-// long, then those that stream keys.  (A chunk of 1024 tokens beside 31 answer tokens, 7B
-// heads, windows of 8192 keys: 225 us, 149 and 99 each alone; 362 in two launches and two
-// merges, row tiles of 32 for the answer tokens.)
+// long, then those that stream keys, in parts that count both (paged_tile_cost).  Every
+// work-group reads all lengths, a sequence a lane, and takes its own from the lanes.
+// (A chunk of 1024 tokens beside 31 answer tokens, 7B heads, windows of 8192 keys: 206 us, 141
+// and 99 each alone; 220 to 228 in parts for the chunk alone; 362 in two launches and
+// two merges, row tiles of 32 for the answer tokens.)
 
 #include "attn_rows_pages.h"
 #include "attn_tile_pages.h"
@@ -22,25 +24,37 @@ namespace {
 template <int D>
 __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
   __shared__ RowsLds<D, 1, 4> lds;
-  paged_rows<D, 1, 4>(a, a.few, blockIdx.x, lds);
+  paged_rows<D, 1, 4>(a, a.few, blockIdx.x, lds, [&](int b) { return sequence(a, b); });
 }
 
 template <int D>
 __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedAttnArgs a) {
   __shared__ union { RowsLds<D, 1, 4> few; RowsLds<D, 2, 4> some; } lds;
   const int blk = blockIdx.x;
-  if (blk < a.some.groups) paged_rows<D, 2, 4>(a, a.some, blk, lds.some);
-  else paged_rows<D, 1, 4>(a, a.few, blk - a.some.groups, lds.few);
+  auto at = [&](int b) { return sequence(a, b); };
+  if (blk < a.some.groups) paged_rows<D, 2, 4>(a, a.some, blk, lds.some, at);
+  else paged_rows<D, 1, 4>(a, a.few, blk - a.some.groups, lds.few, at);
 }
 
 template <int D>
 __global__ __launch_bounds__(kThreads, 1) void paged_mixed_kernel(PagedAttnArgs a) {
   __shared__ union { TileLds<D> tile; RowsLds<D, 1, 8> rows; } lds;
-  const int blk = blockIdx.x;
-  if (blk < a.tile_grid) return paged_tile<D>(a, blk, lds.tile);
+  const LaneSequences y = lane_sequences(a);
+  int blk = blockIdx.x, parts;
+  const int items = all_row_tiles(a, y, parts);
+  // (starts that decrease may count rows twice: more partial results than there is room for)
+  const bool fits = parts == 1 || (items <= a.tile_items && items <= a.tile_slots / parts);
+  const int n_work = fits ? items * parts : 0;
+  if (blk == 0 && threadIdx.x == 0 && a.ws_items) {
+    a.ws_items->items = fits && parts > 1 ? items : 0;
+    a.ws_items->parts = parts;
+  }
+  if (blk < n_work) return paged_tile<D>(a, y, blk, n_work, parts, lds.tile);
+  blk -= n_work;
+  if (blk >= a.some.groups + a.few.groups) return;
   // 16-row tiles for both: the 256-row kernel's accumulation registers leave 128 others, and 32 rows do not fit those
-  const bool some = blk < a.tile_grid + a.some.groups;
-  paged_rows<D, 1, 8>(a, some ? a.some : a.few, blk - a.tile_grid - (some ? 0 : a.some.groups), lds.rows);
+  const bool some = blk < a.some.groups;
+  paged_rows<D, 1, 8>(a, some ? a.some : a.few, blk - (some ? 0 : a.some.groups), lds.rows, [&](int b) { return sequence(a, y, b); });
 }
 
 template <int D>

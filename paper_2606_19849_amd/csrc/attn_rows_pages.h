@@ -37,9 +37,10 @@ struct RowsLds {
   int odd;
 };
 
-// Work-group `blk` of those that take the sequences of class x: row tiles of 16 * NRB rows.
-template <int D, int NRB, int NW>
-__device__ __forceinline__ void paged_rows(const PagedAttnArgs& a, const RowsClass& x, int blk, RowsLds<D, NRB, NW>& lds) {
+// Work-group `blk` of those that take the sequences of class x: row tiles of 16 * NRB rows.  sequence_at(b): sequence b.
+template <int D, int NRB, int NW, class F>
+__device__ __forceinline__ void paged_rows(const PagedAttnArgs& a, const RowsClass& x, int blk, RowsLds<D, NRB, NW>& lds,
+                                           F&& sequence_at) {
   constexpr int NKS = D / 32;              // k-steps of Q K^T
   constexpr int VE = D / 16;               // dims per lane of a V row
   constexpr int RT = 16 * NRB;             // rows of the work-group
@@ -68,7 +69,7 @@ __device__ __forceinline__ void paged_rows(const PagedAttnArgs& a, const RowsCla
   if (next >= a.B * x.parts) return;
   const int b = x.by_parts(next), turned = next - b * x.parts + b, part = turned - x.by_parts(turned) * x.parts;
 
-  const Sequence s = sequence(a, b);
+  const Sequence s = sequence_at(b);
   const int NR = g * s.n;
   if (NR > x.most || NR < x.least || rt * RT >= NR) return;
   const KeyBlocks<BK> blocks(s);

@@ -46,47 +46,94 @@ __device__ __forceinline__ late_args late() {
   return p;
 }
 
-// Row tiles of sequence b on this kernel.
-__device__ __forceinline__ int row_tiles(const PagedAttnArgs& a, int b) {
-  int q0;
-  const int rows = a.Hq / a.Hkv * min(rows_of(a, b, q0), a.max_q);
+// Row tiles on this kernel of a sequence with so many rows.
+__device__ __forceinline__ int row_tiles(const PagedAttnArgs& a, int tokens) {
+  const int rows = a.Hq / a.Hkv * min(tokens, a.max_q);
   return rows >= a.tile_least ? (rows + kBlockM - 1) / kBlockM : 0;
 }
-// Row tiles of all sequences and heads, and the parts that their key ranges are split into.
-__device__ __forceinline__ int all_row_tiles(const PagedAttnArgs& a, int& parts) {
+// The first 64 sequences, one a lane: first row, rows, length.
+struct LaneSequences {
+  int q0, rows, len;
+};
+__device__ __forceinline__ LaneSequences lane_sequences(const PagedAttnArgs& a) {
+  const int lane = threadIdx.x & 63, b = min(lane, a.B - 1);
+  LaneSequences x;
+  x.rows = rows_of(a, b, x.q0);
+  x.rows = lane < a.B ? x.rows : 0;
+  x.len = a.seq_len[b];
+  return x;
+}
+// Sequence b, the same one for all lanes; in scalar registers, whatever the compiler makes of loads whose address it cannot
+// prove to be the same in all lanes.
+__device__ __forceinline__ Sequence sequence(const PagedAttnArgs& a, const LaneSequences& x, int b) {
+  int q0, rows, len;
+  if (a.B <= 64) {
+    q0 = __builtin_amdgcn_readlane(x.q0, b);
+    rows = __builtin_amdgcn_readlane(x.rows, b);
+    len = __builtin_amdgcn_readlane(x.len, b);
+  } else {
+    rows = __builtin_amdgcn_readfirstlane(rows_of(a, b, q0));
+    q0 = __builtin_amdgcn_readfirstlane(q0);
+    len = __builtin_amdgcn_readfirstlane(a.seq_len[b]);
+  }
+  return sequence(a, q0, rows, len);
+}
+// Row tiles of all sequences and heads, and the parts that their key ranges are split into.  Sequences of fewer rows count
+// for their keys, once for the first row tile of 16 and half for each more (they meet in L2).
+__device__ __forceinline__ int all_row_tiles(const PagedAttnArgs& a, const LaneSequences& x, int& parts) {
   const int lane = threadIdx.x & 63;
-  int n = 0, keys = 0;
-  for (int b = lane; b < a.B; b += 64) {
-    const int m = row_tiles(a, b);
+  int n = 0, keys = 0, beside = 0;           // (beside: half blocks)
+  auto add = [&](int q0, int rows, int len) __attribute__((always_inline)) {
+    const int m = row_tiles(a, rows);
+    const Sequence s = sequence(a, q0, rows, len);
     n += m;
-    if (m > 0 && a.tile_parts > 1) {
-      const Sequence s = sequence(a, b);
-      keys = max(keys, KeyBlocks<kKeyTile>(s).upto(last_position(a, s, s.n - 1)));
-    }
+    if (a.tile_parts <= 1 || s.n <= 0) return;
+    const int last = last_position(a, s, s.n - 1);
+    keys = max(keys, m > 0 ? KeyBlocks<kKeyTile>(s).upto(last) : 0);
+    const int tiles16 = (a.Hq / a.Hkv * s.n + 15) / 16;
+    beside += m > 0 ? 0 : min(KeyBlocks<kRowsBlock>(s).upto(last), 1 << 16) * (1 + tiles16);
+  };
+  add(x.q0, x.rows, x.len);
+  for (int b = lane + 64; b < a.B; b += 64) {
+    int q0;
+    const int rows = rows_of(a, b, q0);
+    add(q0, rows, a.seq_len[b]);
   }
   n = __builtin_amdgcn_readlane(wave_scan(n), 63);
   const int items = n * a.Hkv;
   parts = max(a.tile_splits, 1);
   if (a.tile_parts <= 1 || items == 0) return items;
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) keys = max(keys, __shfl_xor(keys, o, 64));
+  // the most keys: lane 63's after the steps of wave_scan
+  keys = max(keys, __builtin_amdgcn_update_dpp(0, keys, 0x111, 0xF, 0xF, true));
+  keys = max(keys, __builtin_amdgcn_update_dpp(0, keys, 0x112, 0xF, 0xF, true));
+  keys = max(keys, __builtin_amdgcn_update_dpp(0, keys, 0x114, 0xF, 0xF, true));
+  keys = max(keys, __builtin_amdgcn_update_dpp(0, keys, 0x118, 0xF, 0xF, true));
+  keys = max(keys, __builtin_amdgcn_update_dpp(0, keys, 0x142, 0xA, 0xF, false));
+  keys = max(keys, __builtin_amdgcn_update_dpp(0, keys, 0x143, 0xC, 0xF, false));
+  keys = __builtin_amdgcn_readlane(keys, 63);
+  const float others = (float)__builtin_amdgcn_readlane(wave_scan(beside), 63) * (float)a.Hkv * (0.5f * paged_block_cost(a.D));
   // lane p - 1 takes p parts; of equal times the fewest
-  static_assert(kPagedTileParts <= 64, "one lane for each number of parts");
-  const int p = lane + 1;
+  static_assert(kPagedTileParts == 16, "one lane of a row for each number of parts");
+  const int p = (lane & 15) + 1;
   const bool fits = p <= a.tile_parts && (p == 1 || items <= a.tile_slots / p);
-  int best = fits ? (int)min(paged_tile_cost(items, keys, p), (int64_t)(1 << 24) - 1) : 1 << 24;
-  best = best * 64 + lane;
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) best = min(best, __shfl_xor(best, o, 64));
-  parts = (__builtin_amdgcn_readfirstlane(best) & 63) + 1;
+  int best = fits ? (int)fminf(32.f * paged_tile_cost(items, keys, p, others), 16777215.f) : 1 << 24;
+  best = best * 64 + p;
+  constexpr int kNone = 0x7FFFFFFF;
+  best = min(best, __builtin_amdgcn_update_dpp(kNone, best, 0x111, 0xF, 0xF, false));
+  best = min(best, __builtin_amdgcn_update_dpp(kNone, best, 0x112, 0xF, 0xF, false));
+  best = min(best, __builtin_amdgcn_update_dpp(kNone, best, 0x114, 0xF, 0xF, false));
+  best = min(best, __builtin_amdgcn_update_dpp(kNone, best, 0x118, 0xF, 0xF, false));
+  parts = __builtin_amdgcn_readlane(best, 15) & 63;
   return items;
 }
 // The sequence whose row tiles, each `times` times, hold item x; its first item and its row tiles.
-__device__ __forceinline__ int sequence_of_item(const PagedAttnArgs& a, int x, int times, int& first, int& tiles) {
+__device__ __forceinline__ int sequence_of_item(const PagedAttnArgs& a, const LaneSequences& y, int x, int times, int& first,
+                                                int& tiles) {
   const int lane = threadIdx.x & 63;
   int before = 0;
   for (int b0 = 0;; b0 += 64) {
-    const int n = b0 + lane < a.B ? row_tiles(a, b0 + lane) : 0;
+    int q0;
+    const int n = b0 == 0 ? row_tiles(a, y.rows) : b0 + lane < a.B ? row_tiles(a, rows_of(a, b0 + lane, q0)) : 0;
     const int upto = before + wave_scan(n) * times;
     const int all = __builtin_amdgcn_readlane(upto, 63);
     if (x < all || b0 + 64 >= a.B) {
@@ -108,8 +155,10 @@ struct TileLds {
   int odd;
 };
 
+// Work-group `blk` of n_work: the row tiles times `parts`.
 template <int D>
-__device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, TileLds<D>& sh) {
+__device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, const LaneSequences& y, int blk, int n_work, int parts,
+                                           TileLds<D>& sh) {
   constexpr int RB = 1;
   typedef PipeTile<D, RB> Tile;
   constexpr int BN = kKeyTile, BM = kBlockM, NW = kThreads / 64;
@@ -134,30 +183,14 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, int blk, Tile
   const int g = a.Hq / a.Hkv;
 
   // ---- work item: the row tiles of one key range side by side (they share its K/V in an XCD's L2), longest first
-  int parts;
-  const int items = all_row_tiles(a, parts), n_work = items * parts;
-  // (starts that decrease may count rows twice: more partial results than there is room for)
-  const bool fits = parts == 1 || (n_work <= a.tile_slots && items <= a.tile_items);
-  if (blk == 0 && tid == 0 && a.ws_items) {
-    a.ws_items->items = fits && parts > 1 ? items : 0;
-    a.ws_items->parts = parts;
-  }
-  if (blk >= n_work || !fits) return;
   const int L = xcd_remap(blk, n_work);
   int first_item, cnt;
-  const int b = __builtin_amdgcn_readfirstlane(sequence_of_item(a, L, a.Hkv * parts, first_item, cnt));
-  // (in scalar registers, whatever the compiler makes of divisions and of loads whose address it cannot prove to be the
-  // same in all lanes: no branch of the key loop may be on lanes)
+  const int b = __builtin_amdgcn_readfirstlane(sequence_of_item(a, y, L, a.Hkv * parts, first_item, cnt));
+  // (in scalar registers, whatever the compiler makes of divisions: no branch of the key loop may be on lanes)
   const int kp = __builtin_amdgcn_readfirstlane((L - first_item) / cnt), rt = cnt - 1 - (L - first_item - kp * cnt);
   const int kv = __builtin_amdgcn_readfirstlane(kp / parts), part = kp - kv * parts;
   if (tid == 0) sh.odd = 0;
-  Sequence s = sequence(a, b);
-  s.q0 = __builtin_amdgcn_readfirstlane(s.q0);
-  s.n = __builtin_amdgcn_readfirstlane(s.n);
-  s.all = __builtin_amdgcn_readfirstlane(s.all);
-  s.H = __builtin_amdgcn_readfirstlane(s.H);
-  s.sink = __builtin_amdgcn_readfirstlane(s.sink);
-  s.first = __builtin_amdgcn_readfirstlane(s.first);
+  const Sequence s = sequence(a, y, b);
   const int NR = g * s.n;
   if (parts > 1 && part == 0 && tid == 0)
     a.ws_items->item[(unsigned)first_item / (unsigned)parts + kv * cnt + cnt - 1 - rt] = TileItem{s.q0, NR, kv, rt, L, cnt};

@@ -111,18 +111,28 @@ struct TileItems {
   int items, parts;         // (items: 0 where nothing is split)
   TileItem item[1];         // tile_items of them
 };
-// Parts of the key ranges of `items` row tiles over `tiles` 64-key tiles: the number with the least time, counted in such
-// tiles (1.35 us with heads of size 128): rounds of work-groups over the CUs, each a start, an end and its keys, then
-// the merge and the partial results' way to memory and back.  (3B heads, 64 row tiles of 139 tiles, us measured with
-// the chunk kernel: 2 parts 126, 3 91.7, 4 84.7, 6 105, 8 96.7.)
-__host__ __device__ inline int64_t paged_tile_cost(int items, int tiles, int p) {
-  const int64_t rounds = ((int64_t)items * p + kNumCUs - 1) / kNumCUs;
-  return 32 * rounds * (6 + (tiles + p - 1) / p) + (p > 1 ? 64 + (int64_t)items * p * 5 / 4 : 0);
+// The time of `items` row tiles over `tiles` 64-key tiles in p parts, beside sequences of few rows whose keys alone
+// take `beside`, counted in such tiles (1.35 us with heads of size 128, 0.9 of size 64).  Rounds of work-groups over
+// the CUs, each a start, an end and its keys, which take longer where more than half of the CUs are at it (the power
+// limit); the CUs that the last round leaves stream the others' keys, 1.3 times their share; what is left of those comes
+// after; then the merge and the partial results' way to memory and back.
+// (Us measured / this, in 1, 2, 3, 4, 6, 8 parts.  7B heads, 1024 tokens over 8192 keys 196, 139, 166, 146, 160, 175 / 196,
+// 134, 179, 157, 179, 202; beside 31 answer tokens 203, 218, 217, 233, 249, 267 / 196, 205, 206, 227, 249, 271; beside 100
+// of them 337, 420, 430, 445, 474, 490 / 343, 405, 406, 427, 449, 471; 256 tokens beside 31 185, 117, 119, 118, 130, 146 /
+// 180, 100, 105, 113, 124, 134; 3B heads, 1024 beside 31 197, 116, 108, 123, 126, 143 / 196, 112, 111, 130, 131, 154.)
+__host__ __device__ inline float paged_tile_cost(int items, int tiles, int p, float beside) {
+  const int64_t n = (int64_t)items * p, full = n > 0 ? (n - 1) / kNumCUs : 0;                // rounds before the last one
+  const float busy = (float)(n - full * kNumCUs) / kNumCUs, each = (float)(6 + (tiles + p - 1) / p);
+  const float last = each * (0.96f + 0.22f * fmaxf(2 * busy - 1, 0.f));
+  return each * 1.18f * (float)full + last + fmaxf(beside - fminf(1.3f * (1 - busy), 1.f) * last, 0.f) +
+         (p > 1 ? 2.f + 0.039f * (float)n : 0.f);
 }
+// 32-key blocks of one KV head at the memory's rate, in the same unit.
+__host__ __device__ constexpr float paged_block_cost(int D) { return D == 128 ? 2.4e-3f : 1.8e-3f; }
 inline int paged_tile_parts(int items, int tiles, int most, int slots) {
   int parts = 1;
   for (int p = 2; p <= most && items * p <= slots; ++p)
-    if (paged_tile_cost(items, tiles, p) < paged_tile_cost(items, tiles, parts)) parts = p;
+    if (paged_tile_cost(items, tiles, p, 0.f) < paged_tile_cost(items, tiles, parts, 0.f)) parts = p;
   return parts;
 }
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream);
@@ -140,14 +150,20 @@ __device__ __forceinline__ int rows_of(const A& a, int b, int& q0) {
   q0 = min(max(a.q_start[b], 0), a.total);
   return min(max(a.q_start[b + 1], q0), a.total) - q0;
 }
-__device__ __forceinline__ Sequence sequence(const PagedAttnArgs& a, int b) {
+__device__ __forceinline__ Sequence sequence(const PagedAttnArgs& a, int q0, int rows, int len) {
   Sequence s;
-  s.all = rows_of(a, b, s.q0);
+  s.q0 = q0;
+  s.all = rows;
   s.n = min(s.all, a.max_q);
-  s.H = min(max(a.seq_len[b], 0), a.width << a.page_shift);
+  s.H = min(max(len, 0), a.width << a.page_shift);
   s.first = a.W < 0 || a.W >= s.H ? 0 : s.H - (int)a.W;
   s.sink = min(a.S, s.first);
   return s;
+}
+__device__ __forceinline__ Sequence sequence(const PagedAttnArgs& a, int b) {
+  int q0;
+  const int rows = rows_of(a, b, q0);
+  return sequence(a, q0, rows, a.seq_len[b]);
 }
 // A row's last position: token t of the sequence's chunk.
 __device__ __forceinline__ int last_position(const PagedAttnArgs& a, const Sequence& s, int t) {

@@ -116,7 +116,7 @@ bool rows_alone(int64_t B, int64_t rows, int64_t all, int64_t Hkv, int64_t keys,
   if (items > (1 << 20)) return false;
   const int tiles = (int)(keys / kKeyTile) + 1;
   const int p = paged_tile_parts((int)items, tiles, std::max(std::min(tiles / kMinSplitTiles, kPagedTileParts), 1), 450);
-  const double t_tile = 4.0 + (D == 128 ? 1.35 : 0.9) / 32 * double(paged_tile_cost((int)items, tiles, p));
+  const double t_tile = 6.5 + (D == 128 ? 1.2 : 0.8) * double(paged_tile_cost((int)items, tiles, p, 0.f));     // (short: no power limit)
   return t_rows <= t_tile;
 }
 

@@ -21,7 +21,7 @@
 // Which sequences these are stands in device memory, so every work-group counts the
 // row tiles of all sequences and finds its own; where they leave CUs idle, key ranges
 // are split and joined by the merge kernel.
-// It is bound by the matrix cores, 69 % busy in a chunk of 2048 tokens over 16384 keys (7B
+// It is bound by the matrix cores, 68 % busy in a chunk of 2048 tokens over 16384 keys (7B
 // heads, 513 GFLOP): 445 to 480 us a call by the box, 1070 to 1150 TFLOP/s; the chunk prefill
 // over a dense ring takes 448 to 469 on the same boxes.  What stands between its matrix
 // instructions counts: with half of the CUs at work a tile takes 1.18 us (the chunk

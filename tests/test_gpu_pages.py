@@ -201,6 +201,22 @@ def test_append(heads, seqs, page):
     assert torch.equal(bits(c.dk), bits(wk)) and torch.equal(bits(c.dv), bits(wv))
 
 
+def test_append_to_the_most_sequences():
+    g = torch.Generator()
+    g.manual_seed(4)
+    seqs = [(int(n), 13) for n in torch.randint(0, 4, (4096,), generator=g)]
+    c = Cache(4, seqs, heads=(1, 1, 64), page=16).device()
+    total = c.q_start[-1]
+    k, v = (torch.randn(total + 2, 1, 64, generator=g).to(torch.bfloat16) for _ in "kv")
+    wk, wv = c.k.clone(), c.v.clone()
+    for b, n in enumerate(c.n):
+        for j in range(n):
+            page, at = c.place(b, c.H[b] + j)
+            wk[page, at], wv[page, at] = k[c.q_start[b] + j], v[c.q_start[b] + j]
+    vico.vico_paged_append(k.to(DEV), v.to(DEV), c.ds, c.dl, c.dk, c.dv, c.dt)
+    assert torch.equal(bits(c.dk.cpu()), bits(wk)) and torch.equal(bits(c.dv.cpu()), bits(wv))
+
+
 def test_append_past_the_table_goes_nowhere():
     c = Cache(3, [(5, 14), (40, 0)], heads=(2, 2, 64), width=1).device()
     wk = c.dk.clone()
@@ -265,6 +281,18 @@ def test_attention_bidirectional(mask):
         check(c, c.attention(flags=vico.VICO_ATTN_BIDIRECTIONAL), c.oracle(bidirectional=True))
         # fewer rows than a sequence has still see all of its chunk
         check(c, c.attention(flags=vico.VICO_ATTN_BIDIRECTIONAL, max_q=70), c.oracle(bidirectional=True, max_q=70))
+
+
+@pytest.mark.parametrize("heads", [SMALL, WIDE, H128], ids=str)
+@pytest.mark.parametrize("many", [64, 65, 150, 300])
+def test_attention_of_many_sequences(many, heads):
+    """More sequences than a wave has lanes, chunks among the first, the last and those between."""
+    chunks = {0: (70, 100), 63: (90, 0), 64: (130, 40), many // 2: (80, 300), many - 1: (66, 17)}
+    for picked in ({}, chunks, {many - 1: (66, 500)}):
+        seqs = [picked.get(b, (b % 3, 11 * b % 97)) for b in range(many)]
+        c = Cache(many, seqs, heads=heads, page=16, sink=3, window=60).device()
+        for splits in (0, 2):
+            check(c, c.attention(splits=splits), c.oracle())
 
 
 def test_attention_scale_and_fewer_rows():

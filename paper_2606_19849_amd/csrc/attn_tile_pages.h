@@ -22,10 +22,10 @@
 // row tiles of all sequences and finds its own; where they leave CUs idle, key ranges
 // are split and joined by the merge kernel.
 // It is bound by the matrix cores, 68 % busy in a chunk of 2048 tokens over 16384 keys (7B
-// heads, 513 GFLOP): 445 to 480 us a call by the box, 1070 to 1150 TFLOP/s; the chunk prefill
-// over a dense ring takes 448 to 469 on the same boxes.  What stands between its matrix
-// instructions counts: with half of the CUs at work a tile takes 1.18 us (the chunk
-// prefill's 1.14), 1.24 with a resource for each tile and its questions asked anew at each.
+// heads, 513 GFLOP): 445 to 500 us a call by the box, 1030 to 1150 TFLOP/s; the chunk prefill
+// over a dense ring took 447 to 473 on two boxes where this took 445 to 468.  What stands
+// between its matrix instructions counts: with half of the CUs at work a tile takes 1.18 us (the
+// chunk prefill's 1.14), 1.24 with a resource for each tile and its questions asked anew at each.
 // A work-group's start takes 6 us: 1.6 for the lengths, 2.2 for page numbers and Q, 1.9
 // for the first tile.
 
@@ -293,7 +293,7 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, const LaneSeq
     n_plain = __builtin_amdgcn_ballot_w64(some & bad) != 0 ? 0 : n_plain;
     const int page = tab[(e0 + my_page) & (2 * kTabHalf - 1)], p0 = pos + 8 * wave;
     const int there = (some & (page >= 0)) ? page : 0;
-    const uint64_t at = (uint64_t)(uint32_t)((there << shift) + (p0 & in_page)) * (uint32_t)rbytes;
+    const uint64_t at = (uint64_t)(((uint32_t)there << shift) + (uint32_t)(p0 & in_page)) * (uint32_t)rbytes;
     run_lo = (uint32_t)at & 0x7FFFFFFFu;
     run_hi = (uint32_t)(at >> 31);
     const uint32_t window = __builtin_amdgcn_readlane(run_hi, 0);

@@ -135,13 +135,16 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
   if (W != VICO_FULL_HISTORY && W < keys) keys = std::min(keys, S + W + n);
   // work-groups: some rounds of them where sequences differ (answer tokens of 32 sequences of 1000 to 16000 keys, us
   // with 4, 8, 12, 16 a CU: 123.0, 124.1, 120.7, 120.2); in a launch with 256-row tiles as many as leave those
-  // room for their partial results, and no more than needed where one long sequence is all that is expected
+  // room for their partial results.  One sequence is no exception: how many of the call's rows are its own stands in
+  // device memory.  (7B heads, room for 2048 rows, us with all of them taken for the sequence's / as here: one token over
+  // 8000 keys 77 / 13, over 262144 keys 3195 / 106, 300 tokens over 8000 keys 169 / 58; all 2048 over 16384 keys
+  // 449 to 453 / 450; where no key range is split, the merge's launch: 300 of 300 over 300 keys 26.7 / 28.5.)
   const int64_t all = int64_t(total) * g;
   const bool tile = rows > kSomeRows && !rows_alone(B, rows, all, Hkv, keys, D);
   const int64_t some_most = tile ? kSomeRows : rows;
   const int64_t groups = int64_t(B) * Hkv;
-  const int64_t target = tile && B == 1 ? 1 : tile ? std::min<int64_t>(std::max<int64_t>(8 * groups, kNumCUs), 4 * kNumCUs)
-                                                 : (B == 1 ? 2 : rows > kFewRows ? 4 : 12) * kNumCUs;
+  const int64_t target = tile ? std::min<int64_t>(std::max<int64_t>(8 * groups, kNumCUs), 4 * kNumCUs)
+                              : (B == 1 ? 2 : rows > kFewRows ? 4 : 12) * kNumCUs;
   if (!plan_rows(&pl->few, 1, std::min<int64_t>(rows, kFewRows), 16, B, Hkv, keys, target, splits)) return VICO_ERR_INVALID_ARG;
   if (pl->few.parts > 1) pl->few_ws = partial_bytes(pl->few.slots, 16, D);
   if (rows > kFewRows) {
@@ -165,12 +168,6 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
     pl->tile_grid = (int)std::max<int64_t>(items, pl->tile_slots);
     pl->tile_items = (int)std::min<int64_t>(items, pl->tile_slots / 2);
     if (pl->tile_items == 0) pl->tile_parts = 1;
-    if (B == 1) {                            // known here: the call's rows are the one sequence's
-      pl->tile_splits = paged_tile_parts((int)items, (int)(keys / kKeyTile), pl->tile_parts, pl->tile_slots);
-      pl->tile_parts = 0;
-      pl->tile_slots = pl->tile_grid = (int)items * pl->tile_splits;
-      pl->tile_items = (int)items;
-    }
   }
   if (std::max(pl->tile_splits, pl->tile_parts) > 1)
     pl->ws_bytes += items_bytes(pl->tile_items) + partial_bytes(pl->tile_slots, kBlockM, D);

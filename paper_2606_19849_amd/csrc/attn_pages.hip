@@ -4,11 +4,11 @@
 // launch has no 256-row tiles); more.  Which sequence is of which class stands in device memory: a launch
 // has work-groups for every sequence in every class that max_q_len allows, and those
 // that find another class end.  What is left of a call in which a class has no
-// sequence is the time of that, about 1 us a 256 work-groups.
+// sequence is the time of that, about 1 us a 256 work-groups (up to 64 sequences).
 //
 // Calls of one class, or of the first two, have kernels of four waves of which a CU
 // holds several, so that one's start is hidden behind another's keys.  With
-// the third, one launch does all: work-groups of the matrix cores first, which are
+// the third, one launch does all (of hundreds of sequences two do, rows_apart): work-groups of the matrix cores first, which are
 // long, then those that stream keys, in parts that count both (paged_tile_cost).  Every
 // work-group reads all lengths, a sequence a lane, and takes its own from the lanes.
 // (A chunk of 1024 tokens beside 31 answer tokens, 7B heads, windows of 8192 keys: 206 us, 141
@@ -83,11 +83,13 @@ template <int D>
 hipError_t launch(const PagedAttnArgs& args, hipStream_t stream) {
   PagedAttnArgs a = args;
   if (a.tile_grid > 0) {
-    hipLaunchKernelGGL(paged_mixed_kernel<D>, dim3((unsigned)(a.tile_grid + a.some.groups + a.few.groups)), dim3(kThreads), 0, stream, a);
-  } else if (a.some.groups > 0) {
-    hipLaunchKernelGGL(paged_rows_kernel<D>, dim3((unsigned)(a.some.groups + a.few.groups)), dim3(256), 0, stream, a);
-  } else {
-    hipLaunchKernelGGL(paged_decode_kernel<D>, dim3((unsigned)a.few.groups), dim3(256), 0, stream, a);
+    PagedAttnArgs t = a;
+    if (a.rows_apart) t.some.groups = t.few.groups = 0;
+    hipLaunchKernelGGL(paged_mixed_kernel<D>, dim3((unsigned)(t.tile_grid + t.some.groups + t.few.groups)), dim3(kThreads), 0, stream, t);
+  }
+  if (a.tile_grid == 0 || a.rows_apart) {
+    if (a.some.groups > 0) hipLaunchKernelGGL(paged_rows_kernel<D>, dim3((unsigned)(a.some.groups + a.few.groups)), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(paged_decode_kernel<D>, dim3((unsigned)a.few.groups), dim3(256), 0, stream, a);
   }
   const hipError_t e = hipGetLastError();
   a.few.merge = merge_groups<D>(a.few, a.B, a.Hkv);

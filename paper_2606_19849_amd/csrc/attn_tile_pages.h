@@ -79,7 +79,7 @@ __device__ __forceinline__ Sequence sequence(const PagedAttnArgs& a, const LaneS
   return sequence(a, q0, rows, len);
 }
 // Row tiles of all sequences and heads, and the parts that their key ranges are split into.  Sequences of fewer rows count
-// for their keys, once for the first row tile of 16 and half for each more (they meet in L2).
+// for their keys, once for the first row tile of 16 and half for each more (they meet in L2), if they are in this launch.
 __device__ __forceinline__ int all_row_tiles(const PagedAttnArgs& a, const LaneSequences& x, int& parts) {
   const int lane = threadIdx.x & 63;
   int n = 0, keys = 0, beside = 0;           // (beside: half blocks)
@@ -91,7 +91,7 @@ __device__ __forceinline__ int all_row_tiles(const PagedAttnArgs& a, const LaneS
     const int last = last_position(a, s, s.n - 1);
     keys = max(keys, m > 0 ? KeyBlocks<kKeyTile>(s).upto(last) : 0);
     const int tiles16 = (a.Hq / a.Hkv * s.n + 15) / 16;
-    beside += m > 0 ? 0 : min(KeyBlocks<kRowsBlock>(s).upto(last), 1 << 16) * (1 + tiles16);
+    beside += m > 0 || a.rows_apart ? 0 : min(KeyBlocks<kRowsBlock>(s).upto(last), 1 << 16) * (1 + tiles16);
   };
   add(x.q0, x.rows, x.len);
   for (int b = lane + 64; b < a.B; b += 64) {

@@ -94,6 +94,7 @@ struct PagedAttnArgs {
   float scale_log2;
   FastDiv by_g, by_kv;
   RowsClass few, some;      // up to 16 rows, up to tile_least - 1 (groups 0: none)
+  int rows_apart;           // these are not in the launch of the 256-row tiles
   // sequences of tile_least rows and more, on 256-row tiles: work-groups (0: none) and those of the merge, the row
   // tiles of all heads that may be split, room for partial results, the parts that the caller asked for (0: the
   // kernel's choice, of tile_parts at most)

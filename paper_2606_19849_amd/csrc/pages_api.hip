@@ -74,6 +74,7 @@ int64_t items_bytes(int64_t items) { return align256(sizeof(TileItems) + items *
 
 struct PagedPlan {
   RowsClass few, some;
+  bool apart;                // 256-row tiles and the others in a launch each
   int some_most, tile_grid, tile_items, tile_slots, tile_parts, tile_splits;
   int64_t few_ws, some_ws, ws_bytes;
 };
@@ -120,6 +121,19 @@ bool rows_alone(int64_t B, int64_t rows, int64_t all, int64_t Hkv, int64_t keys,
   return t_rows <= t_tile;
 }
 
+// Whether sequences of few rows get a launch of their own where the call has 256-row tiles.  Beside those, each of their
+// work-groups (five for a sequence and KV head, most of them of another class) starts with all lengths, about B / 160 us,
+// one work-group a CU; apart, the two kinds wait for each other.
+// Measured, us, one launch / two, 7B heads, a chunk of 1024 tokens over 4000 keys beside decode steps over 200 each: 255
+// of them 165 / 118, 330 204 / 124, 511 288 / 141, 1023 756 / 222, 4095 8578 / 769; over 8000 beside 2000: 255 341 / 395,
+// 330 436 / 427, 511 658 / 546; over 8192 beside 8192: 200 750 / 876; 3B heads, 512 over 4000 beside 1000: 255 136 / 130,
+// 463 179 / 153, 1023 490 / 267, 4095 5093 / 986; small heads, 512 over 2000 beside 1000: 255 81 / 71, 463 118 / 71, 1023
+// 377 / 145, 4095 4603 / 522.
+bool rows_apart(int64_t B, int64_t Hkv, int splits) {
+  const int64_t groups = 5 * B * Hkv * std::max(std::min(splits, kPagedParts), 1);
+  return groups * B > (1 << 21);             // 50 us of all CUs
+}
+
 int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size, int32_t width, int32_t S, int64_t W,
                       int64_t hint, int32_t Hq, int32_t Hkv, int32_t D, int32_t splits, PagedPlan* pl) {
   if (total < 0 || max_q < 0 || S < 0 || W < VICO_FULL_HISTORY || hint < 0 || splits < 0) return VICO_ERR_INVALID_ARG;
@@ -143,12 +157,14 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
   const bool tile = rows > kSomeRows && !rows_alone(B, rows, all, Hkv, keys, D);
   const int64_t some_most = tile ? kSomeRows : rows;
   const int64_t groups = int64_t(B) * Hkv;
-  const int64_t target = tile ? std::min<int64_t>(std::max<int64_t>(8 * groups, kNumCUs), 4 * kNumCUs)
-                              : (B == 1 ? 2 : rows > kFewRows ? 4 : 12) * kNumCUs;
+  pl->apart = tile && rows_apart(B, Hkv, splits);
+  const bool beside = tile && !pl->apart;
+  const int64_t target = beside ? std::min<int64_t>(std::max<int64_t>(8 * groups, kNumCUs), 4 * kNumCUs)
+                                : (B == 1 ? 2 : rows > kFewRows ? 4 : 12) * kNumCUs;
   if (!plan_rows(&pl->few, 1, std::min<int64_t>(rows, kFewRows), 16, B, Hkv, keys, target, splits)) return VICO_ERR_INVALID_ARG;
   if (pl->few.parts > 1) pl->few_ws = partial_bytes(pl->few.slots, 16, D);
   if (rows > kFewRows) {
-    if (!plan_rows(&pl->some, kFewRows + 1, some_most, tile ? 16 : 32, B, Hkv, keys, tile ? std::min<int64_t>(target, kNumCUs / 4) : target, splits))
+    if (!plan_rows(&pl->some, kFewRows + 1, some_most, beside ? 16 : 32, B, Hkv, keys, beside ? std::min<int64_t>(target, kNumCUs / 4) : target, splits))
       return VICO_ERR_INVALID_ARG;
     if (pl->some.parts > 1) pl->some_ws = partial_bytes(pl->some.slots, pl->some.tile_rows, D);
   }
@@ -220,6 +236,23 @@ int vico_paged_attn_plan(int32_t num_seqs, int32_t total_q, int32_t max_q_len, i
   return VICO_OK;
 }
 
+int vico_paged_route(int32_t num_seqs, int32_t total_q, int32_t max_q_len, int32_t page_size, int32_t max_pages,
+                     int32_t sink_len, int64_t window, int64_t keys_hint, int32_t num_q_heads, int32_t num_kv_heads,
+                     int32_t head_dim, int32_t num_splits, int32_t* route_out) {
+  PagedPlan pl;
+  const int st = check_paged_shape(num_seqs, total_q, max_q_len, page_size, max_pages, sink_len, window, keys_hint,
+                                   num_q_heads, num_kv_heads, head_dim, num_splits, &pl);
+  if (st != VICO_OK) return st;
+  const int rows = pl.few.groups + pl.some.groups;
+  const bool beside = pl.tile_grid > 0 && !pl.apart;
+  route_out[0] = pl.tile_grid;
+  route_out[1] = beside ? rows : 0;
+  route_out[2] = beside ? 0 : rows;
+  route_out[3] = pl.few.parts;
+  route_out[4] = pl.some.parts;
+  return VICO_OK;
+}
+
 int vico_paged_attn(const void* q, const int32_t* q_start, const int32_t* seq_len, int32_t num_seqs, int32_t total_q,
                     int32_t max_q_len, const void* k_pages, const void* v_pages, int32_t num_pages, int32_t page_size,
                     const int32_t* page_table, int32_t max_pages, int32_t sink_len, int64_t window, int64_t keys_hint,
@@ -265,6 +298,7 @@ int vico_paged_attn(const void* q, const int32_t* q_start, const int32_t* seq_le
   a.by_kv = FastDiv::by(a.Hkv);
   a.few = pl.few;
   a.some = pl.some;
+  a.rows_apart = pl.apart;
   a.tile_least = pl.some_most + 1;
   a.tile_grid = pl.tile_grid; a.tile_items = pl.tile_items; a.tile_slots = pl.tile_slots;
   a.tile_parts = pl.tile_parts; a.tile_splits = pl.tile_splits;

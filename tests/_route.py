@@ -10,6 +10,7 @@ _NAMES = (TILE, BALANCED, ROWS, GATHER)
 _lib = vico.load_library()
 _lib.vico_attn_route.argtypes = [ctypes.c_int32] * 3 + [ctypes.c_int64] * 2 + [ctypes.c_int32] * 5 + [ctypes.c_void_p]
 _lib.vico_gather_route.argtypes = [ctypes.c_int32] * 5 + [ctypes.c_int64] + [ctypes.c_int32] * 4 + [ctypes.c_void_p]
+_lib.vico_paged_route.argtypes = [ctypes.c_int32] * 6 + [ctypes.c_int64] * 2 + [ctypes.c_int32] * 4 + [ctypes.c_void_p]
 
 
 def _route(call, *args):
@@ -27,3 +28,11 @@ def chunk_route(sh, splits=0, flags=0):
 def gather_route(q_len, tail, sink, slots, segments, hint, heads, splits=0):
     """(kernel, key-range parts, work-groups, 0, K through LDS) of vico_gather_attn; heads: (query, key/value, size)."""
     return _route(_lib.vico_gather_route, q_len, tail, sink, slots, segments, hint, *heads, splits)
+
+
+def paged_route(seqs, total, most, page, width, sink, window, hint, heads, splits=0):
+    """(work-groups of 256-row tiles, of row tiles beside them, of row tiles in a launch of their own, parts of up to 16
+    rows, of more) of vico_paged_attn."""
+    out = (ctypes.c_int32 * 5)()
+    assert _lib.vico_paged_route(seqs, total, most, page, width, sink, window, hint, *heads, splits, out) == 0
+    return tuple(out)

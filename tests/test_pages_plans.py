@@ -3,6 +3,7 @@ the most that its sequences can have."""
 import pytest
 
 import paper_2606_19849_amd as vico
+from tests._route import paged_route
 
 HEADS = {"7b": (28, 4, 128), "3b": (16, 2, 128), "small": (8, 2, 64)}
 
@@ -16,3 +17,18 @@ def test_one_sequence_may_have_fewer_rows_than_the_call(heads, total):
         return vico.vico_paged_attn_plan(1, rows, rows, 256, 1100, 64, vico.VICO_FULL_HISTORY, 262144, *HEADS[heads])
     parts, workspace = plan(total)
     assert parts == plan(1)[0] == 64 and 0 < workspace <= 64 << 20
+
+
+# (a chunk's tokens, keys that every sequence has at most; decode steps beside it): the steps' row tiles measured faster in
+# the launch of the chunk's, and in one of their own
+BESIDE = [("7b", 1024, 9216, [31, 63, 100, 127, 200], []), ("7b", 1024, 9024, [31, 63, 127, 255], [511]),
+          ("7b", 1024, 5024, [31, 63], [511, 1023, 4095]), ("7b", 300, 1300, [31, 63, 127], [1023]),
+          ("3b", 512, 4512, [31, 63], [1023, 4095]), ("small", 512, 2512, [31, 63], [1023, 4095])]
+
+
+@pytest.mark.parametrize("heads,chunk,keys,together,apart", BESIDE)
+def test_many_sequences_beside_a_chunk(heads, chunk, keys, together, apart):
+    """Every work-group beside the 256-row tiles reads all sequences' lengths: thousands of sequences are taken apart."""
+    for steps in together + apart:
+        tiles, beside, alone = paged_route(steps + 1, steps + chunk, chunk, 64, 200, 0, vico.VICO_FULL_HISTORY, keys, HEADS[heads])[:3]
+        assert tiles > 0 and (beside > 0) == (steps in together) and (alone > 0) == (steps in apart), steps

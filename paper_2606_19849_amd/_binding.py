@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import importlib.util
+import operator
 import os
 import re
 import warnings
@@ -34,6 +35,24 @@ VICO_ROPE_ADJACENT = 1
 VICO_ROPE_STRIDED_AXES = 2
 
 _i32, _i64, _f32, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
+
+
+
+class _Whole32:
+    """An argument type that refuses what its C type has no room for (ctypes alone keeps the low bits)."""
+    kind, bits = _i32, 32
+
+    @classmethod
+    def from_param(cls, x):
+        n = operator.index(x)
+        if not -1 << (cls.bits - 1) <= n < 1 << (cls.bits - 1):
+            raise ValueError(f"{n} does not fit {cls.bits} bits")
+        return cls.kind(n)
+
+
+class _Whole64(_Whole32):
+    kind, bits = _i64, 64
+
 
 _SIGNATURES = {
     "vico_kv_append": (_i32, [_vp, _vp, _i32, _vp, _vp, _i32, _i64, _i32, _i32, _vp]),
@@ -104,7 +123,7 @@ def load_library():
         lib = ctypes.CDLL(LIB_PATH)
         for name, (res, args) in _SIGNATURES.items():
             fn = getattr(lib, name)
-            fn.restype, fn.argtypes = res, args
+            fn.restype, fn.argtypes = res, [{_i32: _Whole32, _i64: _Whole64}.get(a, a) for a in args]
         _lib = lib
     return _lib
 

@@ -17,6 +17,8 @@
 #include <ATen/core/Tensor.h>
 #include <c10/hip/HIPStream.h>
 
+#include <stdexcept>
+
 #include "vico_cache.h"
 #include "vico_pages.h"
 
@@ -106,7 +108,12 @@ struct Args {
 // second gives a copy-on-write tensor memory of its own first.
 void* ptr(const at::Tensor* t) { return t && t->numel() > 0 ? const_cast<void*>(t->const_data_ptr()) : nullptr; }
 void* wptr(const at::Tensor* t) { return t && t->numel() > 0 ? t->mutable_data_ptr() : nullptr; }
-int32_t size(const at::Tensor* t, int d) { return t ? (int32_t)t->size(d) : 0; }
+// A size that the interface has no room for is a case for the general path, which refuses it.
+int32_t size(const at::Tensor* t, int d) {
+  const int64_t n = t ? t->size(d) : 0;
+  if (n != (int32_t)n) throw std::out_of_range("size");
+  return (int32_t)n;
+}
 int64_t bytes(const at::Tensor* t) { return t ? t->numel() * (int64_t)t->element_size() : 0; }
 bool shape3(const at::Tensor* t, int64_t a, int64_t b, int64_t c) {
   return t->size(0) == a && t->size(1) == b && t->size(2) == c;
@@ -507,8 +514,7 @@ PyObject* pages_compact(PyObject* const* args, Py_ssize_t n) {
   const at::Tensor *pt = in.tensor(at::kInt, 2), *refs = in.tensor(at::kInt, 1), *mv = in.tensor(at::kInt, 2), *cnt = in.tensor(at::kInt, 1);
   const at::Tensor* ws = in.memory(true);
   void* stream = in.stream();
-  if (!in.ok || mv->size(1) != 2 || !shape1(cnt, 1) || !here(pt, refs, mv, cnt, ws) || !fits(pt) || mv->size(0) != size(mv, 0))
-    Py_RETURN_NONE;
+  if (!in.ok || mv->size(1) != 2 || !shape1(cnt, 1) || !here(pt, refs, mv, cnt, ws) || !fits(pt)) Py_RETURN_NONE;
   void *const t = wptr(pt), *const r = wptr(refs), *const m = wptr(mv), *const c = wptr(cnt), *const w = wptr(ws);
   return called(in, [&] {
     return vico_pages_compact((int32_t*)t, size(pt, 0), size(pt, 1), (int32_t*)r, size(refs, 0), (int32_t*)m, size(mv, 0),
@@ -524,7 +530,7 @@ PyObject* pages_copy(PyObject* const* args, Py_ssize_t n) {
   const at::Tensor* cnt = in.tensor(at::kInt, 1, true);
   void* stream = in.stream();
   if (!in.ok || !same_shape(kp, vp) || mv->size(1) != 2 || (cnt && !shape1(cnt, 1)) || !here(kp, vp, mv, cnt)) Py_RETURN_NONE;
-  if (!fits(kp) || mv->size(0) != size(mv, 0)) Py_RETURN_NONE;
+  if (!fits(kp)) Py_RETURN_NONE;
   void *const a = wptr(kp), *const b = wptr(vp);
   return called(in, [&] {
     return vico_pages_copy(a, b, l ? size(kp, 0) : 1, size(kp, l), size(kp, l + 1), size(kp, l + 2), size(kp, l + 3),

@@ -40,8 +40,13 @@
  *                     calls' q, k, v and out, and take positions seq_len[b] ...
  * The caller moves seq_len on after the last layer.  All of these live in device
  * memory, so the device checks them: a position without a page is neither
- * written nor attended to, rows outside [0, total) do not exist.  A table or pool
- * without an entry is VICO_ERR_CAPACITY where a call has something to do with it.
+ * written nor attended to, rows outside [0, total) do not exist.
+ *
+ * A table or pool without an entry is VICO_ERR_CAPACITY to attention, fork and
+ * reserve where they have a sequence to work for, a pool without one also to
+ * compaction, and to free where the table has entries.  It is no error to append
+ * (no position has a page), to copy (no pair names one) and, for the table, to
+ * free: those have nothing to do and return VICO_OK.
  */
 #ifndef VICO_PAGES_H
 #define VICO_PAGES_H

@@ -32,3 +32,14 @@ def test_many_sequences_beside_a_chunk(heads, chunk, keys, together, apart):
     for steps in together + apart:
         tiles, beside, alone = paged_route(steps + 1, steps + chunk, chunk, 64, 200, 0, vico.VICO_FULL_HISTORY, keys, HEADS[heads])[:3]
         assert tiles > 0 and (beside > 0) == (steps in together) and (alone > 0) == (steps in apart), steps
+
+
+def test_what_a_pool_or_table_without_an_entry_is_to_each_call():
+    from tests import test_pages_host as host
+    for none in (dict(N=0), dict(width=0)):
+        for call, status in ((host._attn, -3), (host._fork, -3), (host._reserve, -3), (host._append, 0)):
+            assert call(**none) == status
+    assert host._free(width=0) == 0 and host._free(N=0) == -3
+    assert host._compact(N=0, most=0) == -3 and host._copy(N=0) == 0
+    # without a sequence or a token there is nothing to do either way
+    assert host._attn(total=0, N=0) == host._fork(B=0, N=0) == host._reserve(B=0, width=0) == host._free(B=0, N=0) == 0

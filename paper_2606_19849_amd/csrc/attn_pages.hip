@@ -8,12 +8,13 @@
 //
 // Calls of one class, or of the first two, have kernels of four waves of which a CU
 // holds several, so that one's start is hidden behind another's keys.  With
-// the third, one launch does all (of hundreds of sequences two do, rows_apart): work-groups of the matrix cores first, which are
+// the third, one launch does all: work-groups of the matrix cores first, which are
 // long, then those that stream keys, in parts that count both (paged_tile_cost).  Every
 // work-group reads all lengths, a sequence a lane, and takes its own from the lanes.
 // (A chunk of 1024 tokens beside 31 answer tokens, 7B heads, windows of 8192 keys: 206 us, 141
 // and 99 each alone; 220 to 228 in parts for the chunk alone; 362 in two launches and
-// two merges, row tiles of 32 for the answer tokens.)
+// two merges, row tiles of 32 for the answer tokens.)  Of hundreds of sequences the
+// lengths take longer than the streams gain, and there are two launches (rows_apart).
 
 #include "attn_rows_pages.h"
 #include "attn_tile_pages.h"

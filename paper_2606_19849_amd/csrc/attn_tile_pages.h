@@ -217,7 +217,8 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, const LaneSeq
   const int sink = s.sink, first = s.first;
   // Tiles [t_plain, t_plain + n_plain) need no mask for this wave, and [t_plain, t_plain + n_whole) none for any row of
   // the work-group: behind those that hold positions between sink and window, before the causal diagonal.  A page that
-  // is none makes all tiles from there on masked ones.
+  // is none makes all tiles from there on masked ones.  (The sink's own tiles are masked ones: no matter at 64 tokens of it,
+  // 10 % of a 2048-token chunk over 16448 keys of which 4096 are the sink's, 7B heads: 520 us for 472.)
   const int t_plain = sink < first ? tiles.of_sink + 1 : 0;
   auto upto_whole = [&](int lim_) __attribute__((always_inline)) {      // tiles that lie wholly in positions <= lim_
     const int n = (lim_ + 1) / BN;
@@ -273,7 +274,9 @@ __device__ __forceinline__ void paged_tile(const PagedAttnArgs& a, const LaneSeq
   };
   u32x4 run_k = resource(late()->k_pages, 0), run_v = resource(late()->v_pages, 0);
   uint32_t run_at = 0, run_window = 0;       // of the tile to be loaded
-  bool far = false;                          // the 64 tiles lie in several windows: moved at each of them
+  // the 64 tiles lie in several windows: moved at each of them (2048 tokens over 16384 keys, 7B heads, pages all over a pool
+  // of 2, 5 and 10 GB: 464, 487 and 487 us; 455 in one of 19 MB)
+  bool far = false;
   auto start_tile = [&](int t) __attribute__((always_inline)) { run_at = __builtin_amdgcn_readlane(run_lo, (t - t_lo) & 63); };
   auto move_window = [&](uint32_t window) __attribute__((always_inline)) {
     if (window == run_window) return;

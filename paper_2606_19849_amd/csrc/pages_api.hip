@@ -67,7 +67,7 @@ void use_workspace(PagesArgs* a, void* workspace) {
 constexpr int kFewRows = 16;
 constexpr int64_t kMaxGroups = int64_t(1) << 23;                           // work-groups of a launch: fewer
 constexpr int kSomeRows = 64;                                              // more: 256-row tiles, in a launch that has them
-constexpr int kRowsOnly = 1024;                                            // a launch may do without them up to here
+constexpr int kRowsOnly = 1024;                                            // a launch may do without them up to here (rows_alone)
 constexpr int64_t kPagedWorkspace = int64_t(64) << 20;                     // most bytes of a split picked by the library
 
 int64_t items_bytes(int64_t items) { return align256(sizeof(TileItems) + items * sizeof(TileItem)); }
@@ -81,6 +81,11 @@ struct PagedPlan {
 int64_t partial_bytes(int64_t slots, int64_t rows, int64_t D) { return align256(slots * rows * D * 4) + align256(slots * rows * 4); }
 
 // A class of sequences with up to `rows` rows over `keys` keys, in work-groups of which `target` are wanted.
+// A part has eight 32-key blocks at least: two steps of each of four waves, 1.1 us each, where the merge's launch costs
+// 3.3.  (Least blocks of a part 4 / 8 / 16 / all in one, us: 7B heads, 35 rows over 500 keys 12.0 / 13.4 / 12.6 / 12.5,
+// over 1000 12.4 / 13.4 / 15.8 / 17.0, over 2000 12.3 / 14.6 / 17.9 / 25.8; four sequences of 70 rows over 1000 15.3 / 14.2 /
+// 16.4 / 17.7, over 2000 24.9 / 18.6 / 18.9 / 26.4; 3B heads, 144 rows over 1000 12.5 / 13.5 / 16.3 / 17.8; one token of 7B
+// heads over 500 9.5 / 10.5 / 9.6 / 9.6, over 2000 9.6 / 11.5 / 14.3 / 22.6, of 16 sequences over 2000 20.1 / 19.0 / 19.3 / 24.1.)
 bool plan_rows(RowsClass* x, int64_t least, int64_t rows, int tile_rows, int64_t B, int64_t Hkv, int64_t keys, int64_t target,
                int splits) {
   x->least = (int)least;
@@ -109,6 +114,10 @@ bool plan_rows(RowsClass* x, int64_t least, int64_t rows, int tile_rows, int64_t
 // 25.9 / 36.6, 511 rows 34.0 / 42.2, over 40000 keys 108.5 / 83.6; eight of 35 rows over 8000 keys 42.3 / 39.9, of 70
 // rows 55.7 / 41.1, of 252 rows over 1000 keys 32.2 / 37.7, over 8000 keys 93.9 / 60.2; 3B heads, eight of 144 rows over
 // 8000 keys 50.1 / 41.5; small heads, one of 292 rows over 8000 keys 14.7 / 25.5, eight 47.9 / 37.9.
+// Past kRowsOnly the 256-row tiles win nearly everywhere, and these formulas, which know no more than the streams, do not
+// see it: one sequence over 300 keys, 7B heads, 1050 rows 36.3 / 22.9, 2100 rows 67.3 / 26.7; 3B heads, 1200 rows 25.2 / 22.8,
+// over 1000 keys 26.4 / 30.6, 2400 rows 37.2 / 26.2; small heads, 1200 rows 15.3 / 18.8, over 1000 keys 15.2 / 23.6, four of
+// them 28.4 / 26.9, 2800 rows 30.5 / 24.9.
 bool rows_alone(int64_t B, int64_t rows, int64_t all, int64_t Hkv, int64_t keys, int D) {
   if (rows > kRowsOnly) return false;
   const double tiles32 = double(Hkv) * (double(all) / 32 + double(B));

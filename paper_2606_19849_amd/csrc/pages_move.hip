@@ -7,8 +7,8 @@
 // memory latencies whatever the number of sequences up to 64, four up to 4096.
 // Copy: a page of one layer is cut into pieces of 16 KB, four units a thread, all of a
 // piece's loads on their way together.
-// Alone: append of 32 tokens (7B heads) 2.8 us, of 18.5k tokens in 16 chunks (3B heads, 38 MB)
-// 7.0, 5.4 TB/s; copy of 905 pages (237 MB) 36, 6.5 TB/s (some of it from the caches).
+// Alone: append of 32 tokens (7B heads) 2.7 us, of 18.5k tokens in 16 chunks (3B heads, 38 MB)
+// 7.0 to 7.4, 5.1 to 5.4 TB/s; copy of 905 pages (237 MB) 36.6, 6.5 TB/s (some of it from the caches).
 
 #include <algorithm>
 

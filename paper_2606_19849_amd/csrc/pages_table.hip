@@ -13,9 +13,9 @@
 // The second launch changes reference counts, so it decides by the flags alone.
 // The tables are small (a 2048-page pool: 8 KB of counts): launches and memory
 // latencies bound these calls, so where one work-group can hold the flags it does all in
-// one launch.  Alone, us: 16 of 32 rows of 186 entries forked 4.4, new tokens of 16 rows
-// in a pool of 1678 pages reserved 5.2; of a pool of 3751 pages a part freed 3.2 to 4.5,
-// flags 2.3, compacted 5.3.
+// one launch.  Alone, us: 16 of 32 rows of 186 entries forked 4.3, new tokens of 16 rows
+// in a pool of 1678 pages reserved 5.0; of a pool of 3751 pages a part freed 3.9 to 4.6,
+// flags 2.7 to 4.6, compacted 5.1 to 5.9.
 
 #include <algorithm>
 

@@ -81,13 +81,13 @@ struct PagedPlan {
 int64_t partial_bytes(int64_t slots, int64_t rows, int64_t D) { return align256(slots * rows * D * 4) + align256(slots * rows * 4); }
 
 // A class of sequences with up to `rows` rows over `keys` keys, in work-groups of which `target` are wanted.
-// A part has eight 32-key blocks at least: two steps of each of four waves, 1.1 us each, where the merge's launch costs
-// 3.3.  (Least blocks of a part 4 / 8 / 16 / all in one, us: 7B heads, 35 rows over 500 keys 12.0 / 13.4 / 12.6 / 12.5,
+// A part has two steps of each wave at least, 1.1 us each, where the merge's launch costs 3.3: eight 32-key blocks on the
+// kernels of four waves, sixteen beside 256-row tiles.  (Four waves, least blocks of a part 4 / 8 / 16 / all in one, us: 7B heads, 35 rows over 500 keys 12.0 / 13.4 / 12.6 / 12.5,
 // over 1000 12.4 / 13.4 / 15.8 / 17.0, over 2000 12.3 / 14.6 / 17.9 / 25.8; four sequences of 70 rows over 1000 15.3 / 14.2 /
 // 16.4 / 17.7, over 2000 24.9 / 18.6 / 18.9 / 26.4; 3B heads, 144 rows over 1000 12.5 / 13.5 / 16.3 / 17.8; one token of 7B
 // heads over 500 9.5 / 10.5 / 9.6 / 9.6, over 2000 9.6 / 11.5 / 14.3 / 22.6, of 16 sequences over 2000 20.1 / 19.0 / 19.3 / 24.1.)
-bool plan_rows(RowsClass* x, int64_t least, int64_t rows, int tile_rows, int64_t B, int64_t Hkv, int64_t keys, int64_t target,
-               int splits) {
+bool plan_rows(RowsClass* x, int64_t least, int64_t rows, int tile_rows, int waves, int64_t B, int64_t Hkv, int64_t keys,
+               int64_t target, int splits) {
   x->least = (int)least;
   x->most = (int)rows;
   x->tile_rows = tile_rows;
@@ -95,7 +95,7 @@ bool plan_rows(RowsClass* x, int64_t least, int64_t rows, int tile_rows, int64_t
   x->merge_rows = (int)std::min<int64_t>(rows, tile_rows);
   const int64_t groups = B * Hkv * x->n_rt, blocks = keys / kRowsBlock + 1;
   x->parts = splits > 0 ? std::min(splits, kPagedParts)
-                        : (int)std::max<int64_t>(std::min(std::min<int64_t>(kPagedParts, target / groups), blocks / 8), 1);
+                        : (int)std::max<int64_t>(std::min(std::min<int64_t>(kPagedParts, target / groups), blocks / (2 * waves)), 1);
   x->per_part = splits > 0 ? 1 : (int)((blocks + x->parts - 1) / x->parts);
   // (a launch has fewer than 2^32 threads: 512 a work-group, and 256 in the merge, with a row or more)
   const int64_t launched = (B * x->parts + 7) / 8 * 8 * Hkv * x->n_rt;
@@ -161,19 +161,21 @@ int check_paged_shape(int32_t B, int32_t total, int32_t max_q, int32_t page_size
   // room for their partial results.  One sequence is no exception: how many of the call's rows are its own stands in
   // device memory.  (7B heads, room for 2048 rows, us with all of them taken for the sequence's / as here: one token over
   // 8000 keys 77 / 13, over 262144 keys 3195 / 106, 300 tokens over 8000 keys 169 / 58; all 2048 over 16384 keys
-  // 449 to 453 / 450; where no key range is split, the merge's launch: 300 of 300 over 300 keys 26.7 / 28.5.)
+  // 449 to 453 / 450; 3B heads, 500 of 500 over 500 keys 33.2 / 35.2, the merge's launch.)
   const int64_t all = int64_t(total) * g;
   const bool tile = rows > kSomeRows && !rows_alone(B, rows, all, Hkv, keys, D);
   const int64_t some_most = tile ? kSomeRows : rows;
   const int64_t groups = int64_t(B) * Hkv;
   pl->apart = tile && rows_apart(B, Hkv, splits);
   const bool beside = tile && !pl->apart;
+  const int waves = beside ? 8 : 4;
   const int64_t target = beside ? std::min<int64_t>(std::max<int64_t>(8 * groups, kNumCUs), 4 * kNumCUs)
                                 : (B == 1 ? 2 : rows > kFewRows ? 4 : 12) * kNumCUs;
-  if (!plan_rows(&pl->few, 1, std::min<int64_t>(rows, kFewRows), 16, B, Hkv, keys, target, splits)) return VICO_ERR_INVALID_ARG;
+  if (!plan_rows(&pl->few, 1, std::min<int64_t>(rows, kFewRows), 16, waves, B, Hkv, keys, target, splits)) return VICO_ERR_INVALID_ARG;
   if (pl->few.parts > 1) pl->few_ws = partial_bytes(pl->few.slots, 16, D);
   if (rows > kFewRows) {
-    if (!plan_rows(&pl->some, kFewRows + 1, some_most, beside ? 16 : 32, B, Hkv, keys, beside ? std::min<int64_t>(target, kNumCUs / 4) : target, splits))
+    if (!plan_rows(&pl->some, kFewRows + 1, some_most, beside ? 16 : 32, waves, B, Hkv, keys,
+                   beside ? std::min<int64_t>(target, kNumCUs / 4) : target, splits))
       return VICO_ERR_INVALID_ARG;
     if (pl->some.parts > 1) pl->some_ws = partial_bytes(pl->some.slots, pl->some.tile_rows, D);
   }
